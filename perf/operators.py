@@ -311,7 +311,7 @@ def _attend_plain(s, q):
 
 
 def _sample_plain(s):
-    """The operator in whole weights: w = 2^32 exp((x - max) / T), rounded."""
+    """The operator in whole weights: w = 2^31 exp((x - max) / T), rounded."""
     x = s["logits"].float()
     rows, vocab = x.shape
     x = torch.where(torch.isnan(x), -math.inf, x)
@@ -328,7 +328,7 @@ def _sample_plain(s):
     top = x[:, :1]
     d = torch.where(x == top, torch.zeros((), device="cuda"), (top - x) * (1.0 / t)[:, None])
     e = torch.exp(-d)
-    w = torch.round(e * 4294967296.0).long()
+    w = torch.round(e * 2147483648.0).long()
     w = w * (torch.arange(vocab, device="cuda")[None, :] < k[:, None])
     mass = torch.cumsum(w, 1)
     need = torch.ceil(top_p.double() * mass[:, -1].double())
@@ -341,7 +341,7 @@ def _sample_plain(s):
     r = torch.minimum(r, total - 1)
     token = (mass <= r[:, None]).sum(1)
     d = torch.zeros_like(d).scatter_(1, order, d)
-    share = (total.double() * 2.0 ** -32).float()
+    share = (total.double() * 2.0 ** -31).float()
     logprob = -d.gather(1, token[:, None])[:, 0] - torch.log(share)
     return {"token": token.to(torch.int32), "logprob": logprob}
 
@@ -427,7 +427,7 @@ def _exact_sample(s):
             logprob.append(0.0)
             continue
         e = torch.exp((x - x.max()) / t)
-        w = torch.round(e * 2.0 ** 32).long()
+        w = torch.round(e * 2.0 ** 31).long()
         order = torch.argsort(x, descending=True, stable=True)
         k = value["top_k"][n] if value["top_k"] is not None and 0 < value["top_k"][n] < vocab else vocab
         kept = order[:k]
@@ -443,5 +443,5 @@ def _exact_sample(s):
         r = min(max(0, int(u[n] * total)), total - 1)
         i = int(kept[int(torch.searchsorted(mass, r, right=True))])
         token.append(i)
-        logprob.append(math.log(float(e[i])) - math.log(total / 2.0 ** 32))
+        logprob.append(math.log(float(e[i])) - math.log(total / 2.0 ** 31))
     return {"token": torch.tensor(token, dtype=torch.int32), "logprob": torch.tensor(logprob, dtype=torch.float64)}
