@@ -51,8 +51,12 @@ typedef enum {
   P4Q_ERR_WORKSPACE_TOO_SMALL = 4,  /* ws_bytes below the queried size */
   P4Q_ERR_CUDA = 5,                 /* a CUDA runtime / launch error */
   P4Q_ERR_TIMEOUT = 6,              /* a bounded device wait ran out */
-  P4Q_ERR_NO_DEVICE = 7             /* no sm_103 device current */
+  P4Q_ERR_NO_DEVICE = 7,            /* no sm_103 device current */
+  P4Q_ERR_INDEX = 8                 /* a kernel met an index outside its table (p4q_device_status) */
 } p4q_status;
+
+/* Element types of the generation operators below (elsewhere fp16 is implied). */
+typedef enum { P4Q_F16 = 0, P4Q_BF16 = 1, P4Q_F32 = 2 } p4q_dtype;
 
 /* Budget split of the selector (Sec. 3.2: alpha = 0.3, beta = 0.2, gamma =
  * 0.5). K_q = floor(alpha_permille * K / 1000) tokens go to query relevance,
@@ -75,7 +79,8 @@ const char* p4q_status_string(p4q_status s);
 
 /* Reads and clears the device error word of the current device after
  * synchronizing `stream`. Returns P4Q_ERR_TIMEOUT if a bounded device wait ran
- * out since the last call, P4Q_ERR_CUDA on a CUDA error, else P4Q_OK. */
+ * out since the last call, else P4Q_ERR_INDEX if a kernel met an index outside
+ * its table, P4Q_ERR_CUDA on a CUDA error, else P4Q_OK. */
 p4q_status p4q_device_status(p4q_stream_t stream);
 
 /* Number of kernels this library has launched in the process so far (all
@@ -491,6 +496,107 @@ p4q_status p4q_select_gather_quant_expanded(const uint16_t* V, int B, int N, int
                                             const p4q_select_params* params, int32_t* idx, uint16_t* X,
                                             uint8_t* Xq, float* s_a, uint8_t* Xu, int32_t* sum_xu, void* ws,
                                             size_t ws_bytes, p4q_stream_t stream);
+
+/* ---------------------------------------------------------------------- */
+/* Generation: a paged key/value cache, attention of one new token over it, */
+/* and the draw of a token from logits                                      */
+/* ---------------------------------------------------------------------- */
+
+/* A paged key/value cache (App. B keeps keys and values in 16 bits) and the
+ * page table of the sequences a call is about. Position t of sequence b lies
+ * in slot t % page_size of page table[b * table_ld + t / page_size]; key and
+ * value of head h there are dh contiguous elements from
+ *   k (v) + page * page_stride + slot * token_stride + h * head_stride,
+ * so either order of slots and heads inside a page is a choice of strides.
+ * A host struct, read during the call; k, v and table are device pointers.
+ * Limits: dtype P4Q_F16 or P4Q_BF16; dh 64 or 128; page_size a power of two
+ * up to 65536; strides positive multiples of 8 elements, at least dh (offsets
+ * are computed in 64 bits); k and v 16-byte aligned, index arrays 4-byte aligned.
+ * A kernel checks every index it takes from device memory: one outside its
+ * table is not followed, and the next p4q_device_status() reports
+ * P4Q_ERR_INDEX. */
+typedef struct {
+  void* k;               /* [pages] pages of keys */
+  void* v;               /* [pages] pages of values */
+  const int32_t* table;  /* [seqs, table_ld] page numbers, columns 0 .. table_cols - 1 */
+  int64_t page_stride, token_stride, head_stride;  /* elements, alike for k and v */
+  int32_t dtype;         /* p4q_dtype of k, v and of the call's rows */
+  int32_t pages, page_size, Hkv, dh;
+  int32_t seqs, table_ld, table_cols;
+} p4q_paged_kv;
+
+/* Rotates q and k by their positions and appends k and v to the cache, for
+ * T tokens (a decode step's one per sequence, or the packed tokens of any
+ * number of prompts). Token i belongs to sequence seq[i] (seq NULL: i) and
+ * takes its position pos[i]; it is rotated by position rot_pos[i] (rot_pos
+ * NULL: pos[i]; the kept tokens of a pruned prompt keep their original
+ * positions). Per head, pair j < rot / 2 of dimensions (a, b) = (j, j + rot / 2),
+ * or (2 j, 2 j + 1) with interleaved != 0, becomes
+ *   (x_a c - x_b s, x_b c + x_a s),  c, s = cos, sin[rot position, j],
+ * computed in fp32 and rounded once; dimensions from rot on and v are copied.
+ * A token with pos[i] < 0 is padding: nothing of it is written. A token with an
+ * index outside its table is not written either (P4Q_ERR_INDEX, see above). Two
+ * tokens for one slot of a call leave one of them there, which one is not said.
+ *   q     [T, ldq], k, v [T, ldk / ldv]   kv->dtype, H and kv->Hkv heads of dh
+ *   cos, sin  [max_pos, rot / 2] fp32
+ *   pos, rot_pos, seq  [T] int32
+ *   q_out [T, ldqo] rotated q, and k_out [T, ldko] rotated k or NULL (written;
+ *         each may be its input with its input's pitch)
+ * Requires rot % 16 == 0, 16 <= rot <= dh, H <= 65535, every ld % 8 == 0 and
+ * at least its row's heads * dh, 16-byte aligned rows and tables of cos and sin.
+ * T == 0 is a no-op. */
+p4q_status p4q_rope_append(const uint16_t* q, int ldq, const uint16_t* k, int ldk, const uint16_t* v, int ldv, int T,
+                           int H, const float* cos, const float* sin, int max_pos, int rot, int interleaved,
+                           const int32_t* pos, const int32_t* rot_pos, const int32_t* seq, const p4q_paged_kv* kv,
+                           uint16_t* q_out, int ldqo, uint16_t* k_out, int ldko, p4q_stream_t stream);
+
+/* Attention of one new token per sequence over its cached positions:
+ *   o[b, h] = sum_{j < lens[b]} p_j v_j,  p = softmax_j(scale q[b, h] . k_j),
+ * with key/value head h / (H / Hkv), and lse[b, h] = ln sum_j exp(scale q . k_j).
+ * A sequence with lens[b] <= 0 has o = 0 and lse = -inf. Positions from lens[b]
+ * on are not read. fp32 products, softmax and sums; o rounded once.
+ * A length beyond the page table's columns is cut to them, and the positions of
+ * a page outside the cache count as masked (both P4Q_ERR_INDEX).
+ *   q, o  [kv->seqs, ldq / ldo] kv->dtype, H heads of dh (o written)
+ *   lens  [kv->seqs] int32
+ *   lse   [kv->seqs, H] fp32, written, or NULL
+ *   ws    device workspace of p4q_paged_attention_workspace_bytes() bytes,
+ *         16-byte aligned, filled with zeros before its first use; each call
+ *         leaves it ready for the next, of any sizes. Calls that may overlap on the
+ *         GPU (on different streams) need a workspace each.
+ * Requires H % Hkv == 0, H <= 65535, a finite scale, ld % 8 == 0 and >= H * dh,
+ * 16-byte aligned rows. kv->seqs == 0 is a no-op. */
+size_t p4q_paged_attention_workspace_bytes(void);
+p4q_status p4q_paged_attention(const uint16_t* q, int ldq, int H, const p4q_paged_kv* kv, const int32_t* lens,
+                               float scale, uint16_t* o, int ldo, float* lse, void* ws, size_t ws_bytes,
+                               p4q_stream_t stream);
+
+/* Draws one token from each row of logits with a given uniform number. With
+ * x_max the row's largest logit and T its temperature:
+ *   d_i = 0 where x_i = x_max, else (x_max - x_i) * (1 / T)    (fp32)
+ *   w_i = 2^31 exp(-d_i) rounded to an integer, so that sums of weights are
+ *         exact and the result depends on no order of summation;
+ *   the tokens by falling logit, ties by rising index, cut to their first top_k
+ *   (top_k <= 0 or >= vocab: all), of these to the shortest head whose weights
+ *   reach max(1, ceil(top_p * their sum)) (top_p >= 1: all), and of these
+ *   to exp(-d_i) >= min(min_p, 1);
+ *   token = the first i, by index, at which the kept weights up to i exceed
+ *   min(floor(u * total), total - 1), total being the kept weights' sum.
+ * T <= 0 (or NaN): the first largest logit. NaN logits count as -inf; where
+ * x_max = +inf only the logits of that value have weight. A row of nothing but
+ * -inf has token -1 and logprob -inf. u outside [0, 1) draws the nearest token.
+ *   logits  [rows, ld] dtype (any p4q_dtype), aligned to their element only
+ *   temperature, top_k, top_p, min_p  [rows] (fp32; int32 top_k), each or NULL
+ *           for T = 1 or no such cut; u [rows] fp32
+ *   token   [rows] int32, written
+ *   logprob [rows] fp32: the logarithm of the share w_i / total with which the
+ *           token was drawn, -d_i - ln(total / 2^31); written, or NULL
+ * Requires 1 <= vocab <= P4Q_MAX_VOCAB, ld >= vocab, rows <= 65535, 4-byte
+ * aligned parameter and output arrays. rows == 0 is a no-op. */
+#define P4Q_MAX_VOCAB 262144
+p4q_status p4q_sample(const void* logits, int dtype, int64_t ld, int rows, int vocab, const float* temperature,
+                      const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* token,
+                      float* logprob, p4q_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -217,6 +217,40 @@ p4q_status check_gemm(const void* Xq, int M, int Kin, const void* Wq, int N, con
   return P4Q_OK;
 }
 
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// Checks a caller's cache description and copies it for the kernels. `used`:
+// the call has rows, so the pointers are needed.
+p4q_status check_paged(const p4q_paged_kv* kv, bool used, PagedCache* out) {
+  if (!kv || kv->pages < 0 || kv->page_size < 1 || kv->Hkv < 1 || kv->dh < 1 || kv->seqs < 0 || kv->table_cols < 0 ||
+      kv->table_ld < kv->table_cols)
+    return P4Q_ERR_INVALID_ARG;
+  if (used && (!kv->k || !kv->v || !kv->table)) return P4Q_ERR_INVALID_ARG;
+  if (kv->page_stride < kv->dh || kv->token_stride < kv->dh || kv->head_stride < kv->dh) return P4Q_ERR_INVALID_ARG;
+  if ((kv->dtype != P4Q_F16 && kv->dtype != P4Q_BF16) || (kv->dh != 64 && kv->dh != 128) || kv->Hkv > 65535 ||
+      kv->page_size > 65536 || (kv->page_size & (kv->page_size - 1)) != 0)
+    return P4Q_ERR_UNSUPPORTED_SHAPE;
+  if (kv->page_stride % 8 != 0 || kv->token_stride % 8 != 0 || kv->head_stride % 8 != 0 || !aligned16(kv->k) ||
+      !aligned16(kv->v) || !aligned4(kv->table))
+    return P4Q_ERR_MISALIGNED;
+  out->k = static_cast<uint16_t*>(kv->k);
+  out->v = static_cast<uint16_t*>(kv->v);
+  out->table = kv->table;
+  out->page_stride = kv->page_stride;
+  out->token_stride = kv->token_stride;
+  out->head_stride = kv->head_stride;
+  out->pages = kv->pages;
+  out->page_log2 = 0;
+  while ((1 << out->page_log2) < kv->page_size) ++out->page_log2;
+  out->Hkv = kv->Hkv;
+  out->dh = kv->dh;
+  out->seqs = kv->seqs;
+  out->table_ld = kv->table_ld;
+  out->table_cols = kv->table_cols;
+  out->bf16 = kv->dtype == P4Q_BF16;
+  return P4Q_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -231,6 +265,7 @@ const char* p4q_status_string(p4q_status s) {
     case P4Q_ERR_CUDA: return "CUDA error";
     case P4Q_ERR_TIMEOUT: return "a bounded device wait timed out";
     case P4Q_ERR_NO_DEVICE: return "no sm_103 device is current";
+    case P4Q_ERR_INDEX: return "a kernel met an index outside its table";
   }
   return "unknown status";
 }
@@ -260,9 +295,11 @@ p4q_status p4q_set_gemm_variant(int variant) {
 p4q_status p4q_device_status(p4q_stream_t stream) {
   if (cudaStreamSynchronize(reinterpret_cast<cudaStream_t>(stream)) != cudaSuccess) return P4Q_ERR_CUDA;
   const unsigned int g = gemm_read_and_clear_error() | gemm8_read_and_clear_error() | quant_read_and_clear_error() |
-                         attn_read_and_clear_error() | fewrows_read_and_clear_error() | peak_read_and_clear_error() | diverse_read_and_clear_error();
+                         attn_read_and_clear_error() | fewrows_read_and_clear_error() | peak_read_and_clear_error() |
+                         diverse_read_and_clear_error();
+  const unsigned int i = rope_read_and_clear_error() | paged_read_and_clear_error();
   if (cudaGetLastError() != cudaSuccess) return P4Q_ERR_CUDA;
-  return g ? P4Q_ERR_TIMEOUT : P4Q_OK;
+  return g ? P4Q_ERR_TIMEOUT : i ? P4Q_ERR_INDEX : P4Q_OK;
 }
 
 p4q_status p4q_test_wait_timeout(uint32_t limit_us, p4q_stream_t stream) {
@@ -352,6 +389,108 @@ p4q_status p4q_causal_attention(const uint16_t* q, int ldq, const uint16_t* k, i
   if (st != P4Q_OK) return st;
   return from_cuda(counted(launch_causal_attention(q, ldq, k, ldk, v, ldv, B, m, H, Hkv, o, ldo,
                                                    reinterpret_cast<cudaStream_t>(stream))));
+}
+
+p4q_status p4q_rope_append(const uint16_t* q, int ldq, const uint16_t* k, int ldk, const uint16_t* v, int ldv, int T,
+                           int H, const float* cos, const float* sin, int max_pos, int rot, int interleaved,
+                           const int32_t* pos, const int32_t* rot_pos, const int32_t* seq, const p4q_paged_kv* kv,
+                           uint16_t* q_out, int ldqo, uint16_t* k_out, int ldko, p4q_stream_t stream) {
+  RopeArgs a;
+  p4q_status st = check_paged(kv, T > 0, &a.kv);
+  if (st != P4Q_OK) return st;
+  if (T < 0 || H < 1 || max_pos < 1 || rot < 1) return P4Q_ERR_INVALID_ARG;
+  if (rot % 16 != 0 || rot > kv->dh || H > 65535) return P4Q_ERR_UNSUPPORTED_SHAPE;
+  const int nq = H * kv->dh, nk = kv->Hkv * kv->dh;
+  if (ldq < nq || ldk < nk || ldv < nk || ldqo < nq || (k_out && ldko < nk)) return P4Q_ERR_INVALID_ARG;
+  if (T > 0 && (!q || !k || !v || !cos || !sin || !pos || !q_out)) return P4Q_ERR_INVALID_ARG;
+  if (!seq && T > kv->seqs) return P4Q_ERR_INVALID_ARG;
+  if (ldq % 8 != 0 || ldk % 8 != 0 || ldv % 8 != 0 || ldqo % 8 != 0 || (k_out && ldko % 8 != 0))
+    return P4Q_ERR_MISALIGNED;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(cos) || !aligned16(sin) || !aligned16(q_out) ||
+      !aligned16(k_out) || !aligned4(pos) || !aligned4(rot_pos) || !aligned4(seq))
+    return P4Q_ERR_MISALIGNED;
+  if (T == 0) return P4Q_OK;
+  if ((st = check_device()) != P4Q_OK) return st;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.q_out = q_out;
+  a.k_out = k_out;
+  a.cos = cos;
+  a.sin = sin;
+  a.pos = pos;
+  a.rot_pos = rot_pos;
+  a.seq = seq;
+  a.ldq = ldq;
+  a.ldk = ldk;
+  a.ldv = ldv;
+  a.ldqo = ldqo;
+  a.ldko = ldko;
+  a.T = T;
+  a.H = H;
+  a.max_pos = max_pos;
+  a.rot = rot;
+  a.interleaved = interleaved != 0;
+  return from_cuda(counted(launch_rope_append(a, reinterpret_cast<cudaStream_t>(stream))));
+}
+
+size_t p4q_paged_attention_workspace_bytes(void) { return paged_attention_workspace_bytes(); }
+
+p4q_status p4q_paged_attention(const uint16_t* q, int ldq, int H, const p4q_paged_kv* kv, const int32_t* lens,
+                               float scale, uint16_t* o, int ldo, float* lse, void* ws, size_t ws_bytes,
+                               p4q_stream_t stream) {
+  PagedAttnArgs a;
+  p4q_status st = check_paged(kv, kv && kv->seqs > 0, &a.kv);
+  if (st != P4Q_OK) return st;
+  if (H < 1 || H % kv->Hkv != 0 || !(scale - scale == 0.0f)) return P4Q_ERR_INVALID_ARG;
+  if (H > 65535) return P4Q_ERR_UNSUPPORTED_SHAPE;
+  if (ldq < H * kv->dh || ldo < H * kv->dh) return P4Q_ERR_INVALID_ARG;
+  if (kv->seqs > 0 && (!q || !lens || !o)) return P4Q_ERR_INVALID_ARG;
+  if (ldq % 8 != 0 || ldo % 8 != 0 || !aligned16(q) || !aligned16(o) || !aligned4(lens) || !aligned4(lse))
+    return P4Q_ERR_MISALIGNED;
+  if (kv->seqs == 0) return P4Q_OK;
+  if (!ws || ws_bytes < paged_attention_workspace_bytes()) return P4Q_ERR_WORKSPACE_TOO_SMALL;
+  if (!aligned16(ws)) return P4Q_ERR_MISALIGNED;
+  if ((st = check_device()) != P4Q_OK) return st;
+  a.q = q;
+  a.o = o;
+  a.lse = lse;
+  a.lens = lens;
+  a.ldq = ldq;
+  a.ldo = ldo;
+  a.H = H;
+  a.scale = scale;
+  a.ws = ws;
+  return from_cuda(counted(launch_paged_attention(a, reinterpret_cast<cudaStream_t>(stream))));
+}
+
+p4q_status p4q_sample(const void* logits, int dtype, int64_t ld, int rows, int vocab, const float* temperature,
+                      const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* token,
+                      float* logprob, p4q_stream_t stream) {
+  if (rows < 0 || vocab < 1 || ld < vocab || dtype < P4Q_F16 || dtype > P4Q_F32) return P4Q_ERR_INVALID_ARG;
+  if (rows > 0 && (!logits || !u || !token)) return P4Q_ERR_INVALID_ARG;
+  if (vocab > P4Q_MAX_VOCAB || rows > 65535) return P4Q_ERR_UNSUPPORTED_SHAPE;
+  if ((reinterpret_cast<uintptr_t>(logits) & (dtype == P4Q_F32 ? 3u : 1u)) != 0 || !aligned4(temperature) ||
+      !aligned4(top_k) || !aligned4(top_p) || !aligned4(min_p) || !aligned4(u) || !aligned4(token) ||
+      !aligned4(logprob))
+    return P4Q_ERR_MISALIGNED;
+  if (rows == 0) return P4Q_OK;
+  p4q_status st = check_device();
+  if (st != P4Q_OK) return st;
+  SampleArgs a;
+  a.logits = logits;
+  a.ld = ld;
+  a.dtype = dtype;
+  a.rows = rows;
+  a.vocab = vocab;
+  a.temperature = temperature;
+  a.top_k = top_k;
+  a.top_p = top_p;
+  a.min_p = min_p;
+  a.u = u;
+  a.token = token;
+  a.logprob = logprob;
+  return from_cuda(counted(launch_sample(a, reinterpret_cast<cudaStream_t>(stream))));
 }
 
 size_t p4q_block_mse_workspace_bytes(int B) {

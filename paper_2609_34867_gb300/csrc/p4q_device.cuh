@@ -11,7 +11,7 @@
 namespace p4q {
 
 // Error bits written to a kernel's device error word.
-enum : unsigned int { kErrTimeout = 1u };
+enum : unsigned int { kErrTimeout = 1u, kErrIndex = 2u };
 
 // A bounded device wait gives up after this many nanoseconds.
 constexpr unsigned long long kWaitLimitNs = 4000000000ull;

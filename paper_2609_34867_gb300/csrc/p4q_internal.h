@@ -183,6 +183,66 @@ cudaError_t launch_causal_attention(const uint16_t* q, long long ldq, const uint
                                     long long ldo, cudaStream_t stream);
 unsigned int attn_read_and_clear_error();
 
+// ------------------------------------------------------------ generation: paged cache, attention over it, sampling
+// Reads an index table of device memory on the device: a kernel follows no page
+// outside the cache. Copied from p4q_paged_kv (page_size = 1 << page_log2).
+struct PagedCache {
+  uint16_t* k = nullptr;
+  uint16_t* v = nullptr;
+  const int32_t* table = nullptr;
+  long long page_stride = 0, token_stride = 0, head_stride = 0;
+  int pages = 0, page_log2 = 0, Hkv = 0, dh = 0, seqs = 0, table_ld = 0, table_cols = 0;
+  bool bf16 = false;
+};
+
+struct RopeArgs {
+  PagedCache kv;
+  const uint16_t* q = nullptr;
+  const uint16_t* k = nullptr;
+  const uint16_t* v = nullptr;
+  uint16_t* q_out = nullptr;
+  uint16_t* k_out = nullptr;  // may be null
+  const float* cos = nullptr;
+  const float* sin = nullptr;
+  const int32_t* pos = nullptr;
+  const int32_t* rot_pos = nullptr;  // null: pos
+  const int32_t* seq = nullptr;      // null: the token's own number
+  long long ldq = 0, ldk = 0, ldv = 0, ldqo = 0, ldko = 0;
+  int T = 0, H = 0, max_pos = 0, rot = 0;
+  bool interleaved = false;
+};
+cudaError_t launch_rope_append(const RopeArgs& a, cudaStream_t stream);
+unsigned int rope_read_and_clear_error();
+
+struct PagedAttnArgs {
+  PagedCache kv;
+  const uint16_t* q = nullptr;
+  uint16_t* o = nullptr;
+  float* lse = nullptr;  // may be null
+  const int32_t* lens = nullptr;
+  long long ldq = 0, ldo = 0;
+  int H = 0;
+  float scale = 0.0f;
+  void* ws = nullptr;
+};
+size_t paged_attention_workspace_bytes();
+cudaError_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t stream);
+unsigned int paged_read_and_clear_error();
+
+struct SampleArgs {
+  const void* logits = nullptr;
+  long long ld = 0;
+  int dtype = 0, rows = 0, vocab = 0;
+  const float* temperature = nullptr;
+  const int32_t* top_k = nullptr;
+  const float* top_p = nullptr;
+  const float* min_p = nullptr;
+  const float* u = nullptr;
+  int32_t* token = nullptr;
+  float* logprob = nullptr;
+};
+cudaError_t launch_sample(const SampleArgs& a, cudaStream_t stream);
+
 // ------------------------------------------------------------ calibration data path
 constexpr int kMseMaxSamples = 1024;
 // CTAs per sample of the block-objective reduction, and its workspace (fp64 partials).

@@ -16,7 +16,8 @@ from . import build as _build
 
 P4Q_OK = 0
 STATUS_NAMES = {0: "P4Q_OK", 1: "P4Q_ERR_INVALID_ARG", 2: "P4Q_ERR_UNSUPPORTED_SHAPE", 3: "P4Q_ERR_MISALIGNED",
-                4: "P4Q_ERR_WORKSPACE_TOO_SMALL", 5: "P4Q_ERR_CUDA", 6: "P4Q_ERR_TIMEOUT", 7: "P4Q_ERR_NO_DEVICE"}
+                4: "P4Q_ERR_WORKSPACE_TOO_SMALL", 5: "P4Q_ERR_CUDA", 6: "P4Q_ERR_TIMEOUT", 7: "P4Q_ERR_NO_DEVICE",
+                8: "P4Q_ERR_INDEX"}
 
 
 class P4QError(RuntimeError):
@@ -28,6 +29,17 @@ class P4QError(RuntimeError):
 class SelectParams(ctypes.Structure):
     _fields_ = [("K", ctypes.c_int32), ("alpha_permille", ctypes.c_int32), ("beta_permille", ctypes.c_int32)]
 
+
+class PagedKV(ctypes.Structure):
+    """p4q_paged_kv: a paged key/value cache and the page table of a call's sequences."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("page_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("Hkv", ctypes.c_int32), ("dh", ctypes.c_int32), ("seqs", ctypes.c_int32),
+                ("table_ld", ctypes.c_int32), ("table_cols", ctypes.c_int32)]
+
+
+DTYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
 
 _lib = None
 
@@ -103,6 +115,15 @@ def lib() -> ctypes.CDLL:
         L.p4q_select_gather_quant.argtypes = [P, I, I, I, P, I, P, P, I, ctypes.POINTER(SelectParams), P, P, P,
                                               P, P, S, P]
         L.p4q_select_gather_quant.restype = st
+        L.p4q_rope_append.argtypes = [P, I, P, I, P, I, I, I, P, P, I, I, I, P, P, P, ctypes.POINTER(PagedKV), P, I, P, I,
+                                      P]
+        L.p4q_rope_append.restype = st
+        L.p4q_paged_attention_workspace_bytes.argtypes = []
+        L.p4q_paged_attention_workspace_bytes.restype = S
+        L.p4q_paged_attention.argtypes = [P, I, I, ctypes.POINTER(PagedKV), P, ctypes.c_float, P, I, P, P, S, P]
+        L.p4q_paged_attention.restype = st
+        L.p4q_sample.argtypes = [P, I, ctypes.c_int64, I, I, P, P, P, P, P, P, P, P]
+        L.p4q_sample.restype = st
         _lib = L
     return _lib
 
@@ -369,6 +390,153 @@ def cls_saliency(q_cls, k_cls, k, stream=None):
     A = torch.empty((q_cls.shape[0], k.shape[1]), dtype=torch.float32, device=k.device)
     p4q_cls_saliency(q_cls, k_cls, k, A, stream)
     return A
+
+
+# ---------------------------------------------------------------- generation
+def _rows16(t, dtype, cols, name):
+    """A CUDA 2-D tensor of `dtype` with unit column stride (a column block of a fused output, say)."""
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.dim() != 2 or not t.is_cuda or \
+            (t.stride(1) != 1 and t.shape[1] > 1):
+        raise TypeError(f"{name}: expected a CUDA {dtype} 2-D tensor with unit column stride")
+    if cols is not None and t.shape[1] != cols:
+        raise ValueError(f"{name} has {t.shape[1]} columns, expected {cols}")
+
+
+def _vector(t, dtype, n, name):
+    if t is None:
+        return
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.dim() != 1 or not t.is_cuda or \
+            (t.shape[0] > 1 and t.stride(0) != 1):
+        raise TypeError(f"{name}: expected a contiguous CUDA {dtype} vector")
+    if t.shape[0] != n:
+        raise ValueError(f"{name} has {t.shape[0]} entries, expected {n}")
+
+
+def _ld(t):
+    """Row pitch in elements (a single row's stride says nothing: its columns)."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], (t.shape[1] + 7) // 8 * 8)
+
+
+def paged_kv(k_cache, v_cache, table):
+    """The PagedKV of caches [pages, page_size, Hkv, dh] (any order of slots and
+    heads in memory, as strides; unit stride along dh) and a page table [seqs,
+    pages per sequence] int32."""
+    if not isinstance(k_cache, torch.Tensor) or k_cache.dtype not in (torch.float16, torch.bfloat16) or \
+            k_cache.dim() != 4 or not k_cache.is_cuda or k_cache.stride(3) != 1:
+        raise TypeError("k_cache: expected a CUDA fp16 or bf16 tensor [pages, page_size, Hkv, dh], unit stride along dh")
+    if not isinstance(v_cache, torch.Tensor) or v_cache.dtype != k_cache.dtype or not v_cache.is_cuda or \
+            v_cache.shape != k_cache.shape or v_cache.stride() != k_cache.stride():
+        raise TypeError("v_cache: expected a CUDA tensor of k_cache's type, shape and strides")
+    if not isinstance(table, torch.Tensor) or table.dtype != torch.int32 or table.dim() != 2 or not table.is_cuda or \
+            (table.shape[1] > 1 and table.stride(1) != 1):
+        raise TypeError("table: expected a CUDA int32 2-D tensor with unit column stride")
+    pages, size, heads, dh = k_cache.shape
+    ps, ts, hs, _ = k_cache.stride()
+    seqs, cols = table.shape
+    return PagedKV(k_cache.data_ptr(), v_cache.data_ptr(), table.data_ptr(), ps if pages > 1 else max(ps, dh),
+                   ts if size > 1 else dh, hs if heads > 1 else dh, DTYPES[k_cache.dtype], pages, size, heads, dh,
+                   seqs, table.stride(0) if seqs > 1 else cols, cols)
+
+
+def p4q_rope_append(q, k, v, cos, sin, pos, k_cache, v_cache, table, q_out, k_out=None, seq=None, rot_pos=None,
+                    interleaved=False, stream=None):
+    """Rotates q and k of T tokens by their positions and appends k and v to the
+    paged cache. q, q_out [T, H*dh], k, v, k_out [T, Hkv*dh]: 2-D views of the
+    cache's type; cos, sin [positions, rot/2] fp32; pos, rot_pos, seq [T] int32;
+    caches and table as paged_kv(). q_out may be q, and k_out k."""
+    kv = paged_kv(k_cache, v_cache, table)
+    T, dt = q.shape[0], k_cache.dtype
+    _rows16(q, dt, None, "q"); _rows16(q_out, dt, q.shape[1], "q_out")
+    for t, name in ((k, "k"), (v, "v"), (k_out, "k_out")):
+        if t is not None:
+            _rows16(t, dt, kv.Hkv * kv.dh, name)
+    if q.shape[1] % kv.dh:
+        raise ValueError(f"q has {q.shape[1]} columns, not a multiple of the head dimension {kv.dh}")
+    if k.shape[0] != T or v.shape[0] != T or q_out.shape[0] != T or (k_out is not None and k_out.shape[0] != T):
+        raise ValueError("q, k, v and the outputs differ in rows")
+    _need(cos, torch.float32, 2, "cos"); _need(sin, torch.float32, 2, "sin")
+    if cos.shape != sin.shape:
+        raise ValueError("cos and sin differ in shape")
+    if pos is None:
+        raise TypeError("pos: expected a contiguous CUDA torch.int32 vector")
+    _vector(pos, torch.int32, T, "pos"); _vector(rot_pos, torch.int32, T, "rot_pos")
+    _vector(seq, torch.int32, T, "seq")
+    _check(lib().p4q_rope_append(_ptr(q), _ld(q), _ptr(k), _ld(k), _ptr(v), _ld(v), T, q.shape[1] // kv.dh, _ptr(cos),
+                                 _ptr(sin), cos.shape[0], 2 * cos.shape[1], int(interleaved), _ptr(pos),
+                                 _ptr(rot_pos), _ptr(seq), ctypes.byref(kv), _ptr(q_out), _ld(q_out), _ptr(k_out),
+                                 0 if k_out is None else _ld(k_out), _stream(stream)), "p4q_rope_append")
+
+
+def p4q_paged_attention_workspace_bytes() -> int:
+    return int(lib().p4q_paged_attention_workspace_bytes())
+
+
+def paged_attention_workspace(device):
+    """A workspace for p4q_paged_attention (zeroed; one per stream)."""
+    return torch.zeros((p4q_paged_attention_workspace_bytes(),), dtype=torch.uint8, device=device)
+
+
+def p4q_paged_attention(q, k_cache, v_cache, table, lens, o, ws, scale=None, lse=None, stream=None):
+    """Attention of one new token per sequence over its lens[b] cached positions.
+    q, o [seqs, H*dh]: 2-D views of the cache's type; lens [seqs] int32; lse
+    [seqs, H] fp32 or None; scale defaults to 1 / sqrt(dh); ws as
+    paged_attention_workspace() gives it; caches and table as paged_kv()."""
+    kv = paged_kv(k_cache, v_cache, table)
+    dt = k_cache.dtype
+    _rows16(q, dt, None, "q"); _rows16(o, dt, q.shape[1], "o")
+    H = q.shape[1] // kv.dh
+    if q.shape[1] % kv.dh:
+        raise ValueError(f"q has {q.shape[1]} columns, not a multiple of the head dimension {kv.dh}")
+    if q.shape[0] != kv.seqs or o.shape[0] != kv.seqs:
+        raise ValueError("q, o and the page table differ in sequences")
+    if lens is None:
+        raise TypeError("lens: expected a contiguous CUDA torch.int32 vector")
+    _vector(lens, torch.int32, kv.seqs, "lens")
+    _need(ws, torch.uint8, 1, "ws")
+    if lse is not None:
+        _need(lse, torch.float32, 2, "lse")
+        if lse.shape != (kv.seqs, H):
+            raise ValueError(f"lse has shape {tuple(lse.shape)}, expected {(kv.seqs, H)}")
+    _check(lib().p4q_paged_attention(_ptr(q), _ld(q), H, ctypes.byref(kv), _ptr(lens),
+                                     kv.dh ** -0.5 if scale is None else float(scale), _ptr(o), _ld(o), _ptr(lse),
+                                     _ptr(ws), ws.numel(), _stream(stream)), "p4q_paged_attention")
+
+
+def paged_attention(q, k_cache, v_cache, table, lens, ws=None, scale=None, stream=None):
+    """Allocating wrapper of p4q_paged_attention: returns o."""
+    if ws is None:
+        ws = paged_attention_workspace(q.device)
+    o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    p4q_paged_attention(q, k_cache, v_cache, table, lens, o, ws, scale, None, stream)
+    return o
+
+
+def p4q_sample(logits, u, token, logprob=None, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
+    """Draws token[n] from row n of logits ([rows, vocab] fp16, bf16 or fp32,
+    unit column stride) with the uniform number u[n]. u, logprob, temperature,
+    top_p, min_p [rows] fp32; token, top_k [rows] int32; all but u and token
+    optional."""
+    if not isinstance(logits, torch.Tensor) or logits.dtype not in DTYPES or logits.dim() != 2 or \
+            not logits.is_cuda or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise TypeError("logits: expected a CUDA fp16, bf16 or fp32 2-D tensor with unit column stride")
+    rows, vocab = logits.shape
+    if u is None or token is None:
+        raise TypeError("u and token are needed")
+    for t, dt, name in ((u, torch.float32, "u"), (token, torch.int32, "token"), (logprob, torch.float32, "logprob"),
+                        (temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"),
+                        (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p")):
+        _vector(t, dt, rows, name)
+    _check(lib().p4q_sample(_ptr(logits), DTYPES[logits.dtype], logits.stride(0) if rows > 1 else vocab, rows, vocab,
+                            _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(u), _ptr(token),
+                            _ptr(logprob), _stream(stream)), "p4q_sample")
+
+
+def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
+    """Allocating wrapper of p4q_sample: returns (token, logprob)."""
+    token = torch.empty((logits.shape[0],), dtype=torch.int32, device=logits.device)
+    logprob = torch.empty((logits.shape[0],), dtype=torch.float32, device=logits.device)
+    p4q_sample(logits, u, token, logprob, temperature, top_k, top_p, min_p, stream)
+    return token, logprob
 
 
 # ---------------------------------------------------------------- helpers
