@@ -461,7 +461,10 @@ p4q_status p4q_paged_attention(const uint16_t* q, int ldq, int H, const p4q_page
   a.H = H;
   a.scale = scale;
   a.ws = ws;
-  return from_cuda(counted(launch_paged_attention(a, reinterpret_cast<cudaStream_t>(stream))));
+  unsigned int launches = 0;
+  const cudaError_t e = launch_paged_attention(a, reinterpret_cast<cudaStream_t>(stream), &launches);
+  counted(cudaSuccess, launches);
+  return from_cuda(e);
 }
 
 p4q_status p4q_sample(const void* logits, int dtype, int64_t ld, int rows, int vocab, const float* temperature,

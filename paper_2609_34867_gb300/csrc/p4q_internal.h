@@ -226,7 +226,8 @@ struct PagedAttnArgs {
   void* ws = nullptr;
 };
 size_t paged_attention_workspace_bytes();
-cudaError_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t stream);
+// Adds the kernels it launches (one, or two where units are shared) to *launches.
+cudaError_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t stream, unsigned int* launches);
 unsigned int paged_read_and_clear_error();
 
 struct SampleArgs {

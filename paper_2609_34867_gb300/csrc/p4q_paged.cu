@@ -38,17 +38,20 @@ __device__ unsigned int g_paged_err;
 
 namespace {
 
-constexpr int kWarps = 8;
+constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
-constexpr int kMaxGrid = 512;    // CTAs of a launch at most (partial results of the workspace)
-constexpr int kMinTiles = 2;     // tiles per CTA at least, unless there are fewer
+constexpr int kMaxGrid = 640;    // CTAs of a launch at most (partial results of the workspace)
+constexpr int kMinTiles = 4;     // tiles per CTA at least, of one unit
+constexpr int kUnitCost = 2;     // what a unit costs beside its tiles, in tiles
 constexpr float kShift = 7.0f;   // p = 2^(score - reference + 7): small p keep their bits in fp16
 constexpr float kMove = 8.0f;    // a reference moves when a score exceeds it by 2^8
 
-// Workspace: a counter per CTA (zero between calls), then two partial results
-// per CTA: 16 maxima, 16 sums, 16 x 128 values.
+// Workspace: for each CTA the unit that begins in it and goes on in others
+// (batch index, unit, last CTA; last CTA -1: none), then two partial results per
+// CTA (of a unit that began before it, of one that goes on behind it): 16
+// maxima, 16 sums, 16 x 128 values.
 constexpr int kPartFloats = 32 + 16 * 128;
-constexpr size_t kWsBytes = kMaxGrid * sizeof(int) + static_cast<size_t>(kMaxGrid) * 2 * kPartFloats * sizeof(float);
+constexpr size_t kWsBytes = kMaxGrid * (sizeof(int4) + 2 * kPartFloats * sizeof(float));
 
 template <bool kBf16>
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -69,26 +72,57 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
   return d;
 }
 
+// A shared-memory load that stays where it is (not hoisted out of a loop).
+__device__ __forceinline__ uint4 reload16(const uint4* p) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(smem_u32(p)));
+  return v;
+}
+
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 
-__device__ __forceinline__ uint4 load16(const uint16_t* p, bool valid) {
-  return valid ? ldg_stream16(p) : make_uint4(0u, 0u, 0u, 0u);
+// Output of head h (dimensions d .. d + 3) and its logarithm of the sum, from
+// the reference maximum, the sum and the values against it.
+template <bool kBf16>
+__device__ __forceinline__ void write_out(const PagedAttnArgs& a, int b, int h, int d, float m, float sum, float4 v) {
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  uint2 w;
+  w.x = pack2<kBf16>(v.x * inv, v.y * inv);
+  w.y = pack2<kBf16>(v.z * inv, v.w * inv);
+  *reinterpret_cast<uint2*>(a.o + b * a.ldo + static_cast<long long>(h) * a.kv.dh + d) = w;
+  if (d == 0 && a.lse)
+    a.lse[static_cast<long long>(b) * a.H + h] = sum == 0.0f ? -INFINITY : (m - kShift) * 0.6931471805599453f + logf(sum);
 }
 
-struct Plan {  // what a CTA computes from the lengths
-  long long total;   // tiles of all units
-  long long first;   // this CTA's tiles: first .. last - 1
-  long long last;
-  int grid;          // CTAs that have a range
-  int b, u, tile;    // where `first` lies
+// How the tiles of all units in one row are dealt: CTA c has q of them from
+// c q + min(c, r), one more if c < r.
+struct Plan {
+  unsigned long long q, r;
+  unsigned long long first;  // this CTA's
+  unsigned long long at;     // the tiles of the sequences before b
+  int b;                     // the sequence that `first` lies in
+  int pieces;                // 1: a CTA for each kMinTiles of a unit; 0: equal ranges
 };
 
+// The places of a unit in that row: its tiles and then what it costs beside them
+// (without which CTAs of many short units finished last: 24 sequences of up to
+// 2048 x 40 heads 118 us), or its tiles rounded up to whole pieces.
+__device__ __forceinline__ int span_of(int tiles, int pieces) {
+  return pieces ? (tiles + kMinTiles - 1) / kMinTiles * kMinTiles : tiles + kUnitCost;
+}
+
+// 64-bit quotients of numbers that mostly fit in 32.
+__device__ __forceinline__ unsigned long long quotient(unsigned long long a, unsigned long long b) {
+  if (((a | b) >> 32) == 0) return static_cast<unsigned int>(a) / static_cast<unsigned int>(b);
+  return a / b;
+}
+
 template <bool kBf16, int kDh, int kNt, bool kSmallPage>
-__global__ void __launch_bounds__(kThreads, kNt == 1 ? 2 : 1) paged_attention_kernel(const PagedAttnArgs a) {
+__global__ void __launch_bounds__(kThreads, kNt == 1 ? 3 : 2) paged_attention_kernel(const PagedAttnArgs a) {
   constexpr int kHeads = 8 * kNt;
   constexpr int kRep = 128 / kDh;          // blocks of 16 positions per warp and tile: 8 KB of keys and values
   constexpr int kTile = 16 * kRep * kWarps;
@@ -96,17 +130,17 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 2 : 1) paged_attention_ke
   constexpr int kVc = kDh / 64;            // of a value row
   extern __shared__ __align__(16) float so[];  // [kWarps][kHeads][kDh]
   __shared__ float sm[kWarps][kHeads], sl[kWarps][kHeads];
-  __shared__ long long scan[kWarps + 1];
+  __shared__ uint4 sq[kWarps][kNt][kKc][32];  // the query operand, lane by lane (in registers it made the loop spill)
+  __shared__ unsigned long long scan[2][kWarps];
   __shared__ Plan plan;
-  __shared__ int joined;
 
   const PagedCache& c = a.kv;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const int group = a.H / c.Hkv, parts = (group + kHeads - 1) / kHeads, units = c.Hkv * parts;
   const long long room = static_cast<long long>(c.table_cols) << c.page_log2;
   const float c2 = a.scale * 1.4426950408889634f;
-  int* counters = static_cast<int*>(a.ws);
-  float* partial = reinterpret_cast<float*>(counters + kMaxGrid);
+  int4* split = static_cast<int4*>(a.ws);
+  float* partial = reinterpret_cast<float*>(split + kMaxGrid);
 
   pdl_wait();
   pdl_launch_dependents();
@@ -118,58 +152,95 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 2 : 1) paged_attention_ke
   auto tiles_of = [&](int n) { return n <= kTile ? 1 : (n + kTile - 1) / kTile; };
 
   // The tiles before this thread's sequences, their sum, and from these the
-  // CTA's range and where it begins.
+  // CTA's range and where it begins. Few tiles: a CTA for each kMinTiles of a
+  // unit, so that none has two units one after the other; else equal ranges.
   {
+    typedef unsigned long long u64;
     const int per = (c.seqs + kThreads - 1) / kThreads, b0 = min(c.seqs, tid * per), b1 = min(c.seqs, b0 + per);
-    long long mine = 0;
+    u64 mine = 0, padded = 0;
     for (int b = b0; b < b1; ++b) {
+      const int n = tiles_of(length(b));
       if (a.lens[b] > room && blockIdx.x == 0) atomicOr(&g_paged_err, kErrIndex);
-      mine += tiles_of(length(b));
+      mine += span_of(n, 0);
+      padded += span_of(n, 1);
     }
-    long long upto = mine;
+    u64 upto = mine, upto_p = padded;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-      const long long v = __shfl_up_sync(0xFFFFFFFFu, upto, d);
-      if (lane >= d) upto += v;
+      const u64 v = __shfl_up_sync(0xFFFFFFFFu, upto, d), w = __shfl_up_sync(0xFFFFFFFFu, upto_p, d);
+      if (lane >= d) {
+        upto += v;
+        upto_p += w;
+      }
     }
-    if (lane == 31) scan[warp] = upto;
+    if (lane == 31) {
+      scan[0][warp] = upto;
+      scan[1][warp] = upto_p;
+    }
     __syncthreads();
-    long long all = 0;
+    u64 all = 0, all_p = 0;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
-      if (w < warp) upto += scan[w];
-      all += scan[w];
+      if (w < warp) {
+        upto += scan[0][w];
+        upto_p += scan[1][w];
+      }
+      all += scan[0][w];
+      all_p += scan[1][w];
     }
-    const long long total = all * units;
-    const int grid = static_cast<int>(max(1ll, min(static_cast<long long>(gridDim.x), total / kMinTiles)));
-    const int cta = static_cast<int>(blockIdx.x);
-    if (cta >= grid) return;  // (the whole CTA)
-    const long long first = total * cta / grid, last = total * (cta + 1) / grid;
+    const bool pieces = all_p * units <= static_cast<u64>(gridDim.x) * kMinTiles;
+    const u64 total = (pieces ? all_p : all) * units, cta = blockIdx.x;
+    if (pieces) {
+      upto = upto_p;
+      mine = padded;
+    }
+    const u64 q = pieces ? kMinTiles : quotient(total, gridDim.x), r = pieces ? 0 : total - q * gridDim.x;
+    const u64 first = cta * q + min(cta, r);
+    if (tid == 0) split[blockIdx.x] = make_int4(0, 0, -1, 0);
+    if (first >= total) return;  // (the whole CTA)
     if (first >= (upto - mine) * units && first < upto * units) {
-      long long at = (upto - mine) * units;
+      u64 at = (upto - mine) * units;
       for (int b = b0; b < b1; ++b) {
-        const int n = tiles_of(length(b));
-        if (first < at + static_cast<long long>(n) * units) {
+        const u64 n = static_cast<u64>(span_of(tiles_of(length(b)), pieces)) * units;
+        if (first < at + n) {
           plan.b = b;
-          plan.u = static_cast<int>((first - at) / n);
-          plan.tile = static_cast<int>((first - at) % n);
           break;
         }
-        at += static_cast<long long>(n) * units;
+        at += n;
       }
-      plan.total = total;
+      plan.q = q;
+      plan.r = r;
       plan.first = first;
-      plan.last = last;
-      plan.grid = grid;
+      plan.at = at;
+      plan.pieces = pieces;
     }
     __syncthreads();
   }
 
-  long long x = plan.first;
-  int b = plan.b, u = plan.u, tile = plan.tile;
-  while (x < plan.last) {
-    const int len = length(b), tiles = tiles_of(len);
-    const int tile_end = static_cast<int>(min(static_cast<long long>(tiles), tile + (plan.last - x)));
+  unsigned long long x = plan.first;
+  const unsigned long long last = x + plan.q + (blockIdx.x < plan.r ? 1 : 0);
+  int b = plan.b, u, tile;
+  {
+    const int span = span_of(tiles_of(length(b)), plan.pieces);
+    u = static_cast<int>(quotient(x - plan.at, span));
+    tile = static_cast<int>(x - plan.at - static_cast<unsigned long long>(u) * span);
+  }
+  while (x < last && b < c.seqs) {
+    const int len = length(b), tiles = tiles_of(len), span = span_of(tiles, plan.pieces);
+    const int stop = static_cast<int>(min(static_cast<unsigned long long>(span), tile + (last - x)));
+    const int tile_end = min(tiles, stop);
+    auto next_unit = [&]() {
+      x += stop - tile;
+      tile = 0;
+      if (++u == units) {
+        u = 0;
+        ++b;
+      }
+    };
+    if (tile >= tile_end) {  // none of its tiles are in the range
+      next_unit();
+      continue;
+    }
     const int hk = u / parts, h0 = hk * group + (u % parts) * kHeads;
     const int heads = min(kHeads, hk * group + group - h0);
     const int32_t* table = c.table + static_cast<long long>(b) * c.table_ld;
@@ -177,7 +248,7 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 2 : 1) paged_attention_ke
     const uint16_t* vh = c.v + hk * c.head_stride + g * 8;
     const int slots = (1 << c.page_log2) - 1;
 
-    // Element offset of position j (in the cache, without the head), -1 if it is not to be read.
+    // Element offset of position j in the cache (without the head), -1 if it is not to be read.
     auto offset = [&](int j) -> long long {
       if (j >= len) return -1;
       const int page = table[j >> c.page_log2];
@@ -188,7 +259,8 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 2 : 1) paged_attention_ke
       return page * c.page_stride + (j & slots) * c.token_stride;
     };
 
-    uint32_t qf[kNt][kKc][4];  // Q: head g of each 8, dimensions 32 i + 8 t ..
+    // Q: head g of each 8, dimensions 32 i + 8 t .. (each warp has its own copy)
+    __syncwarp();
 #pragma unroll
     for (int n = 0; n < kNt; ++n)
 #pragma unroll
@@ -196,11 +268,9 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 2 : 1) paged_attention_ke
         const int h = 8 * n + g;
         uint4 v = make_uint4(0u, 0u, 0u, 0u);
         if (h < heads) v = *reinterpret_cast<const uint4*>(a.q + b * a.ldq + static_cast<long long>(h0 + h) * kDh + 32 * i + 8 * t);
-        qf[n][i][0] = v.x;
-        qf[n][i][1] = v.y;
-        qf[n][i][2] = v.z;
-        qf[n][i][3] = v.w;
+        sq[warp][n][i][lane] = v;
       }
+    __syncwarp();
 
     float o[kNt][kVc][4][4];  // O^T: [.][hh][j]: dimensions 64 hh + 8 g + 2 j (+ 1), heads 2 t, 2 t + 1
     float ref[kNt][2], l[kNt][2];
@@ -221,11 +291,11 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 2 : 1) paged_attention_ke
 
     uint4 kr[kRep][kKc][2], vr[kRep][kVc][4];
     // With pages of 16 and more a block of 16 positions lies in one page: its
-    // offset is looked up a tile ahead of its loads. With smaller pages each
-    // row's is.
+    // offset is looked up a tile ahead of its loads, and its rows past the
+    // length are read too (they are the page's) but do not count. With smaller
+    // pages each row has an offset.
     constexpr int kLook = kSmallPage ? 6 : 1;
     long long off[kRep][kLook];
-    uint32_t live = 0;  // bits 2 rep, 2 rep + 1: the keys of rows g, g + 8 of the loaded blocks count
     auto look = [&](int tl) {
 #pragma unroll
       for (int r = 0; r < kRep; ++r) {
@@ -242,32 +312,55 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 2 : 1) paged_attention_ke
         }
       }
     };
+    // The keys of rows g, g + 8 of block r that count: bits 2 r, 2 r + 1 (of
+    // the loaded keys: live).
+    uint32_t live = 0;
     auto load_k = [&](int tl) {
       live = 0;
 #pragma unroll
       for (int r = 0; r < kRep; ++r) {
         const int j = tl * kTile + (warp * kRep + r) * 16;
+        if (kSmallPage) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const long long at = kSmallPage ? off[r][e] : off[r][0] + (g + 8 * e) * c.token_stride;
-          const bool valid = kSmallPage ? off[r][e] >= 0 : (off[r][0] >= 0 && j + g + 8 * e < len);
-          live |= valid ? 1u << (2 * r + e) : 0u;
+          for (int e = 0; e < 2; ++e) {
+            const bool valid = off[r][e] >= 0;
+            live |= valid ? 1u << (2 * r + e) : 0u;
 #pragma unroll
-          for (int i = 0; i < kKc; ++i) kr[r][i][e] = load16(kh + at + 32 * i, valid);
+            for (int i = 0; i < kKc; ++i) {
+              kr[r][i][e] = make_uint4(0u, 0u, 0u, 0u);
+              if (valid) kr[r][i][e] = ldg_stream16(kh + off[r][e] + 32 * i);
+            }
+          }
+        } else if (off[r][0] >= 0) {
+          live |= (j + g < len ? 1u << (2 * r) : 0u) | (j + g + 8 < len ? 2u << (2 * r) : 0u);
+          const uint16_t* p = kh + off[r][0] + g * c.token_stride;
+#pragma unroll
+          for (int i = 0; i < kKc; ++i) kr[r][i][0] = ldg_stream16(p + 32 * i);
+          p += 8 * c.token_stride;
+#pragma unroll
+          for (int i = 0; i < kKc; ++i) kr[r][i][1] = ldg_stream16(p + 32 * i);
         }
       }
     };
     auto load_v = [&](int tl) {
 #pragma unroll
       for (int r = 0; r < kRep; ++r) {
-        const int j = tl * kTile + (warp * kRep + r) * 16;
+        if (kSmallPage) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int row = 2 * t + (e & 1) + 4 * (e & 2);
-          const long long at = kSmallPage ? off[r][2 + e] : off[r][0] + row * c.token_stride;
-          const bool valid = kSmallPage ? off[r][2 + e] >= 0 : (off[r][0] >= 0 && j + row < len);
+          for (int e = 0; e < 4; ++e)
 #pragma unroll
-          for (int hh = 0; hh < kVc; ++hh) vr[r][hh][e] = load16(vh + at + 64 * hh, valid);
+            for (int hh = 0; hh < kVc; ++hh) {
+              vr[r][hh][e] = make_uint4(0u, 0u, 0u, 0u);
+              if (off[r][2 + e] >= 0) vr[r][hh][e] = ldg_stream16(vh + off[r][2 + e] + 64 * hh);
+            }
+        } else if (off[r][0] >= 0) {
+          const uint16_t* p = vh + off[r][0] + 2 * t * c.token_stride;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {  // rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+#pragma unroll
+            for (int hh = 0; hh < kVc; ++hh) vr[r][hh][e] = ldg_stream16(p + 64 * hh);
+            p += (e == 1 ? 7 : 1) * c.token_stride;
+          }
         }
       }
     };
@@ -287,24 +380,47 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 2 : 1) paged_attention_ke
           for (int e = 0; e < 4; ++e) s[r][n][e] = 0.0f;
 #pragma unroll
           for (int i = 0; i < kKc; ++i) {
-            mma16816<kBf16>(s[r][n], kr[r][i][0].x, kr[r][i][1].x, kr[r][i][0].y, kr[r][i][1].y, qf[n][i][0], qf[n][i][1]);
-            mma16816<kBf16>(s[r][n], kr[r][i][0].z, kr[r][i][1].z, kr[r][i][0].w, kr[r][i][1].w, qf[n][i][2], qf[n][i][3]);
+            const uint4 q = reload16(&sq[warp][n][i][lane]);
+            mma16816<kBf16>(s[r][n], kr[r][i][0].x, kr[r][i][1].x, kr[r][i][0].y, kr[r][i][1].y, q.x, q.y);
+            mma16816<kBf16>(s[r][n], kr[r][i][0].z, kr[r][i][1].z, kr[r][i][0].w, kr[r][i][1].w, q.z, q.w);
           }
         }
       const uint32_t counts = live;
       if (more) load_k(tl + 1);
       // scores in powers of two; positions that do not count have none
+#pragma unroll
+      for (int r = 0; r < kRep; ++r)
+#pragma unroll
+        for (int n = 0; n < kNt; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[r][n][e] *= c2;
+      constexpr uint32_t kAll = (1u << (2 * kRep)) - 1u;
+      if (!__all_sync(0xFFFFFFFFu, counts == kAll)) {
+#pragma unroll
+        for (int r = 0; r < kRep; ++r) {
+#pragma unroll
+          for (int n = 0; n < kNt; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (!(counts >> (2 * r + (e >> 1)) & 1u)) s[r][n][e] = -INFINITY;
+          // values of these positions may be anything: 0 (p is 0, but 0 times infinity is not)
+          const uint32_t rows = __ballot_sync(0xFFFFFFFFu, t == 0 && (counts >> (2 * r) & 1u)) |
+                                __ballot_sync(0xFFFFFFFFu, t == 0 && (counts >> (2 * r) & 2u)) << 1;  // row i: bit 4 i, 4 (i - 8) + 1
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (!(rows >> (4 * (2 * t + (e & 1)) + (e >> 1)) & 1u)) {
+#pragma unroll
+              for (int hh = 0; hh < kVc; ++hh) vr[r][hh][e] = make_uint4(0u, 0u, 0u, 0u);
+            }
+        }
+      }
       bool move = false;
 #pragma unroll
       for (int r = 0; r < kRep; ++r)
 #pragma unroll
         for (int n = 0; n < kNt; ++n)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float y = (counts >> (2 * r + (e >> 1)) & 1u) ? s[r][n][e] * c2 : -INFINITY;
-            s[r][n][e] = y;
-            move = move || y > ref[n][e & 1] + kMove;
-          }
+          for (int e = 0; e < 4; ++e) move = move || s[r][n][e] > ref[n][e & 1] + kMove;
       if (__any_sync(0xFFFFFFFFu, move)) {
 #pragma unroll
         for (int n = 0; n < kNt; ++n)
@@ -370,156 +486,213 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 2 : 1) paged_attention_ke
       }
     }
 
-    // The CTA's warps joined: each scales its part to the largest reference.
-#pragma unroll
-    for (int n = 0; n < kNt; ++n)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-#pragma unroll
-        for (int d = 4; d < 32; d <<= 1) l[n][e] += __shfl_xor_sync(0xFFFFFFFFu, l[n][e], d);
-        if (g == 0) {
-          sm[warp][8 * n + 2 * t + e] = ref[n][e];
-          sl[warp][8 * n + 2 * t + e] = l[n][e];
-        }
-      }
-    __syncthreads();
+    // The warps' parts into shared memory.
 #pragma unroll
     for (int n = 0; n < kNt; ++n)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int h = 8 * n + 2 * t + e;
-        float m = sm[0][h];
 #pragma unroll
-        for (int w = 1; w < kWarps; ++w) m = fmaxf(m, sm[w][h]);
-        const float f = ref[n][e] == -INFINITY ? 0.0f : exp2_fast(ref[n][e] - m);
+        for (int d = 4; d < 32; d <<= 1) l[n][e] += __shfl_xor_sync(0xFFFFFFFFu, l[n][e], d);
+        if (g == 0) {
+          sm[warp][h] = ref[n][e];
+          sl[warp][h] = l[n][e];
+        }
         if (h < heads) {
 #pragma unroll
           for (int hh = 0; hh < kVc; ++hh) {
             float* d = so + (warp * kHeads + h) * kDh + 64 * hh + 8 * g;
 #pragma unroll
             for (int j = 0; j < 4; j += 2)
-              *reinterpret_cast<float4*>(d + 2 * j) = make_float4(o[n][hh][j][e] * f, o[n][hh][j][e + 2] * f,
-                                                                  o[n][hh][j + 1][e] * f, o[n][hh][j + 1][e + 2] * f);
+              *reinterpret_cast<float4*>(d + 2 * j) = make_float4(o[n][hh][j][e], o[n][hh][j][e + 2],
+                                                                  o[n][hh][j + 1][e], o[n][hh][j + 1][e + 2]);
           }
         }
       }
     __syncthreads();
 
-    // (head, four dimensions) per thread and step: maximum, sum and values
-    auto write = [&](int h, int d, float m, float sum, float4 v) {
-      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-      uint2 w;
-      w.x = pack2<kBf16>(v.x * inv, v.y * inv);
-      w.y = pack2<kBf16>(v.z * inv, v.w * inv);
-      *reinterpret_cast<uint2*>(a.o + b * a.ldo + static_cast<long long>(h0 + h) * kDh + d) = w;
-      if (d == 0 && a.lse)
-        a.lse[static_cast<long long>(b) * a.H + h0 + h] =
-            sum == 0.0f ? -INFINITY : (m - kShift) * 0.6931471805599453f + logf(sum);
-    };
-    const bool whole = tile == 0 && tile_end == tiles;
-    const int cta = static_cast<int>(blockIdx.x);
-    float* part = partial + static_cast<size_t>(2 * cta + (tile == 0 ? 1 : 0)) * kPartFloats;
-    for (int i = tid; i < heads * (kDh / 4); i += kThreads) {
-      const int h = i / (kDh / 4), d = (i % (kDh / 4)) * 4;
-      float m = sm[0][h], sum = 0.0f;
+    // Their maxima, sums and values added up, to done(head, dimension, maximum, sum, four values).
+    auto add_warps = [&](auto&& done) {
+      for (int i = tid; i < heads * (kDh / 4); i += kThreads) {
+        const int h = i / (kDh / 4), d = (i % (kDh / 4)) * 4;
+        float m = sm[0][h], sum = 0.0f;
 #pragma unroll
-      for (int w = 1; w < kWarps; ++w) m = fmaxf(m, sm[w][h]);
-      float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int w = 1; w < kWarps; ++w) m = fmaxf(m, sm[w][h]);
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        const float f = sm[w][h] == -INFINITY ? 0.0f : exp2_fast(sm[w][h] - m);
-        sum += sl[w][h] * f;
-        const float4 z = *reinterpret_cast<const float4*>(so + (w * kHeads + h) * kDh + d);
-        v.x += z.x;
-        v.y += z.y;
-        v.z += z.z;
-        v.w += z.w;
+        for (int w = 0; w < kWarps; ++w) {
+          const float f = sm[w][h] == -INFINITY ? 0.0f : exp2_fast(sm[w][h] - m);
+          const float4 z = *reinterpret_cast<const float4*>(so + (w * kHeads + h) * kDh + d);
+          sum += sl[w][h] * f;
+          v.x += z.x * f;
+          v.y += z.y * f;
+          v.z += z.z * f;
+          v.w += z.w * f;
+        }
+        done(h, d, m, sum, v);
       }
-      if (whole) {
-        write(h, d, m, sum, v);
-      } else {
+    };
+    if (tile == 0 && tile_end == tiles) {
+      add_warps([&](int h, int d, float m, float sum, float4 v) { write_out<kBf16>(a, b, h0 + h, d, m, sum, v); });
+    } else {
+      float* part = partial + static_cast<size_t>(2 * blockIdx.x + (tile == 0 ? 1 : 0)) * kPartFloats;
+      add_warps([&](int h, int d, float m, float sum, float4 v) {
         if (d == 0) {
           part[h] = m;
           part[16 + h] = sum;
         }
         *reinterpret_cast<float4*>(part + 32 + h * kDh + d) = v;
-      }
-    }
-    if (!whole) {
-      // The unit's CTAs: c0 (whose part is the second of its two) .. c1.
-      const long long x0 = x - tile;
-      const int c0 = static_cast<int>(((x0 + 1) * plan.grid - 1) / plan.total);
-      const int c1 = static_cast<int>(((x0 + tiles) * plan.grid - 1) / plan.total);
-      __threadfence();
-      __syncthreads();
-      if (tid == 0) joined = atomicAdd(counters + c0, 1) == c1 - c0;
-      __syncthreads();
-      if (joined) {
-        __threadfence();
-        for (int i = tid; i < heads * (kDh / 4); i += kThreads) {
-          const int h = i / (kDh / 4), d = (i % (kDh / 4)) * 4;
-          float m = -INFINITY, sum = 0.0f;
-          float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-          for (int k = c0; k <= c1; ++k) m = fmaxf(m, __ldcg(partial + static_cast<size_t>(2 * k + (k == c0)) * kPartFloats + h));
-          for (int k = c0; k <= c1; ++k) {
-            const float* p = partial + static_cast<size_t>(2 * k + (k == c0)) * kPartFloats;
-            const float mk = __ldcg(p + h), f = mk == -INFINITY ? 0.0f : exp2_fast(mk - m);
-            const float4 z = __ldcg(reinterpret_cast<const float4*>(p + 32 + h * kDh + d));
-            sum += __ldcg(p + 16 + h) * f;
-            v.x += z.x * f;
-            v.y += z.y * f;
-            v.z += z.z * f;
-            v.w += z.w * f;
-          }
-          write(h, d, m, sum, v);
-        }
-        if (tid == 0) counters[c0] = 0;  // ready for the next call
+      });
+      if (tile == 0 && tid == 0) {  // who else has parts of the unit
+        const unsigned long long y = x + tiles - 1, more = plan.r * (plan.q + 1);
+        split[blockIdx.x] =
+            make_int4(b, u, static_cast<int>(y < more ? quotient(y, plan.q + 1) : plan.r + quotient(y - more, plan.q)), 0);
       }
     }
     __syncthreads();  // the shared results have been read
 
-    x += tile_end - tile;
-    tile = 0;
-    if (++u == units) {
-      u = 0;
-      ++b;
+    next_unit();
+  }
+}
+
+// Joins the units that several CTAs share: CTA x the one that begins in CTA x of
+// the kernel before, from the parts of that one and the following. A warp takes
+// one head's, kBatch at a time with their loads in flight together (one after
+// the other, 76 parts of 4 heads took 15 us); with fewer heads than warps,
+// several warps share a head.
+constexpr int kJoinWarps = 8;
+
+template <bool kBf16, int kDh, int kNt>
+__global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const PagedAttnArgs a) {
+  constexpr int kHeads = 8 * kNt, kBatch = 16, kJd = kDh / 32;  // parts; dimensions per lane
+  __shared__ __align__(16) float so[kJoinWarps][kDh];
+  __shared__ float sm[kJoinWarps], sl[kJoinWarps];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int group = a.H / a.kv.Hkv, parts = (group + kHeads - 1) / kHeads;
+  pdl_wait();
+  pdl_launch_dependents();
+  const int4* split = static_cast<const int4*>(a.ws);
+  const float* partial = reinterpret_cast<const float*>(split + kMaxGrid);
+  const int4 unit = split[blockIdx.x];
+  const int c0 = static_cast<int>(blockIdx.x), c1 = unit.z;
+  if (c1 < 0) return;
+  const int hk = unit.y / parts, h0 = hk * group + (unit.y % parts) * kHeads, heads = min(kHeads, hk * group + group - h0);
+  const int ways = max(1, kJoinWarps / heads), at_once = kJoinWarps / ways;  // heads
+  for (int hb = 0; hb < heads; hb += at_once) {
+    const int h = hb + warp / ways, way = warp % ways;
+    if (h < heads && h < hb + at_once) {
+      float jm = -INFINITY, jl = 0.0f, jo[kJd];
+#pragma unroll
+      for (int e = 0; e < kJd; ++e) jo[e] = 0.0f;
+      for (int k0 = c0 + way; k0 <= c1; k0 += kBatch * ways) {
+        float mk[kBatch], lk[kBatch], z[kBatch][kJd];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+          const int k = k0 + i * ways;
+          const float* p = partial + static_cast<size_t>(2 * k + (k == c0)) * kPartFloats;
+          mk[i] = -INFINITY;
+          lk[i] = 0.0f;
+#pragma unroll
+          for (int e = 0; e < kJd; ++e) z[i][e] = 0.0f;
+          if (k <= c1) {
+            mk[i] = p[h];
+            lk[i] = p[16 + h];
+            if (kJd == 4) {
+              const float4 v = *(reinterpret_cast<const float4*>(p + 32 + h * kDh) + lane);
+              z[i][0] = v.x;
+              z[i][1] = v.y;
+              z[i][2 % kJd] = v.z;
+              z[i][3 % kJd] = v.w;
+            } else {
+              const float2 v = *(reinterpret_cast<const float2*>(p + 32 + h * kDh) + lane);
+              z[i][0] = v.x;
+              z[i][1] = v.y;
+            }
+          }
+        }
+        float m = jm;
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) m = fmaxf(m, mk[i]);
+        const float of = jm == -INFINITY ? 0.0f : exp2_fast(jm - m);
+        jm = m;
+        jl *= of;
+#pragma unroll
+        for (int e = 0; e < kJd; ++e) jo[e] *= of;
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+          const float f = mk[i] == -INFINITY ? 0.0f : exp2_fast(mk[i] - m);
+          jl += lk[i] * f;
+#pragma unroll
+          for (int e = 0; e < kJd; ++e) jo[e] += z[i][e] * f;
+        }
+      }
+      if (lane == 0) {
+        sm[warp] = jm;
+        sl[warp] = jl;
+      }
+#pragma unroll
+      for (int e = 0; e < kJd; ++e) so[warp][lane * kJd + e] = jo[e];
     }
+    __syncthreads();
+    for (int i = threadIdx.x; i < at_once * (kDh / 4); i += 32 * kJoinWarps) {
+      const int k = i / (kDh / 4), d = (i % (kDh / 4)) * 4;
+      if (hb + k >= heads) continue;
+      float m = -INFINITY, sum = 0.0f;
+      for (int w = k * ways; w < k * ways + ways; ++w) m = fmaxf(m, sm[w]);
+      float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      for (int w = k * ways; w < k * ways + ways; ++w) {
+        const float f = sm[w] == -INFINITY ? 0.0f : exp2_fast(sm[w] - m);
+        const float4 z = *reinterpret_cast<const float4*>(&so[w][d]);
+        sum += sl[w] * f;
+        v.x += z.x * f;
+        v.y += z.y * f;
+        v.z += z.z * f;
+        v.w += z.w * f;
+      }
+      write_out<kBf16>(a, unit.x, h0 + hb + k, d, m, sum, v);
+    }
+    __syncthreads();
   }
 }
 
 template <bool kBf16, int kDh, int kNt, bool kSmallPage>
-cudaError_t launch(const PagedAttnArgs& a, cudaStream_t stream) {
+cudaError_t launch(const PagedAttnArgs& a, cudaStream_t stream, unsigned int* launches) {
   constexpr size_t smem = static_cast<size_t>(kWarps) * 8 * kNt * kDh * sizeof(float);
   static SmemLimit limit;
   auto* kernel = paged_attention_kernel<kBf16, kDh, kNt, kSmallPage>;
-  if (smem > 32 * 1024) {
-    const cudaError_t e = limit.allow(kernel, smem);
-    if (e != cudaSuccess) return e;
-  }
+  const cudaError_t le = limit.allow(kernel, smem);
+  if (le != cudaSuccess) return le;
   // CTAs for every tile that the table has room for, at most a wave
   const int group = a.H / a.kv.Hkv;
   const long long units = static_cast<long long>(a.kv.Hkv) * ((group + 8 * kNt - 1) / (8 * kNt)) * a.kv.seqs;
   constexpr int kTile = 16 * (128 / kDh) * kWarps;
   const long long room = std::max(1ll, ((static_cast<long long>(a.kv.table_cols) << a.kv.page_log2) + kTile - 1) / kTile);
-  const int wave = std::min(kMaxGrid, num_sms() * (kNt == 1 ? 2 : 1));
+  const int wave = std::min(kMaxGrid, num_sms() * (kNt == 1 ? 3 : 2));
   const int grid = room >= wave || units >= wave ? wave : static_cast<int>(std::min<long long>(wave, units * room));
-  return launch_pdl(kernel, dim3(static_cast<unsigned>(grid)), dim3(kThreads), smem, stream, a);
+  cudaError_t e = launch_pdl(kernel, dim3(static_cast<unsigned>(grid)), dim3(kThreads), smem, stream, a);
+  if (e != cudaSuccess) return e;
+  ++*launches;
+  // no unit can have more than one piece: nothing to join
+  if (room <= kMinTiles && units <= grid) return cudaSuccess;
+  e = launch_pdl(join_kernel<kBf16, kDh, kNt>, dim3(static_cast<unsigned>(grid)), dim3(32 * kJoinWarps), 0, stream, a);
+  if (e == cudaSuccess) ++*launches;
+  return e;
 }
 
 template <bool kBf16, int kDh>
-cudaError_t launch_for(const PagedAttnArgs& a, cudaStream_t stream) {
+cudaError_t launch_for(const PagedAttnArgs& a, cudaStream_t stream, unsigned int* launches) {
   const bool wide = a.H / a.kv.Hkv > 8, small = a.kv.page_log2 < 4;
-  if (wide) return small ? launch<kBf16, kDh, 2, true>(a, stream) : launch<kBf16, kDh, 2, false>(a, stream);
-  return small ? launch<kBf16, kDh, 1, true>(a, stream) : launch<kBf16, kDh, 1, false>(a, stream);
+  if (wide) return small ? launch<kBf16, kDh, 2, true>(a, stream, launches) : launch<kBf16, kDh, 2, false>(a, stream, launches);
+  return small ? launch<kBf16, kDh, 1, true>(a, stream, launches) : launch<kBf16, kDh, 1, false>(a, stream, launches);
 }
 
 }  // namespace
 
 size_t paged_attention_workspace_bytes() { return kWsBytes; }
 
-cudaError_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t stream) {
-  if (a.kv.bf16) return a.kv.dh == 64 ? launch_for<true, 64>(a, stream) : launch_for<true, 128>(a, stream);
-  return a.kv.dh == 64 ? launch_for<false, 64>(a, stream) : launch_for<false, 128>(a, stream);
+cudaError_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t stream, unsigned int* launches) {
+  if (a.kv.bf16) return a.kv.dh == 64 ? launch_for<true, 64>(a, stream, launches) : launch_for<true, 128>(a, stream, launches);
+  return a.kv.dh == 64 ? launch_for<false, 64>(a, stream, launches) : launch_for<false, 128>(a, stream, launches);
 }
 
 unsigned int paged_read_and_clear_error() {

@@ -9,6 +9,9 @@
   python -m paper_2609_34867_gb300.kernel_cases swiglu M K LD [--reps R]
   python -m paper_2609_34867_gb300.kernel_cases rmsnorm M K [--reps R]
   python -m paper_2609_34867_gb300.kernel_cases attn B M H [--reps R]
+  python -m paper_2609_34867_gb300.kernel_cases append T H HKV [--reps R]
+  python -m paper_2609_34867_gb300.kernel_cases attend B L H HKV [--reps R]
+  python -m paper_2609_34867_gb300.kernel_cases sample B V {plain,top_k,top_p,min_p} [--reps R]
   python -m paper_2609_34867_gb300.kernel_cases mse B M D [--reps R]
   python -m paper_2609_34867_gb300.kernel_cases topk B N K [--reps R]
   python -m paper_2609_34867_gb300.kernel_cases peak {f8,s8,dp4a} ITERS [--reps R]
@@ -43,6 +46,11 @@ selects the first replayed launch.
   attn    p4q_causal_attention on B samples of M positions, H heads of 128
           (flops: 2 x 2 x 128 x M (M + 1) / 2 per sample and head, the
           causal Q K^T and P V; bytes: q, k, v in, o out, fp16);
+  append  p4q_rope_append of T tokens of one sequence, H and HKV heads of 128,
+          pages of 16, bf16 (bytes: 4 T (H + 2 HKV) 128 in and out);
+  attend  p4q_paged_attention, B sequences of L positions, H heads over HKV
+          of 128, shuffled pages of 16, bf16 (bytes: 4 B L HKV 128 in);
+  sample  p4q_sample on B x V fp32 logits with one cut (bytes: 4 B V in);
   mse     p4q_block_mse on B samples of M rows x D fp16 (bytes: 4 B M D in);
   topk    p4q_topk_replacement on B x N fp32 score pairs (bytes: 8 B N in);
   peak    p4q_peak_probe: the throughput loop of one integer contraction
@@ -191,7 +199,8 @@ def _sweep(kind: str, reps: int, dev):
 
 def main(argv=None):
     ap = argparse.ArgumentParser()
-    ap.add_argument("case", choices=["gemm", "gemm8", "quant", "requant", "requant1", "select", "saliency", "swiglu", "rmsnorm", "attn",
+    ap.add_argument("case", choices=["gemm", "gemm8", "quant", "requant", "requant1", "select", "saliency", "swiglu", "rmsnorm", "attn", "append", "attend",
+                                     "sample",
                                      "mse", "topk", "peak", "sweep", "hostlink"])
     ap.add_argument("args", nargs="+")
     ap.add_argument("--reps", type=int, default=3)
@@ -281,6 +290,44 @@ def main(argv=None):
         nbytes = 4 * B * M * H * 128 * 2
         print(f"attn {B}x{M} H={H}: {ms * 1e3:.1f} us/call, {flops / ms / 1e9:.1f} TFLOP/s, "
               f"{nbytes / ms / 1e6:.1f} GB/s")
+    elif a.case == "append":
+        T, H, HK = (int(x) for x in a.args)
+        g = torch.Generator(device=dev).manual_seed(0)
+        y = torch.randn((T, (H + 2 * HK) * 128), generator=g, device=dev).bfloat16()
+        q, k, v = y[:, :H * 128], y[:, H * 128:(H + HK) * 128], y[:, (H + HK) * 128:]
+        pages = (T + 15) // 16
+        kc, vc = (torch.empty((pages, 16, HK, 128), dtype=torch.bfloat16, device=dev) for _ in range(2))
+        table = torch.randperm(pages, generator=g, device=dev).to(torch.int32)[None]
+        pos = torch.arange(T, dtype=torch.int32, device=dev)
+        seq = torch.zeros((T,), dtype=torch.int32, device=dev)
+        cos, sin = (torch.rand((T, 64), generator=g, device=dev) for _ in range(2))
+        out = torch.empty((T, H * 128), dtype=torch.bfloat16, device=dev)
+        ms = _timed(lambda: p4q.p4q_rope_append(q, k, v, cos, sin, pos, kc, vc, table, out, seq=seq), a.reps, dev)
+        nbytes = 4 * T * (H + 2 * HK) * 128
+        print(f"append {T} H={H}/{HK}: {ms * 1e3:.1f} us/call, {nbytes / ms / 1e6:.1f} GB/s")
+    elif a.case == "attend":
+        B, L, H, HK = (int(x) for x in a.args)
+        g = torch.Generator(device=dev).manual_seed(0)
+        per = (L + 15) // 16
+        kc, vc = (torch.randn((B * per, 16, HK, 128), generator=g, device=dev).bfloat16() for _ in range(2))
+        table = torch.randperm(B * per, generator=g, device=dev).to(torch.int32).view(B, per)
+        lens = torch.full((B,), L, dtype=torch.int32, device=dev)
+        q = torch.randn((B, H * 128), generator=g, device=dev).bfloat16()
+        out, ws = torch.empty_like(q), p4q.paged_attention_workspace(dev)
+        ms = _timed(lambda: p4q.p4q_paged_attention(q, kc, vc, table, lens, out, ws), a.reps, dev)
+        nbytes = 4 * B * L * HK * 128
+        print(f"attend {B}x{L} H={H}/{HK}: {ms * 1e3:.1f} us/call, {nbytes / ms / 1e6:.1f} GB/s")
+    elif a.case == "sample":
+        B, V, cut = int(a.args[0]), int(a.args[1]), a.args[2]
+        g = torch.Generator(device=dev).manual_seed(0)
+        x = torch.randn((B, V), generator=g, device=dev) * 2.5
+        u = torch.rand((B,), generator=g, device=dev)
+        kw = {"plain": {}, "top_k": {"top_k": torch.full((B,), 50, dtype=torch.int32, device=dev)},
+              "top_p": {"top_p": torch.full((B,), 0.9, device=dev)},
+              "min_p": {"min_p": torch.full((B,), 0.05, device=dev)}}[cut]
+        token = torch.empty((B,), dtype=torch.int32, device=dev)
+        ms = _timed(lambda: p4q.p4q_sample(x, u, token, **kw), a.reps, dev)
+        print(f"sample {B}x{V} {cut}: {ms * 1e3:.1f} us/call, {4 * B * V / ms / 1e6:.1f} GB/s")
     elif a.case == "mse":
         B, M, D = (int(x) for x in a.args)
         g = torch.Generator(device=dev).manual_seed(0)
