@@ -41,7 +41,7 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kMaxGrid = 640;    // CTAs of a launch at most (partial results of the workspace)
-constexpr int kMinTiles = 4;     // tiles per CTA at least, of one unit
+constexpr int kMinTiles = 3;     // tiles per CTA at least, of one unit
 constexpr int kUnitCost = 2;     // what a unit costs beside its tiles, in tiles
 constexpr float kShift = 7.0f;   // p = 2^(score - reference + 7): small p keep their bits in fp16
 constexpr float kMove = 8.0f;    // a reference moves when a score exceeds it by 2^8
@@ -556,15 +556,15 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 3 : 2) paged_attention_ke
 }
 
 // Joins the units that several CTAs share: CTA x the one that begins in CTA x of
-// the kernel before, from the parts of that one and the following. A warp takes
-// one head's, kBatch at a time with their loads in flight together (one after
-// the other, 76 parts of 4 heads took 15 us); with fewer heads than warps,
-// several warps share a head.
-constexpr int kJoinWarps = 8;
+// the kernel before, from the parts of that one and the following; CTA (x, y)
+// its heads 4 y .. 4 y + 3. The parts of a head are divided among several warps,
+// which take kBatch at a time with their loads in flight together (one after the
+// other, 76 parts of 4 heads took 15 us).
+constexpr int kJoinWarps = 16, kJoinHeads = 4;
 
 template <bool kBf16, int kDh, int kNt>
 __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const PagedAttnArgs a) {
-  constexpr int kHeads = 8 * kNt, kBatch = 16, kJd = kDh / 32;  // parts; dimensions per lane
+  constexpr int kHeads = 8 * kNt, kBatch = 8, kJd = kDh / 32;  // parts; dimensions per lane
   __shared__ __align__(16) float so[kJoinWarps][kDh];
   __shared__ float sm[kJoinWarps], sl[kJoinWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -576,82 +576,80 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const PagedAttnAr
   const int4 unit = split[blockIdx.x];
   const int c0 = static_cast<int>(blockIdx.x), c1 = unit.z;
   if (c1 < 0) return;
-  const int hk = unit.y / parts, h0 = hk * group + (unit.y % parts) * kHeads, heads = min(kHeads, hk * group + group - h0);
-  const int ways = max(1, kJoinWarps / heads), at_once = kJoinWarps / ways;  // heads
-  for (int hb = 0; hb < heads; hb += at_once) {
-    const int h = hb + warp / ways, way = warp % ways;
-    if (h < heads && h < hb + at_once) {
-      float jm = -INFINITY, jl = 0.0f, jo[kJd];
+  const int hk = unit.y / parts, h0 = hk * group + (unit.y % parts) * kHeads;
+  const int first = static_cast<int>(blockIdx.y) * kJoinHeads;
+  const int heads = min(kJoinHeads, min(kHeads, hk * group + group - h0) - first);  // of this CTA
+  if (heads <= 0) return;
+  const int ways = kJoinWarps / heads, k = warp / ways, way = warp % ways, h = first + k;
+  if (k < heads) {
+    float jm = -INFINITY, jl = 0.0f, jo[kJd];
 #pragma unroll
-      for (int e = 0; e < kJd; ++e) jo[e] = 0.0f;
-      for (int k0 = c0 + way; k0 <= c1; k0 += kBatch * ways) {
-        float mk[kBatch], lk[kBatch], z[kBatch][kJd];
+    for (int e = 0; e < kJd; ++e) jo[e] = 0.0f;
+    for (int k0 = c0 + way; k0 <= c1; k0 += kBatch * ways) {
+      float mk[kBatch], lk[kBatch], z[kBatch][kJd];
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-          const int k = k0 + i * ways;
-          const float* p = partial + static_cast<size_t>(2 * k + (k == c0)) * kPartFloats;
-          mk[i] = -INFINITY;
-          lk[i] = 0.0f;
+      for (int i = 0; i < kBatch; ++i) {
+        const int cta = k0 + i * ways;
+        const float* p = partial + static_cast<size_t>(2 * cta + (cta == c0)) * kPartFloats;
+        mk[i] = -INFINITY;
+        lk[i] = 0.0f;
 #pragma unroll
-          for (int e = 0; e < kJd; ++e) z[i][e] = 0.0f;
-          if (k <= c1) {
-            mk[i] = p[h];
-            lk[i] = p[16 + h];
-            if (kJd == 4) {
-              const float4 v = *(reinterpret_cast<const float4*>(p + 32 + h * kDh) + lane);
-              z[i][0] = v.x;
-              z[i][1] = v.y;
-              z[i][2 % kJd] = v.z;
-              z[i][3 % kJd] = v.w;
-            } else {
-              const float2 v = *(reinterpret_cast<const float2*>(p + 32 + h * kDh) + lane);
-              z[i][0] = v.x;
-              z[i][1] = v.y;
-            }
+        for (int e = 0; e < kJd; ++e) z[i][e] = 0.0f;
+        if (cta <= c1) {
+          mk[i] = p[h];
+          lk[i] = p[16 + h];
+          if (kJd == 4) {
+            const float4 v = *(reinterpret_cast<const float4*>(p + 32 + h * kDh) + lane);
+            z[i][0] = v.x;
+            z[i][1] = v.y;
+            z[i][2 % kJd] = v.z;
+            z[i][3 % kJd] = v.w;
+          } else {
+            const float2 v = *(reinterpret_cast<const float2*>(p + 32 + h * kDh) + lane);
+            z[i][0] = v.x;
+            z[i][1] = v.y;
           }
         }
-        float m = jm;
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i) m = fmaxf(m, mk[i]);
-        const float of = jm == -INFINITY ? 0.0f : exp2_fast(jm - m);
-        jm = m;
-        jl *= of;
-#pragma unroll
-        for (int e = 0; e < kJd; ++e) jo[e] *= of;
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-          const float f = mk[i] == -INFINITY ? 0.0f : exp2_fast(mk[i] - m);
-          jl += lk[i] * f;
-#pragma unroll
-          for (int e = 0; e < kJd; ++e) jo[e] += z[i][e] * f;
-        }
       }
-      if (lane == 0) {
-        sm[warp] = jm;
-        sl[warp] = jl;
-      }
+      float m = jm;
 #pragma unroll
-      for (int e = 0; e < kJd; ++e) so[warp][lane * kJd + e] = jo[e];
+      for (int i = 0; i < kBatch; ++i) m = fmaxf(m, mk[i]);
+      const float of = jm == -INFINITY ? 0.0f : exp2_fast(jm - m);
+      jm = m;
+      jl *= of;
+#pragma unroll
+      for (int e = 0; e < kJd; ++e) jo[e] *= of;
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        const float f = mk[i] == -INFINITY ? 0.0f : exp2_fast(mk[i] - m);
+        jl += lk[i] * f;
+#pragma unroll
+        for (int e = 0; e < kJd; ++e) jo[e] += z[i][e] * f;
+      }
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < at_once * (kDh / 4); i += 32 * kJoinWarps) {
-      const int k = i / (kDh / 4), d = (i % (kDh / 4)) * 4;
-      if (hb + k >= heads) continue;
-      float m = -INFINITY, sum = 0.0f;
-      for (int w = k * ways; w < k * ways + ways; ++w) m = fmaxf(m, sm[w]);
-      float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      for (int w = k * ways; w < k * ways + ways; ++w) {
-        const float f = sm[w] == -INFINITY ? 0.0f : exp2_fast(sm[w] - m);
-        const float4 z = *reinterpret_cast<const float4*>(&so[w][d]);
-        sum += sl[w] * f;
-        v.x += z.x * f;
-        v.y += z.y * f;
-        v.z += z.z * f;
-        v.w += z.w * f;
-      }
-      write_out<kBf16>(a, unit.x, h0 + hb + k, d, m, sum, v);
+    if (lane == 0) {
+      sm[warp] = jm;
+      sl[warp] = jl;
     }
-    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < kJd; ++e) so[warp][lane * kJd + e] = jo[e];
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < heads * (kDh / 4); i += 32 * kJoinWarps) {
+    const int n = i / (kDh / 4), d = (i % (kDh / 4)) * 4, w0 = n * ways;
+    float m = -INFINITY, sum = 0.0f;
+    for (int w = w0; w < w0 + ways; ++w) m = fmaxf(m, sm[w]);
+    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int w = w0; w < w0 + ways; ++w) {
+      const float f = sm[w] == -INFINITY ? 0.0f : exp2_fast(sm[w] - m);
+      const float4 z = *reinterpret_cast<const float4*>(&so[w][d]);
+      sum += sl[w] * f;
+      v.x += z.x * f;
+      v.y += z.y * f;
+      v.z += z.z * f;
+      v.w += z.w * f;
+    }
+    write_out<kBf16>(a, unit.x, h0 + first + n, d, m, sum, v);
   }
 }
 
@@ -674,7 +672,9 @@ cudaError_t launch(const PagedAttnArgs& a, cudaStream_t stream, unsigned int* la
   ++*launches;
   // no unit can have more than one piece: nothing to join
   if (room <= kMinTiles && units <= grid) return cudaSuccess;
-  e = launch_pdl(join_kernel<kBf16, kDh, kNt>, dim3(static_cast<unsigned>(grid)), dim3(32 * kJoinWarps), 0, stream, a);
+  const unsigned slices = (std::min(group, 8 * kNt) + kJoinHeads - 1) / kJoinHeads;
+  e = launch_pdl(join_kernel<kBf16, kDh, kNt>, dim3(static_cast<unsigned>(grid), slices), dim3(32 * kJoinWarps), 0, stream,
+                 a);
   if (e == cudaSuccess) ++*launches;
   return e;
 }

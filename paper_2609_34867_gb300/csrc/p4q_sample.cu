@@ -14,9 +14,13 @@
 // rounds to 0 past d = 22.2; those come last and are never drawn, so they take
 // no part). The CTAs add up a slice of the bins each, scan it, and the bin in
 // which the wanted sum is reached follows. Its tokens, mostly a few, go to
-// one CTA, which ranks them. Bins of more tokens than the list holds are
-// divided again by the logits' ordered bit patterns, at most three times (11 of 32
-// bits each); a bin of equal logits is cut by index.
+// one list and are ranked. Bins of more tokens than the list holds are divided
+// again by the logits' ordered bit patterns, at most three times (11 of 32 bits
+// each); a bin of equal logits is cut by index. Shared-memory atomics are what
+// a histogram costs, so tokens that the cut cannot reach stay out of it: for
+// top-k those below the k-th of the threads' own maxima (a CTA alone has k tokens
+// above it), for top-p those whose weights, all of them together, are less than
+// what may be cut off.
 // The draw: kept weights per warp (a warp's tokens are consecutive), their prefix
 // over the cluster, and the one warp that contains the drawn number walks
 // its tokens.
@@ -36,7 +40,7 @@ constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
 constexpr int kBins = 2048;
-constexpr float kBinScale = 92.0f;  // 2048 / 92 = 22.26 > 22.18 = ln(2^32): a token past the bins has weight 0
+constexpr float kBinScale = 92.0f;  // 2047 / 92 = 22.25 > 22.18 = ln(2^32): a token past the bins has weight 0
 constexpr int kList = 512;
 
 struct Shared {
@@ -44,12 +48,13 @@ struct Shared {
   uint32_t lkey[kList], lidx[kList], lw[kList];
   u64 warp_sum[kWarps];
   // written by the other CTAs of the cluster
-  u64 slice_total[kMaxCluster], mass[kMaxCluster], ties[kMaxCluster];
+  u64 slice_total[kMaxCluster], mass[kMaxCluster], sum[kMaxCluster], ties[kMaxCluster];
   uint32_t max_key[kMaxCluster], first_max[kMaxCluster];
   u64 need;
   uint32_t bin, cut_key, cut_idx;
   uint32_t list_n, key_min, key_max;  // (of the cluster's first CTA)
   uint32_t red[kWarps];
+  int last_bin;  // (of this CTA)
 };
 
 __device__ __forceinline__ float float_of_key(uint32_t k) {
@@ -178,6 +183,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
       mine4[(st * 32 + lane) * 2 + 1] = make_float4(f[4], f[5], f[6], f[7]);
     }
   }
+  const float own_max = mx;
   __syncwarp();
   // f(logit, token) for this lane's four tokens of a step
   const int i0 = w0 + lane * 4 - skip;
@@ -242,38 +248,123 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
     return;
   }
 
-  const float inv_t = 1.0f / temp;
-  auto dist = [&](float v) { return v == mx ? 0.0f : (mx - v) * inv_t; };
-  auto weight = [&](float e) { return __float2uint_rn(e * 2147483648.0f); };
+  // (T = inf: not 0, so that a logit of -inf stays infinitely far)
+  const float inv_t = fmaxf(1.0f / temp, 1.17549435e-38f);
+  // (the largest itself: 0, also where the product is NaN: of infinite logits, of a denormal T)
+  auto dist = [&](float v) { return fmaxf((mx - v) * inv_t, 0.0f); };
+  auto weight = [&](float d) { return __float2uint_rn(expf(-d) * 2147483648.0f); };
+  auto d_bin = [&](float d, int* bin) {  // false: past the bins
+    const float f = fmaf(d, kBinScale, 8388608.0f);  // d in bins, rounded, behind 2^23
+    *bin = __float_as_int(f) & 0x7FFFFF;
+    return f < 8388608.0f + kBins;
+  };
   float cut_x = -INFINITY;  // the last kept token
   int cut_i = INT_MAX;
   auto keeps = [&](float v, int i) { return v > cut_x || (v == cut_x && i <= cut_i); };
+  // A sum over the cluster's threads; *before: that of the warps before this one.
+  auto sum_all = [&](u64 v, u64* slots, u64* before) -> u64 {
+    v = warp_add(v);
+    __syncthreads();  // (the sums of a scan before have been read)
+    if (lane == 0) s.warp_sum[warp] = v;
+    __syncthreads();
+    u64 cta = 0, at = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      if (w < warp) at += s.warp_sum[w];
+      cta += s.warp_sum[w];
+    }
+    if (tid == 0) put64(&slots[rank], cta);
+    sync_all();
+    u64 total = 0;
+    for (int r = 0; r < cs; ++r) {
+      if (r < rank) at += slots[r];
+      total += slots[r];
+    }
+    *before = at;
+    return total;
+  };
 
   // Shortens the kept head: to `need` tokens (by_mass false), or to the first
   // tokens whose weights reach ceil(share * the kept weights' sum).
   auto shorten = [&](const bool by_mass, u64 need, float share) {
+    const bool all_kept = cut_x == -INFINITY;
+    auto reach = [&](u64 total) -> u64 {
+      const double want = ceil(static_cast<double>(share) * static_cast<double>(total));
+      return want < 1.0 ? 1ull : static_cast<u64>(want);
+    };
+    int last_bin = kBins - 1;  // tokens of later bins are past the cut
+    if (by_mass && all_kept) {
+      u64 sum = 0, before;
+      each([&](float v, int i) { sum += weight(dist(v)); });
+      sum = sum_all(sum, s.sum, &before);
+      need = reach(sum);
+      // Tokens of weight <= (sum - need) / V have no more than sum - need together. Bin b + 1 begins half a
+      // bin behind b's middle, and a weight is off by half a unit: one unit and one bin less.
+      const float spare = static_cast<float>((sum - need) / static_cast<unsigned int>(V));
+      if (spare > 2.0f) last_bin = min(last_bin, static_cast<int>((21.487563f - logf(spare - 1.0f)) * kBinScale) + 2);
+    }
+    for (int i = tid; i < kBins; i += kThreads) {
+      s.lo[i] = 0;
+      s.hi[i] = 0;
+    }
+    __syncthreads();
+    if (!by_mass && need <= kThreads) {
+      // the bin of the need-th of the threads' largest logits (in the array that counts leave free)
+      int bin;
+      if (d_bin(dist(own_max), &bin)) atomicAdd(&s.hi[bin], 1u);
+      if (tid == 0) s.last_bin = kBins - 1;
+      __syncthreads();
+      constexpr int kPer = kBins / kThreads;
+      uint32_t c[kPer], own = 0;
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) {
+        c[j] = s.hi[tid * kPer + j];
+        own += c[j];
+      }
+      uint32_t upto = own;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+        if (lane >= d) upto += v;
+      }
+      if (lane == 31) s.red[warp] = upto;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w)
+        if (w < warp) upto += s.red[w];
+      if (own > 0 && upto >= need && upto - own < need) {
+        uint32_t at = upto - own;
+        int j = 0;
+        while ((at += c[j]) < need) ++j;
+        s.last_bin = tid * kPer + j;
+      }
+      __syncthreads();
+      last_bin = s.last_bin;
+    }
     uint32_t key_lo = 0, key_hi = 0;
     int shift = 0;
     for (int level = 0;; ++level) {
       // the bin of a token (falling logits have rising bins), or -1
       auto bin_of = [&](float v, int i) -> int {
         if (level == 0) {
-          const float f = dist(v) * kBinScale;
-          return f < static_cast<float>(kBins) && keeps(v, i) ? static_cast<int>(f) : -1;
+          int bin;
+          return d_bin(dist(v), &bin) && bin <= last_bin && keeps(v, i) ? bin : -1;
         }
         const uint32_t k = float_order_key(v);
         return k >= key_lo && k <= key_hi && keeps(v, i) ? static_cast<int>((key_hi - k) >> shift) : -1;
       };
-      for (int i = tid; i < kBins; i += kThreads) {
-        s.lo[i] = 0;
-        if (by_mass) s.hi[i] = 0;
+      if (level > 0) {
+        for (int i = tid; i < kBins; i += kThreads) {
+          s.lo[i] = 0;
+          s.hi[i] = 0;
+        }
+        __syncthreads();
       }
-      __syncthreads();
       each([&](float v, int i) {
         const int bin = bin_of(v, i);
         if (bin >= 0) {
           if (by_mass) {
-            const uint32_t w = weight(expf(-dist(v)));
+            const uint32_t w = weight(dist(v));
             atomicAdd(&s.lo[bin], w & 0xFFFFu);
             if (w >> 16) atomicAdd(&s.hi[bin], w >> 16);
           } else {
@@ -295,10 +386,12 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
         bins[j] = 0;
         if (j < per && tid * per < slice) {
           const int bin = rank * slice + tid * per + j;
-          for (int r = 0; r < cs; ++r) {
-            bins[j] += ld_cluster_u32(mapa_shared(smem_u32(&s.lo[bin]), r));
-            if (by_mass) bins[j] += static_cast<u64>(ld_cluster_u32(mapa_shared(smem_u32(&s.hi[bin]), r))) << 16;
-          }
+#pragma unroll
+          for (int r = 0; r < kMaxCluster; ++r)
+            if (r < cs) {
+              bins[j] += ld_cluster_u32(mapa_shared(smem_u32(&s.lo[bin]), r));
+              if (by_mass) bins[j] += static_cast<u64>(ld_cluster_u32(mapa_shared(smem_u32(&s.hi[bin]), r))) << 16;
+            }
         }
         own += bins[j];
       }
@@ -319,12 +412,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
         total += s.slice_total[r];
       }
       if (level == 0) {
-        if (by_mass) {
-          const double want = ceil(static_cast<double>(share) * static_cast<double>(total));
-          need = want < 1.0 ? 1ull : static_cast<u64>(want);
-        } else if (total <= need) {
-          return;  // every token that may be drawn is among the first `need`
-        }
+        if (by_mass && !all_kept) need = reach(total);
+        if (total < need) return;  // fewer tokens than `need` may be drawn at all
       }
       if (own > 0 && upto - own < need && need <= upto) {
         u64 at = upto - own;
@@ -363,7 +452,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
             if (bin_of(v, i) == bin && at < kList) {
               st_shared_cluster_u32(at_first(&s.lkey[at]), float_order_key(v));
               st_shared_cluster_u32(at_first(&s.lidx[at]), static_cast<uint32_t>(i));
-              if (by_mass) st_shared_cluster_u32(at_first(&s.lw[at]), weight(expf(-dist(v))));
+              if (by_mass) st_shared_cluster_u32(at_first(&s.lw[at]), weight(dist(v)));
               ++at;
             }
           });
@@ -373,25 +462,37 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
       const uint32_t found = ld_cluster_u32(at_first(&s.list_n));
       key_lo = ld_cluster_u32(at_first(&s.key_min));
       key_hi = ld_cluster_u32(at_first(&s.key_max));
-      if (found <= kList) {
-        if (rank == 0 && tid < static_cast<int>(found)) {
-          const uint32_t k = s.lkey[tid], i = s.lidx[tid];
+      if (found <= kList) {  // every CTA ranks them for itself
+        uint32_t k = 0, i = 0, w = 1;
+        if (tid < static_cast<int>(found)) {
+          k = ld_cluster_u32(at_first(&s.lkey[tid]));
+          i = ld_cluster_u32(at_first(&s.lidx[tid]));
+          if (by_mass) w = ld_cluster_u32(at_first(&s.lw[tid]));
+          if (rank > 0) {
+            s.lkey[tid] = k;
+            s.lidx[tid] = i;
+            if (by_mass) s.lw[tid] = w;
+          }
+        }
+        __syncthreads();
+        if (tid < static_cast<int>(found)) {
           u64 before = 0;
           for (uint32_t j = 0; j < found; ++j) {
             const uint32_t kj = s.lkey[j];
             if (kj > k || (kj == k && s.lidx[j] < i)) before += by_mass ? s.lw[j] : 1u;
           }
-          if (before < need && need <= before + (by_mass ? s.lw[tid] : 1u)) {
-            put32(&s.cut_key, k);
-            put32(&s.cut_idx, i);
+          if (before < need && need <= before + w) {
+            s.cut_key = k;
+            s.cut_idx = i;
           }
         }
+        __syncthreads();
         break;
       }
       if (key_lo == key_hi) {  // equal logits: so many of them, by index
         const float v = float_of_key(key_lo);
         if (by_mass) {
-          const uint32_t w = weight(expf(-dist(v)));
+          const uint32_t w = weight(dist(v));
           need = (need + w - 1) / w;
         }
         auto same = [&](float u, int i) { return u == v && keeps(u, i); };
@@ -425,12 +526,12 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
             first = __shfl_sync(0xFFFFFFFFu, to, 31);
           }
         }
+        sync_all();
         break;
       }
       const int bits = 32 - __clz(key_hi - key_lo);
       shift = max(0, bits - 11);
     }
-    sync_all();
     cut_x = float_of_key(s.cut_key);
     cut_i = static_cast<int>(s.cut_idx);
   };
@@ -441,30 +542,18 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
   if (top_p < 1.0f) shorten(true, 0, top_p);
 
   const float min_p = a.min_p && a.min_p[n] > 0.0f ? fminf(a.min_p[n], 1.0f) : 0.0f;
+  // past d_max exp(-d) < min_p for certain (weights are 0 past 22.2)
+  const float d_max = fminf(min_p > 0.0f ? 1e-5f - 1.000001f * logf(min_p) : 23.0f, 23.0f);
   auto kept = [&](float v, int i) -> uint32_t {  // the kept weight
-    if (!keeps(v, i)) return 0u;
-    const float e = expf(-dist(v));
-    return e < min_p ? 0u : weight(e);
+    const float d = dist(v);
+    if (!(d <= d_max) || !keeps(v, i)) return 0u;
+    const float e = expf(-d);
+    return e < min_p ? 0u : __float2uint_rn(e * 2147483648.0f);
   };
-  u64 mine = 0;
+  u64 mine = 0, at;
   each([&](float v, int i) { mine += kept(v, i); });
   mine = warp_add(mine);
-  __syncthreads();  // (the sums of a scan before have been read)
-  if (lane == 0) s.warp_sum[warp] = mine;
-  __syncthreads();
-  u64 cta = 0, at = 0;
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) {
-    if (w < warp) at += s.warp_sum[w];
-    cta += s.warp_sum[w];
-  }
-  if (tid == 0) put64(&s.mass[rank], cta);
-  sync_all();
-  u64 total = 0;
-  for (int r = 0; r < cs; ++r) {
-    if (r < rank) at += s.mass[r];
-    total += s.mass[r];
-  }
+  const u64 total = sum_all(lane == 0 ? mine : 0ull, s.mass, &at);
   const double want = floor(static_cast<double>(a.u[n]) * static_cast<double>(total));
   u64 r = want > 0.0 ? static_cast<u64>(fmin(want, 9.0e15)) : 0ull;
   if (r > total - 1) r = total - 1;

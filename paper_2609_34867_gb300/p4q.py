@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -28,15 +29,6 @@ class P4QError(RuntimeError):
 
 class SelectParams(ctypes.Structure):
     _fields_ = [("K", ctypes.c_int32), ("alpha_permille", ctypes.c_int32), ("beta_permille", ctypes.c_int32)]
-
-
-class PagedKV(ctypes.Structure):
-    """p4q_paged_kv: a paged key/value cache and the page table of a call's sequences."""
-    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("table", ctypes.c_void_p),
-                ("page_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
-                ("dtype", ctypes.c_int32), ("pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
-                ("Hkv", ctypes.c_int32), ("dh", ctypes.c_int32), ("seqs", ctypes.c_int32),
-                ("table_ld", ctypes.c_int32), ("table_cols", ctypes.c_int32)]
 
 
 DTYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
@@ -115,12 +107,12 @@ def lib() -> ctypes.CDLL:
         L.p4q_select_gather_quant.argtypes = [P, I, I, I, P, I, P, P, I, ctypes.POINTER(SelectParams), P, P, P,
                                               P, P, S, P]
         L.p4q_select_gather_quant.restype = st
-        L.p4q_rope_append.argtypes = [P, I, P, I, P, I, I, I, P, P, I, I, I, P, P, P, ctypes.POINTER(PagedKV), P, I, P, I,
+        L.p4q_rope_append.argtypes = [P, I, P, I, P, I, I, I, P, P, I, I, I, P, P, P, P, P, I, P, I,
                                       P]
         L.p4q_rope_append.restype = st
         L.p4q_paged_attention_workspace_bytes.argtypes = []
         L.p4q_paged_attention_workspace_bytes.restype = S
-        L.p4q_paged_attention.argtypes = [P, I, I, ctypes.POINTER(PagedKV), P, ctypes.c_float, P, I, P, P, S, P]
+        L.p4q_paged_attention.argtypes = [P, I, I, P, P, ctypes.c_float, P, I, P, P, S, P]
         L.p4q_paged_attention.restype = st
         L.p4q_sample.argtypes = [P, I, ctypes.c_int64, I, I, P, P, P, P, P, P, P, P]
         L.p4q_sample.restype = st
@@ -393,78 +385,102 @@ def cls_saliency(q_cls, k_cls, k, stream=None):
 
 
 # ---------------------------------------------------------------- generation
-def _rows16(t, dtype, cols, name):
-    """A CUDA 2-D tensor of `dtype` with unit column stride (a column block of a fused output, say)."""
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.dim() != 2 or not t.is_cuda or \
-            (t.stride(1) != 1 and t.shape[1] > 1):
+# These calls sit in a decode loop, where a call's host time counts: each tensor's
+# shape and strides are asked for once, and the cache description goes to the
+# library as packed bytes (a ctypes structure of it took as long as the launch).
+_PAGED_KV = struct.Struct("@PPPqqq8i")  # p4q_paged_kv
+
+
+def _rows(t, dtype, rows, cols, name):
+    """Checks a CUDA matrix of `dtype` with unit column stride (a column block of
+    a fused output, say) and gives its pitch; cols None: any, rows None: any."""
+    try:
+        n, m = t.shape
+        pitch, step = t.stride()
+    except (AttributeError, ValueError):
+        raise TypeError(f"{name}: expected a CUDA {dtype} 2-D tensor with unit column stride") from None
+    if t.dtype is not dtype or not t.is_cuda or (step != 1 and m > 1):
         raise TypeError(f"{name}: expected a CUDA {dtype} 2-D tensor with unit column stride")
-    if cols is not None and t.shape[1] != cols:
-        raise ValueError(f"{name} has {t.shape[1]} columns, expected {cols}")
+    if cols is not None and m != cols:
+        raise ValueError(f"{name} has {m} columns, expected {cols}")
+    if rows is not None and n != rows:
+        raise ValueError(f"{name} has {n} rows, expected {rows}")
+    # (a single row's stride says nothing)
+    return pitch if n > 1 else (m + 7) // 8 * 8
 
 
 def _vector(t, dtype, n, name):
-    if t is None:
-        return
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.dim() != 1 or not t.is_cuda or \
-            (t.shape[0] > 1 and t.stride(0) != 1):
+    """The address of a contiguous CUDA vector of n values."""
+    try:
+        (m,) = t.shape
+    except (AttributeError, ValueError):
+        raise TypeError(f"{name}: expected a contiguous CUDA {dtype} vector") from None
+    if t.dtype is not dtype or not t.is_cuda or (m > 1 and t.stride(0) != 1):
         raise TypeError(f"{name}: expected a contiguous CUDA {dtype} vector")
-    if t.shape[0] != n:
-        raise ValueError(f"{name} has {t.shape[0]} entries, expected {n}")
+    if m != n:
+        raise ValueError(f"{name} has {m} entries, expected {n}")
+    return t.data_ptr()
 
 
-def _ld(t):
-    """Row pitch in elements (a single row's stride says nothing: its columns)."""
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], (t.shape[1] + 7) // 8 * 8)
+def _optional(t, dtype, n, name):
+    return None if t is None else _vector(t, dtype, n, name)
 
 
-def paged_kv(k_cache, v_cache, table):
-    """The PagedKV of caches [pages, page_size, Hkv, dh] (any order of slots and
-    heads in memory, as strides; unit stride along dh) and a page table [seqs,
-    pages per sequence] int32."""
-    if not isinstance(k_cache, torch.Tensor) or k_cache.dtype not in (torch.float16, torch.bfloat16) or \
-            k_cache.dim() != 4 or not k_cache.is_cuda or k_cache.stride(3) != 1:
+def _paged_kv(k_cache, v_cache, table):
+    """(p4q_paged_kv as bytes, type, Hkv, dh, seqs) of caches [pages, page_size,
+    Hkv, dh] (any order of slots and heads in memory, as strides; unit stride
+    along dh) and a page table [seqs, pages per sequence] int32."""
+    try:
+        shape, strides, dt = k_cache.shape, k_cache.stride(), k_cache.dtype
+        pages, size, heads, dh = shape
+        ps, ts, hs, step = strides
+    except (AttributeError, ValueError):
+        dt = None
+    if (dt is not torch.float16 and dt is not torch.bfloat16) or step != 1 or not k_cache.is_cuda:
         raise TypeError("k_cache: expected a CUDA fp16 or bf16 tensor [pages, page_size, Hkv, dh], unit stride along dh")
-    if not isinstance(v_cache, torch.Tensor) or v_cache.dtype != k_cache.dtype or not v_cache.is_cuda or \
-            v_cache.shape != k_cache.shape or v_cache.stride() != k_cache.stride():
+    if not isinstance(v_cache, torch.Tensor) or v_cache.dtype is not dt or not v_cache.is_cuda or \
+            v_cache.shape != shape or v_cache.stride() != strides:
         raise TypeError("v_cache: expected a CUDA tensor of k_cache's type, shape and strides")
-    if not isinstance(table, torch.Tensor) or table.dtype != torch.int32 or table.dim() != 2 or not table.is_cuda or \
-            (table.shape[1] > 1 and table.stride(1) != 1):
+    try:
+        seqs, cols = table.shape
+        ld, step = table.stride()
+    except (AttributeError, ValueError):
+        raise TypeError("table: expected a CUDA int32 2-D tensor with unit column stride") from None
+    if table.dtype is not torch.int32 or not table.is_cuda or (step != 1 and cols > 1):
         raise TypeError("table: expected a CUDA int32 2-D tensor with unit column stride")
-    pages, size, heads, dh = k_cache.shape
-    ps, ts, hs, _ = k_cache.stride()
-    seqs, cols = table.shape
-    return PagedKV(k_cache.data_ptr(), v_cache.data_ptr(), table.data_ptr(), ps if pages > 1 else max(ps, dh),
-                   ts if size > 1 else dh, hs if heads > 1 else dh, DTYPES[k_cache.dtype], pages, size, heads, dh,
-                   seqs, table.stride(0) if seqs > 1 else cols, cols)
+    kv = _PAGED_KV.pack(k_cache.data_ptr(), v_cache.data_ptr(), table.data_ptr(), ps if pages > 1 else max(ps, dh),
+                        ts if size > 1 else dh, hs if heads > 1 else dh, DTYPES[dt], pages, size, heads, dh, seqs,
+                        ld if seqs > 1 else cols, cols)
+    return kv, dt, heads, dh, seqs
 
 
 def p4q_rope_append(q, k, v, cos, sin, pos, k_cache, v_cache, table, q_out, k_out=None, seq=None, rot_pos=None,
                     interleaved=False, stream=None):
     """Rotates q and k of T tokens by their positions and appends k and v to the
-    paged cache. q, q_out [T, H*dh], k, v, k_out [T, Hkv*dh]: 2-D views of the
-    cache's type; cos, sin [positions, rot/2] fp32; pos, rot_pos, seq [T] int32;
-    caches and table as paged_kv(). q_out may be q, and k_out k."""
-    kv = paged_kv(k_cache, v_cache, table)
-    T, dt = q.shape[0], k_cache.dtype
-    _rows16(q, dt, None, "q"); _rows16(q_out, dt, q.shape[1], "q_out")
-    for t, name in ((k, "k"), (v, "v"), (k_out, "k_out")):
-        if t is not None:
-            _rows16(t, dt, kv.Hkv * kv.dh, name)
-    if q.shape[1] % kv.dh:
-        raise ValueError(f"q has {q.shape[1]} columns, not a multiple of the head dimension {kv.dh}")
-    if k.shape[0] != T or v.shape[0] != T or q_out.shape[0] != T or (k_out is not None and k_out.shape[0] != T):
-        raise ValueError("q, k, v and the outputs differ in rows")
+    paged cache (k_cache, v_cache [pages, page_size, Hkv, dh] fp16 or bf16, any
+    order of slots and heads in memory; table [seqs, pages per sequence] int32).
+    q, q_out [T, H*dh], k, v, k_out [T, Hkv*dh]: 2-D views of the cache's type;
+    cos, sin [positions, rot/2] fp32; pos, rot_pos, seq [T] int32. q_out may be
+    q, and k_out k."""
+    kv, dt, heads, dh, _ = _paged_kv(k_cache, v_cache, table)
+    ldq = _rows(q, dt, None, None, "q")
+    T, width = q.shape
+    if width % dh:
+        raise ValueError(f"q has {width} columns, not a multiple of the head dimension {dh}")
+    ldk, ldv = _rows(k, dt, T, heads * dh, "k"), _rows(v, dt, T, heads * dh, "v")
+    ldqo = _rows(q_out, dt, T, width, "q_out")
+    ldko = 0 if k_out is None else _rows(k_out, dt, T, heads * dh, "k_out")
     _need(cos, torch.float32, 2, "cos"); _need(sin, torch.float32, 2, "sin")
-    if cos.shape != sin.shape:
+    max_pos, half = cos.shape
+    if sin.shape != cos.shape:
         raise ValueError("cos and sin differ in shape")
-    if pos is None:
-        raise TypeError("pos: expected a contiguous CUDA torch.int32 vector")
-    _vector(pos, torch.int32, T, "pos"); _vector(rot_pos, torch.int32, T, "rot_pos")
-    _vector(seq, torch.int32, T, "seq")
-    _check(lib().p4q_rope_append(_ptr(q), _ld(q), _ptr(k), _ld(k), _ptr(v), _ld(v), T, q.shape[1] // kv.dh, _ptr(cos),
-                                 _ptr(sin), cos.shape[0], 2 * cos.shape[1], int(interleaved), _ptr(pos),
-                                 _ptr(rot_pos), _ptr(seq), ctypes.byref(kv), _ptr(q_out), _ld(q_out), _ptr(k_out),
-                                 0 if k_out is None else _ld(k_out), _stream(stream)), "p4q_rope_append")
+    status = lib().p4q_rope_append(
+        q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, T, width // dh, cos.data_ptr(), sin.data_ptr(), max_pos,
+        2 * half, 1 if interleaved else 0, _vector(pos, torch.int32, T, "pos"),
+        _optional(rot_pos, torch.int32, T, "rot_pos"), _optional(seq, torch.int32, T, "seq"), kv, q_out.data_ptr(),
+        ldqo, _ptr(k_out), ldko, _stream(stream))
+    if status:
+        raise P4QError(status, "p4q_rope_append")
 
 
 def p4q_paged_attention_workspace_bytes() -> int:
@@ -472,34 +488,32 @@ def p4q_paged_attention_workspace_bytes() -> int:
 
 
 def paged_attention_workspace(device):
-    """A workspace for p4q_paged_attention (zeroed; one per stream)."""
-    return torch.zeros((p4q_paged_attention_workspace_bytes(),), dtype=torch.uint8, device=device)
+    """A workspace for p4q_paged_attention (one per stream)."""
+    return torch.empty((p4q_paged_attention_workspace_bytes(),), dtype=torch.uint8, device=device)
 
 
 def p4q_paged_attention(q, k_cache, v_cache, table, lens, o, ws, scale=None, lse=None, stream=None):
     """Attention of one new token per sequence over its lens[b] cached positions.
     q, o [seqs, H*dh]: 2-D views of the cache's type; lens [seqs] int32; lse
     [seqs, H] fp32 or None; scale defaults to 1 / sqrt(dh); ws as
-    paged_attention_workspace() gives it; caches and table as paged_kv()."""
-    kv = paged_kv(k_cache, v_cache, table)
-    dt = k_cache.dtype
-    _rows16(q, dt, None, "q"); _rows16(o, dt, q.shape[1], "o")
-    H = q.shape[1] // kv.dh
-    if q.shape[1] % kv.dh:
-        raise ValueError(f"q has {q.shape[1]} columns, not a multiple of the head dimension {kv.dh}")
-    if q.shape[0] != kv.seqs or o.shape[0] != kv.seqs:
-        raise ValueError("q, o and the page table differ in sequences")
-    if lens is None:
-        raise TypeError("lens: expected a contiguous CUDA torch.int32 vector")
-    _vector(lens, torch.int32, kv.seqs, "lens")
+    paged_attention_workspace() gives it; caches and table as in p4q_rope_append."""
+    kv, dt, heads, dh, seqs = _paged_kv(k_cache, v_cache, table)
+    ldq = _rows(q, dt, seqs, None, "q")
+    width = q.shape[1]
+    if width % dh:
+        raise ValueError(f"q has {width} columns, not a multiple of the head dimension {dh}")
+    ldo = _rows(o, dt, seqs, width, "o")
     _need(ws, torch.uint8, 1, "ws")
     if lse is not None:
         _need(lse, torch.float32, 2, "lse")
-        if lse.shape != (kv.seqs, H):
-            raise ValueError(f"lse has shape {tuple(lse.shape)}, expected {(kv.seqs, H)}")
-    _check(lib().p4q_paged_attention(_ptr(q), _ld(q), H, ctypes.byref(kv), _ptr(lens),
-                                     kv.dh ** -0.5 if scale is None else float(scale), _ptr(o), _ld(o), _ptr(lse),
-                                     _ptr(ws), ws.numel(), _stream(stream)), "p4q_paged_attention")
+        if lse.shape != (seqs, width // dh):
+            raise ValueError(f"lse has shape {tuple(lse.shape)}, expected {(seqs, width // dh)}")
+    status = lib().p4q_paged_attention(
+        q.data_ptr(), ldq, width // dh, kv, _vector(lens, torch.int32, seqs, "lens"),
+        dh ** -0.5 if scale is None else scale, o.data_ptr(), ldo, _ptr(lse), ws.data_ptr(), ws.numel(),
+        _stream(stream))
+    if status:
+        raise P4QError(status, "p4q_paged_attention")
 
 
 def paged_attention(q, k_cache, v_cache, table, lens, ws=None, scale=None, stream=None):
@@ -516,19 +530,22 @@ def p4q_sample(logits, u, token, logprob=None, temperature=None, top_k=None, top
     unit column stride) with the uniform number u[n]. u, logprob, temperature,
     top_p, min_p [rows] fp32; token, top_k [rows] int32; all but u and token
     optional."""
-    if not isinstance(logits, torch.Tensor) or logits.dtype not in DTYPES or logits.dim() != 2 or \
-            not logits.is_cuda or (logits.shape[1] > 1 and logits.stride(1) != 1):
+    try:
+        rows, vocab = logits.shape
+        ld, step = logits.stride()
+        dt = DTYPES[logits.dtype]
+    except (AttributeError, ValueError, KeyError):
+        raise TypeError("logits: expected a CUDA fp16, bf16 or fp32 2-D tensor with unit column stride") from None
+    if not logits.is_cuda or (step != 1 and vocab > 1):
         raise TypeError("logits: expected a CUDA fp16, bf16 or fp32 2-D tensor with unit column stride")
-    rows, vocab = logits.shape
-    if u is None or token is None:
-        raise TypeError("u and token are needed")
-    for t, dt, name in ((u, torch.float32, "u"), (token, torch.int32, "token"), (logprob, torch.float32, "logprob"),
-                        (temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"),
-                        (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p")):
-        _vector(t, dt, rows, name)
-    _check(lib().p4q_sample(_ptr(logits), DTYPES[logits.dtype], logits.stride(0) if rows > 1 else vocab, rows, vocab,
-                            _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(u), _ptr(token),
-                            _ptr(logprob), _stream(stream)), "p4q_sample")
+    f32 = torch.float32
+    status = lib().p4q_sample(
+        logits.data_ptr(), dt, ld if rows > 1 else vocab, rows, vocab, _optional(temperature, f32, rows, "temperature"),
+        _optional(top_k, torch.int32, rows, "top_k"), _optional(top_p, f32, rows, "top_p"),
+        _optional(min_p, f32, rows, "min_p"), _vector(u, f32, rows, "u"), _vector(token, torch.int32, rows, "token"),
+        _optional(logprob, f32, rows, "logprob"), _stream(stream))
+    if status:
+        raise P4QError(status, "p4q_sample")
 
 
 def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):

@@ -142,7 +142,7 @@ def test_the_binding_refuses_what_it_cannot_pass():
     cache = torch.zeros((16, 16, 4, 128), dtype=torch.float16)
     table = torch.zeros((2, 8), dtype=torch.int32)
     with pytest.raises(TypeError):
-        p4q.paged_kv(cache, cache, table)  # not on a GPU
+        p4q._paged_kv(cache, cache, table)  # not on a GPU
     with pytest.raises(TypeError):
         p4q.p4q_paged_attention(q, cache, cache, table, table[:, 0], q, None)
     with pytest.raises(TypeError):
