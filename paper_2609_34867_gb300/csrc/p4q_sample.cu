@@ -7,25 +7,26 @@
 // then rising index"; each cut is the last token of that head.
 //
 // A cluster of CTAs takes a row; its logits are read once and stay in shared
-// memory, a slice of the row in each CTA (in registers, 32 a thread, the values
-// that the passes below derive from them spilled).
+// memory, a slice of the row in each CTA.
 // A cut is found as follows. A histogram over d in steps of 1 / 92 (counts for
 // top-k, weights for top-p) covers every token whose weight is not 0 (2^31 e^-d
 // rounds to 0 past d = 22.2; those come last and are never drawn, so they take
-// no part). The CTAs add up a slice of the bins each, scan it, and the bin in
-// which the wanted sum is reached follows. Its tokens, mostly a few, go to
-// one list and are ranked. Bins of more tokens than the list holds are divided
-// again by the logits' ordered bit patterns, at most three times (11 of 32 bits
-// each); a bin of equal logits is cut by index. Shared-memory atomics are what
-// a histogram costs, so tokens that the cut cannot reach stay out of it: for
-// top-k those below the k-th of the threads' own maxima (a CTA alone has k tokens
-// above it), for top-p those whose weights, all of them together, are less than
-// what may be cut off.
-// The draw: kept weights per warp (a warp's tokens are consecutive), their prefix
-// over the cluster, and the one warp that contains the drawn number walks
-// its tokens.
+// no part). Every CTA gets the sums of all CTAs' groups of 32 bins, one warp of it
+// finds the group and, from the CTAs' bins of that, the bin in which the wanted
+// sum is reached. The bin's tokens, mostly a few, are gathered in every CTA and
+// ranked. (Two barriers of the cluster per cut; a scan divided among the CTAs and
+// a ranking by one thread per token took 30 k cycles where this takes 7.) Bins
+// of more tokens than the lists hold are
+// divided again by the logits' ordered bit patterns, at most three times (11 of 32
+// bits each); a bin of equal logits is cut by index.
+// The draw: kept weights per CTA (behind a top-p cut they are known from the
+// histogram) and their prefix over the cluster; then the one CTA that contains the
+// drawn number finds the warp (a warp's tokens are consecutive), and that
+// warp walks its tokens.
 #include <climits>
 #include <cuda_runtime.h>
+
+#include <type_traits>
 
 #include "p4q_device.cuh"
 #include "p4q_elem.cuh"
@@ -41,20 +42,25 @@ constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
 constexpr int kBins = 2048;
 constexpr float kBinScale = 92.0f;  // 2047 / 92 = 22.25 > 22.18 = ln(2^32): a token past the bins has weight 0
-constexpr int kList = 512;
+constexpr int kList = 512;          // tokens of a bin that are ranked, at most
+constexpr int kOwn = 256;           // of one CTA
+
+constexpr int kGroups = kBins / 32;
 
 struct Shared {
   uint32_t lo[kBins], hi[kBins];  // counts, or the weights' low and high 16 bits
-  uint32_t lkey[kList], lidx[kList], lw[kList];
+  u64 own[kOwn];                  // the CTA's tokens of the bin: key, complement of the index
+  u64 list[kList];                // the cluster's
+  uint32_t weight[kList];
   u64 warp_sum[kWarps];
-  // written by the other CTAs of the cluster
-  u64 slice_total[kMaxCluster], mass[kMaxCluster], sum[kMaxCluster], ties[kMaxCluster];
-  uint32_t max_key[kMaxCluster], first_max[kMaxCluster];
-  u64 need;
-  uint32_t bin, cut_key, cut_idx;
-  uint32_t list_n, key_min, key_max;  // (of the cluster's first CTA)
+  // values of each CTA of the cluster, written by it
+  u64 group[kMaxCluster][kGroups];  // its sums over 32 bins
+  u64 mass[kMaxCluster];
+  uint32_t max_key[kMaxCluster], first_max[kMaxCluster], own_n[kMaxCluster], key_min[kMaxCluster], key_max[kMaxCluster];
+  u64 need, total, draw;
+  u64 cut;                        // the last kept token
+  uint32_t bin, n, kmin, kmax;    // of the CTA's list: its length, smallest and largest key
   uint32_t red[kWarps];
-  int last_bin;  // (of this CTA)
 };
 
 __device__ __forceinline__ float float_of_key(uint32_t k) {
@@ -67,18 +73,14 @@ __device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t a) {
   return v;
 }
 
-__device__ __forceinline__ uint32_t add_cluster_u32(uint32_t a, uint32_t v) {
-  uint32_t old;
-  asm volatile("atom.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(old) : "r"(a), "r"(v) : "memory");
-  return old;
+__device__ __forceinline__ u64 ld_cluster_u64(uint32_t a) {
+  u64 v;
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a) : "memory");
+  return v;
 }
 
-__device__ __forceinline__ void min_cluster_u32(uint32_t a, uint32_t v) {
-  asm volatile("red.shared::cluster.min.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory");
-}
-
-__device__ __forceinline__ void max_cluster_u32(uint32_t a, uint32_t v) {
-  asm volatile("red.shared::cluster.max.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory");
+__device__ __forceinline__ void st_shared_cluster_u64(uint32_t a, u64 v) {
+  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(v) : "memory");
 }
 
 __device__ __forceinline__ u64 warp_add(u64 v) {
@@ -108,14 +110,20 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
     if (cs > 1) cluster_sync();
     else __syncthreads();
   };
-  auto put32 = [&](uint32_t* p, uint32_t v) {  // the variable in every CTA of the cluster
+  // The variable in every CTA of the cluster: by one thread, or by a warp's lanes.
+  auto put32 = [&](uint32_t* p, uint32_t v) {
     for (int r = 0; r < cs; ++r) st_shared_cluster_u32(mapa_shared(smem_u32(p), r), v);
   };
   auto put64 = [&](u64* p, u64 v) {
     put32(reinterpret_cast<uint32_t*>(p), static_cast<uint32_t>(v));
     put32(reinterpret_cast<uint32_t*>(p) + 1, static_cast<uint32_t>(v >> 32));
   };
-  auto at_first = [&](uint32_t* p) { return mapa_shared(smem_u32(p), 0); };
+  auto put64_lanes = [&](u64* p, u64 v) {
+    if (lane < cs) st_shared_cluster_u64(mapa_shared(smem_u32(p), lane), v);
+  };
+  auto put32_lanes = [&](uint32_t* p, uint32_t v) {
+    if (lane < cs) st_shared_cluster_u32(mapa_shared(smem_u32(p), lane), v);
+  };
 
   pdl_wait();
   pdl_launch_dependents();
@@ -129,7 +137,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
   row -= skip * kSize;
   const int w0 = (rank * kWarps + warp) * steps * 128;  // the warp's first element
   float4* const mine4 = xs + warp * steps * 32;
-  auto clean = [](float v) { return v != v ? -INFINITY : v + 0.0f; };  // NaN counts as -inf, -0 as +0
+  auto clean = [](float v) { return fmaxf(v, -INFINITY); };  // NaN counts as -inf
   float mx = -INFINITY;
   if (kType == 2) {
 #pragma unroll 4
@@ -183,9 +191,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
       mine4[(st * 32 + lane) * 2 + 1] = make_float4(f[4], f[5], f[6], f[7]);
     }
   }
-  const float own_max = mx;
   __syncwarp();
-  // f(logit, token) for this lane's four tokens of a step
+  // f(logit, token) for this lane's four tokens of a step; for all of them
   const int i0 = w0 + lane * 4 - skip;
   auto four = [&](int st, auto&& f) {
     const float4 v = mine4[st * 32 + lane];
@@ -199,20 +206,16 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
 #pragma unroll 2
     for (int st = 0; st < steps; ++st) four(st, f);
   };
+  auto key_of = [](float v) { return float_order_key(v + 0.0f); };  // (-0 as +0)
 
   // the row's largest logit
   {
-    const uint32_t k = __reduce_max_sync(0xFFFFFFFFu, float_order_key(mx));
+    const uint32_t k = __reduce_max_sync(0xFFFFFFFFu, key_of(mx));
     if (lane == 0) s.red[warp] = k;
-    if (tid == 0) {
-      s.list_n = 0;
-      s.key_min = 0xFFFFFFFFu;
-      s.key_max = 0;
-    }
     __syncthreads();
     if (warp == 0) {
       const uint32_t all = __reduce_max_sync(0xFFFFFFFFu, s.red[lane & (kWarps - 1)]);
-      if (lane == 0) put32(&s.max_key[rank], all);
+      put32_lanes(&s.max_key[rank], all);
     }
     sync_all();
     uint32_t best = s.max_key[0];
@@ -237,7 +240,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
     __syncthreads();
     if (tid == 0) {
       for (int w = 1; w < kWarps; ++w) first = min(first, s.red[w]);
-      st_shared_cluster_u32(at_first(&s.first_max[rank]), first);
+      st_shared_cluster_u32(mapa_shared(smem_u32(&s.first_max[rank]), 0), first);
     }
     sync_all();
     if (rank == 0 && tid == 0) {
@@ -260,234 +263,181 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
   };
   float cut_x = -INFINITY;  // the last kept token
   int cut_i = INT_MAX;
-  auto keeps = [&](float v, int i) { return v > cut_x || (v == cut_x && i <= cut_i); };
-  // A sum over the cluster's threads; *before: that of the warps before this one.
-  auto sum_all = [&](u64 v, u64* slots, u64* before) -> u64 {
-    v = warp_add(v);
-    __syncthreads();  // (the sums of a scan before have been read)
-    if (lane == 0) s.warp_sum[warp] = v;
-    __syncthreads();
-    u64 cta = 0, at = 0;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      if (w < warp) at += s.warp_sum[w];
-      cta += s.warp_sum[w];
-    }
-    if (tid == 0) put64(&slots[rank], cta);
-    sync_all();
-    u64 total = 0;
-    for (int r = 0; r < cs; ++r) {
-      if (r < rank) at += slots[r];
-      total += slots[r];
-    }
-    *before = at;
-    return total;
-  };
+  auto keeps = [&](float v, int i) { return v >= cut_x && !(v == cut_x && i > cut_i); };
+  u64 cta_mass = 0;  // the kept weights of the CTA, where known
+  bool known = false;
 
-  // Shortens the kept head: to `need` tokens (by_mass false), or to the first
-  // tokens whose weights reach ceil(share * the kept weights' sum).
-  auto shorten = [&](const bool by_mass, u64 need, float share) {
-    const bool all_kept = cut_x == -INFINITY;
-    auto reach = [&](u64 total) -> u64 {
-      const double want = ceil(static_cast<double>(share) * static_cast<double>(total));
-      return want < 1.0 ? 1ull : static_cast<u64>(want);
-    };
-    int last_bin = kBins - 1;  // tokens of later bins are past the cut
-    if (by_mass && all_kept) {
-      u64 sum = 0, before;
-      each([&](float v, int i) { sum += weight(dist(v)); });
-      sum = sum_all(sum, s.sum, &before);
-      need = reach(sum);
-      // Tokens of weight <= (sum - need) / V have no more than sum - need together. Bin b + 1 begins half a
-      // bin behind b's middle, and a weight is off by half a unit: one unit and one bin less.
-      const float spare = static_cast<float>((sum - need) / static_cast<unsigned int>(V));
-      if (spare > 2.0f) last_bin = min(last_bin, static_cast<int>((21.487563f - logf(spare - 1.0f)) * kBinScale) + 2);
-    }
-    for (int i = tid; i < kBins; i += kThreads) {
-      s.lo[i] = 0;
-      s.hi[i] = 0;
-    }
-    __syncthreads();
-    if (!by_mass && need <= kThreads) {
-      // the bin of the need-th of the threads' largest logits (in the array that counts leave free)
-      int bin;
-      if (d_bin(dist(own_max), &bin)) atomicAdd(&s.hi[bin], 1u);
-      if (tid == 0) s.last_bin = kBins - 1;
-      __syncthreads();
-      constexpr int kPer = kBins / kThreads;
-      uint32_t c[kPer], own = 0;
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) {
-        c[j] = s.hi[tid * kPer + j];
-        own += c[j];
-      }
-      uint32_t upto = own;
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, upto, d);
-        if (lane >= d) upto += v;
-      }
-      if (lane == 31) s.red[warp] = upto;
-      __syncthreads();
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w)
-        if (w < warp) upto += s.red[w];
-      if (own > 0 && upto >= need && upto - own < need) {
-        uint32_t at = upto - own;
-        int j = 0;
-        while ((at += c[j]) < need) ++j;
-        s.last_bin = tid * kPer + j;
-      }
-      __syncthreads();
-      last_bin = s.last_bin;
-    }
+  // Shortens the kept head: to `need` tokens, or (by_mass) to the first tokens
+  // whose weights reach ceil(share * the kept weights' sum).
+  auto shorten = [&](auto mass_c, u64 need, float share) {
+    constexpr bool by_mass = decltype(mass_c)::value;
     uint32_t key_lo = 0, key_hi = 0;
     int shift = 0;
+    u64 below = 0;  // (by_mass) the CTA's weights before the bin
     for (int level = 0;; ++level) {
-      // the bin of a token (falling logits have rising bins), or -1
-      auto bin_of = [&](float v, int i) -> int {
-        if (level == 0) {
-          int bin;
-          return d_bin(dist(v), &bin) && bin <= last_bin && keeps(v, i) ? bin : -1;
-        }
-        const uint32_t k = float_order_key(v);
-        return k >= key_lo && k <= key_hi && keeps(v, i) ? static_cast<int>((key_hi - k) >> shift) : -1;
-      };
-      if (level > 0) {
-        for (int i = tid; i < kBins; i += kThreads) {
-          s.lo[i] = 0;
-          s.hi[i] = 0;
-        }
-        __syncthreads();
+      for (int i = tid; i < kBins; i += kThreads) {
+        s.lo[i] = 0;
+        if (by_mass) s.hi[i] = 0;
       }
+      if (tid == 0) {
+        s.n = 0;
+        s.kmin = 0xFFFFFFFFu;
+        s.kmax = 0;
+      }
+      __syncthreads();
+      // the bin of a token (falling logits have rising bins), or false
+      auto bin_of = [&](float v, float d, int* bin) {
+        if (level == 0) return d_bin(d, bin);
+        const uint32_t k = key_of(v);
+        *bin = static_cast<int>((key_hi - k) >> shift);
+        return k >= key_lo && k <= key_hi;
+      };
       each([&](float v, int i) {
-        const int bin = bin_of(v, i);
-        if (bin >= 0) {
-          if (by_mass) {
-            const uint32_t w = weight(dist(v));
-            atomicAdd(&s.lo[bin], w & 0xFFFFu);
-            if (w >> 16) atomicAdd(&s.hi[bin], w >> 16);
-          } else {
-            atomicAdd(&s.lo[bin], 1u);
-          }
+        if (by_mass && !keeps(v, i)) return;
+        const float d = dist(v);
+        int bin;
+        if (!bin_of(v, d, &bin)) return;
+        if (by_mass) {
+          const uint32_t w = weight(d);
+          atomicAdd(&s.lo[bin], w & 0xFFFFu);
+          if (w >> 16) atomicAdd(&s.hi[bin], w >> 16);
+        } else {
+          atomicAdd(&s.lo[bin], 1u);
         }
       });
-      sync_all();
-      if (rank == 0 && tid == 0) {
-        s.list_n = 0;
-        s.key_min = 0xFFFFFFFFu;
-        s.key_max = 0;
-      }
-      // this CTA's slice of the bins over the cluster, `per` bins per thread
-      const int slice = kBins / cs, per = max(1, slice / kThreads);
-      u64 bins[kBins / kThreads], own = 0;
-#pragma unroll
-      for (int j = 0; j < kBins / kThreads; ++j) {
-        bins[j] = 0;
-        if (j < per && tid * per < slice) {
-          const int bin = rank * slice + tid * per + j;
-#pragma unroll
-          for (int r = 0; r < kMaxCluster; ++r)
-            if (r < cs) {
-              bins[j] += ld_cluster_u32(mapa_shared(smem_u32(&s.lo[bin]), r));
-              if (by_mass) bins[j] += static_cast<u64>(ld_cluster_u32(mapa_shared(smem_u32(&s.hi[bin]), r))) << 16;
-            }
-        }
-        own += bins[j];
-      }
-      u64 upto = warp_scan(own);
-      if (lane == 31) s.warp_sum[warp] = upto;
       __syncthreads();
-      u64 all = 0;
+      // sums of 32 bins each, to every CTA
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        if (w < warp) upto += s.warp_sum[w];
-        all += s.warp_sum[w];
-      }
-      if (tid == 0) put64(&s.slice_total[rank], all);
-      sync_all();
-      u64 total = 0;
-      for (int r = 0; r < cs; ++r) {
-        if (r < rank) upto += s.slice_total[r];
-        total += s.slice_total[r];
-      }
-      if (level == 0) {
-        if (by_mass && !all_kept) need = reach(total);
-        if (total < need) return;  // fewer tokens than `need` may be drawn at all
-      }
-      if (own > 0 && upto - own < need && need <= upto) {
-        u64 at = upto - own;
-        int j = 0;
-        while (j + 1 < per && at + bins[j] < need) at += bins[j++];
-        put32(&s.bin, static_cast<uint32_t>(rank * slice + tid * per + j));
-        put64(&s.need, need - at);
+      for (int j = 0; j < kGroups / kWarps; ++j) {
+        const int g = warp * (kGroups / kWarps) + j;
+        u64 v = s.lo[g * 32 + lane];
+        if (by_mass) v += static_cast<u64>(s.hi[g * 32 + lane]) << 16;
+        v = warp_add(v);
+        put64_lanes(&s.group[rank][g], v);
       }
       sync_all();
-      const int bin = static_cast<int>(s.bin);
+      if (warp == 0) {  // the group, then the bin in which the sum is reached
+        u64 g0 = 0, g1 = 0;
+#pragma unroll
+        for (int r = 0; r < kMaxCluster; ++r)
+          if (r < cs) {
+            g0 += s.group[r][2 * lane];
+            g1 += s.group[r][2 * lane + 1];
+          }
+        u64 upto = warp_scan(g0 + g1);
+        const u64 total = __shfl_sync(0xFFFFFFFFu, upto, 31);
+        u64 want = need;
+        if (by_mass && level == 0) {
+          const double part = ceil(static_cast<double>(share) * static_cast<double>(total));
+          want = part < 1.0 ? 1ull : static_cast<u64>(part);
+        }
+        // (not reached at all: the last group, and the caller goes by `total`)
+        const uint32_t there = __ballot_sync(0xFFFFFFFFu, upto >= want);
+        const int at_lane = there ? __ffs(there) - 1 : 31;
+        const u64 before = upto - g0 - g1;
+        const bool second = before + g0 < want;
+        const int g = __shfl_sync(0xFFFFFFFFu, 2 * lane + (second ? 1 : 0), at_lane);
+        want -= __shfl_sync(0xFFFFFFFFu, second ? before + g0 : before, at_lane);
+        u64 v = 0;
+#pragma unroll
+        for (int r = 0; r < kMaxCluster; ++r)
+          if (r < cs) {
+            v += ld_cluster_u32(mapa_shared(smem_u32(&s.lo[g * 32 + lane]), r));
+            if (by_mass) v += static_cast<u64>(ld_cluster_u32(mapa_shared(smem_u32(&s.hi[g * 32 + lane]), r))) << 16;
+          }
+        upto = warp_scan(v);
+        if (upto >= want && upto - v < want) {
+          s.bin = static_cast<uint32_t>(g * 32 + lane);
+          s.need = want - (upto - v);
+        }
+        if (lane == 0) s.total = total;
+      }
+      __syncthreads();
+      if (!by_mass && level == 0 && s.total <= need) return;  // every token that may be drawn is among the first `need`
+      const int cut_bin = static_cast<int>(s.bin);
       need = s.need;
-      // its tokens into the first CTA's list
-      uint32_t c = 0, kmin = 0xFFFFFFFFu, kmax = 0;
+      // The bin's tokens of this CTA; what it has before them.
+      uint32_t kmin = 0xFFFFFFFFu, kmax = 0;
       each([&](float v, int i) {
-        if (bin_of(v, i) == bin) {
-          const uint32_t k = float_order_key(v);
-          ++c;
+        int bin;
+        const bool in = bin_of(v, dist(v), &bin) && bin == cut_bin && (!by_mass || keeps(v, i));
+        const uint32_t with = __ballot_sync(0xFFFFFFFFu, in);
+        if (with == 0) return;
+        uint32_t at = 0;
+        if (lane == 0) at = atomicAdd(&s.n, static_cast<uint32_t>(__popc(with)));
+        at = __shfl_sync(0xFFFFFFFFu, at, 0) + static_cast<uint32_t>(__popc(with & ((1u << lane) - 1u)));
+        if (in) {
+          const uint32_t k = key_of(v);
           kmin = min(kmin, k);
           kmax = max(kmax, k);
+          if (at < kOwn) s.own[at] = static_cast<u64>(k) << 32 | static_cast<uint32_t>(~i);
         }
       });
-      const uint32_t in_warp = __reduce_add_sync(0xFFFFFFFFu, c);
-      if (in_warp > 0) {
-        kmin = __reduce_min_sync(0xFFFFFFFFu, kmin);
-        kmax = __reduce_max_sync(0xFFFFFFFFu, kmax);
-        const uint32_t before = static_cast<uint32_t>(warp_scan(c)) - c;
-        uint32_t at = 0;
-        if (lane == 0) {
-          at = add_cluster_u32(at_first(&s.list_n), in_warp);
-          min_cluster_u32(at_first(&s.key_min), kmin);
-          max_cluster_u32(at_first(&s.key_max), kmax);
-        }
-        at = __shfl_sync(0xFFFFFFFFu, at, 0) + before;
-        if (c > 0 && at < kList) {
-          each([&](float v, int i) {
-            if (bin_of(v, i) == bin && at < kList) {
-              st_shared_cluster_u32(at_first(&s.lkey[at]), float_order_key(v));
-              st_shared_cluster_u32(at_first(&s.lidx[at]), static_cast<uint32_t>(i));
-              if (by_mass) st_shared_cluster_u32(at_first(&s.lw[at]), weight(dist(v)));
-              ++at;
-            }
-          });
-        }
+      if (kmin <= kmax) {
+        atomicMin(&s.kmin, kmin);
+        atomicMax(&s.kmax, kmax);
+      }
+      if (by_mass) {
+        u64 sum = 0;
+        for (int i = tid; i < cut_bin; i += kThreads) sum += s.lo[i] + (static_cast<u64>(s.hi[i]) << 16);
+        sum = warp_add(sum);
+        if (lane == 0) s.warp_sum[warp] = sum;
+      }
+      __syncthreads();
+      if (by_mass) {
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) below += s.warp_sum[w];
+      }
+      if (warp == 0) {
+        put32_lanes(&s.own_n[rank], s.n);
+        put32_lanes(&s.key_min[rank], s.kmin);
+        put32_lanes(&s.key_max[rank], s.kmax);
       }
       sync_all();
-      const uint32_t found = ld_cluster_u32(at_first(&s.list_n));
-      key_lo = ld_cluster_u32(at_first(&s.key_min));
-      key_hi = ld_cluster_u32(at_first(&s.key_max));
-      if (found <= kList) {  // every CTA ranks them for itself
-        uint32_t k = 0, i = 0, w = 1;
-        if (tid < static_cast<int>(found)) {
-          k = ld_cluster_u32(at_first(&s.lkey[tid]));
-          i = ld_cluster_u32(at_first(&s.lidx[tid]));
-          if (by_mass) w = ld_cluster_u32(at_first(&s.lw[tid]));
-          if (rank > 0) {
-            s.lkey[tid] = k;
-            s.lidx[tid] = i;
-            if (by_mass) s.lw[tid] = w;
-          }
+      uint32_t found = 0, most = 0;
+      key_lo = 0xFFFFFFFFu;
+      key_hi = 0;
+      for (int r = 0; r < cs; ++r) {
+        found += s.own_n[r];
+        most = max(most, s.own_n[r]);
+        key_lo = min(key_lo, s.key_min[r]);
+        key_hi = max(key_hi, s.key_max[r]);
+      }
+      if (found <= kList && most <= kOwn) {  // every CTA ranks them for itself
+        for (uint32_t i = tid; i < found; i += kThreads) {
+          int r = 0;
+          uint32_t j = i;
+          while (j >= s.own_n[r]) j -= s.own_n[r++];
+          const u64 t = ld_cluster_u64(mapa_shared(smem_u32(&s.own[j]), r));
+          s.list[i] = t;
+          if (by_mass) s.weight[i] = weight(dist(float_of_key(static_cast<uint32_t>(t >> 32))));
         }
         __syncthreads();
-        if (tid < static_cast<int>(found)) {
+        for (uint32_t i = warp; i < found; i += kWarps) {  // a warp per token: what comes before it
+          const u64 t = s.list[i];
           u64 before = 0;
-          for (uint32_t j = 0; j < found; ++j) {
-            const uint32_t kj = s.lkey[j];
-            if (kj > k || (kj == k && s.lidx[j] < i)) before += by_mass ? s.lw[j] : 1u;
+          if (by_mass) {
+            for (uint32_t j = lane; j < found; j += 32) before += s.list[j] > t ? s.weight[j] : 0u;
+            before = warp_add(before);
+          } else {
+            uint32_t c = 0;
+            for (uint32_t j = lane; j < found; j += 32) c += s.list[j] > t ? 1u : 0u;
+            before = __reduce_add_sync(0xFFFFFFFFu, c);
           }
-          if (before < need && need <= before + w) {
-            s.cut_key = k;
-            s.cut_idx = i;
-          }
+          if (before < need && need <= before + (by_mass ? s.weight[i] : 1u) && lane == 0) s.cut = t;
         }
         __syncthreads();
-        break;
+        const u64 last = s.cut;
+        cut_x = float_of_key(static_cast<uint32_t>(last >> 32));
+        cut_i = static_cast<int>(~static_cast<uint32_t>(last));
+        if (by_mass) {
+          u64 sum = 0;
+          for (uint32_t j = lane; j < s.own_n[rank]; j += 32)
+            if (s.own[j] >= last) sum += weight(dist(float_of_key(static_cast<uint32_t>(s.own[j] >> 32))));
+          cta_mass = below + warp_add(sum);
+          known = true;
+        }
+        return;
       }
       if (key_lo == key_hi) {  // equal logits: so many of them, by index
         const float v = float_of_key(key_lo);
@@ -499,27 +449,22 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
         uint32_t m = 0;
         each([&](float u, int i) { m += same(u, i) ? 1u : 0u; });
         m = __reduce_add_sync(0xFFFFFFFFu, m);
+        __syncthreads();
         if (lane == 0) s.red[warp] = m;
         __syncthreads();
-        u64 cta = 0, first = 0;
-        for (int w = 0; w < kWarps; ++w) {
-          if (w < warp) first += s.red[w];
-          cta += s.red[w];
-        }
-        if (tid == 0) put64(&s.ties[rank], cta);
-        sync_all();
-        for (int r = 0; r < rank; ++r) first += s.ties[r];
+        u64 first = 0;
+        for (int w = 0; w < warp; ++w) first += s.red[w];
+        for (int r = 0; r < rank; ++r) first += s.own_n[r];
         if (first < need && need <= first + m) {  // (the warp alike)
           for (int st = 0; st < steps && first < need; ++st) {
-            uint32_t mine = 0;
-            four(st, [&](float u, int i) { mine += same(u, i) ? 1u : 0u; });
-            const u64 to = first + warp_scan(mine);
-            if (to - mine < need && need <= to) {
-              u64 at = to - mine;
+            uint32_t c = 0;
+            four(st, [&](float u, int i) { c += same(u, i) ? 1u : 0u; });
+            const u64 to = first + warp_scan(c);
+            if (to - c < need && need <= to) {
+              u64 at = to - c;
               four(st, [&](float u, int i) {
                 if (same(u, i) && ++at == need) {
-                  put32(&s.cut_key, key_lo);
-                  put32(&s.cut_idx, static_cast<uint32_t>(i));
+                  put64(&s.cut, static_cast<uint32_t>(i));
                 }
               });
             }
@@ -527,19 +472,19 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
           }
         }
         sync_all();
-        break;
+        cut_x = v;
+        cut_i = static_cast<int>(s.cut);
+        return;
       }
       const int bits = 32 - __clz(key_hi - key_lo);
       shift = max(0, bits - 11);
     }
-    cut_x = float_of_key(s.cut_key);
-    cut_i = static_cast<int>(s.cut_idx);
   };
 
   const int top_k = a.top_k ? a.top_k[n] : 0;
-  if (top_k > 0 && top_k < V) shorten(false, static_cast<u64>(top_k), 0.0f);
+  if (top_k > 0 && top_k < V) shorten(std::false_type{}, static_cast<u64>(top_k), 0.0f);
   const float top_p = a.top_p ? a.top_p[n] : 1.0f;
-  if (top_p < 1.0f) shorten(true, 0, top_p);
+  if (top_p < 1.0f) shorten(std::true_type{}, 0, top_p);
 
   const float min_p = a.min_p && a.min_p[n] > 0.0f ? fminf(a.min_p[n], 1.0f) : 0.0f;
   // past d_max exp(-d) < min_p for certain (weights are 0 past 22.2)
@@ -550,13 +495,39 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
     const float e = expf(-d);
     return e < min_p ? 0u : __float2uint_rn(e * 2147483648.0f);
   };
-  u64 mine = 0, at;
-  each([&](float v, int i) { mine += kept(v, i); });
-  mine = warp_add(mine);
-  const u64 total = sum_all(lane == 0 ? mine : 0ull, s.mass, &at);
-  const double want = floor(static_cast<double>(a.u[n]) * static_cast<double>(total));
-  u64 r = want > 0.0 ? static_cast<u64>(fmin(want, 9.0e15)) : 0ull;
-  if (r > total - 1) r = total - 1;
+  u64 mine = 0;  // of the warp
+  auto add_warps = [&]() {
+    u64 sum = 0;
+    each([&](float v, int i) { sum += kept(v, i); });
+    mine = warp_add(sum);
+    __syncthreads();  // (the sums of a scan before have been read)
+    if (lane == 0) s.warp_sum[warp] = mine;
+    __syncthreads();
+  };
+  known = known && min_p == 0.0f;
+  if (!known) {
+    add_warps();
+    cta_mass = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) cta_mass += s.warp_sum[w];
+  }
+  if (warp == 0) put64_lanes(&s.mass[rank], cta_mass);
+  sync_all();
+  if (tid == 0) {  // (64-bit floating point is slow: once)
+    u64 total = 0;
+    for (int r = 0; r < cs; ++r) total += s.mass[r];
+    const double want = floor(static_cast<double>(a.u[n]) * static_cast<double>(total));
+    const u64 r = want > 0.0 ? static_cast<u64>(fmin(want, 9.0e15)) : 0ull;
+    s.draw = min(r, total - 1);
+    s.total = total;
+  }
+  __syncthreads();
+  const u64 r = s.draw, total = s.total;
+  u64 at = 0;
+  for (int k = 0; k < rank; ++k) at += s.mass[k];
+  if (r < at || r >= at + s.mass[rank]) return;  // another CTA's
+  if (known) add_warps();
+  for (int w = 0; w < warp; ++w) at += s.warp_sum[w];
   if (at <= r && r < at + mine) {  // (the warp alike)
     for (int st = 0; st < steps && at <= r; ++st) {
       u64 c = 0;
