@@ -139,57 +139,69 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
   float4* const mine4 = xs + warp * steps * 32;
   auto clean = [](float v) { return fmaxf(v, -INFINITY); };  // NaN counts as -inf
   float mx = -INFINITY;
-  if (kType == 2) {
-#pragma unroll 4
-    for (int st = 0; st < steps; ++st) {
-      const int e = w0 + (st * 32 + lane) * 4;
-      float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-      const float* p = reinterpret_cast<const float*>(row) + e;
-      if (e >= skip && e + 4 <= end) {
-        v = *reinterpret_cast<const float4*>(p);
-      } else {
-        if (e >= skip && e < end) v.x = p[0];
-        if (e + 1 >= skip && e + 1 < end) v.y = p[1];
-        if (e + 2 >= skip && e + 2 < end) v.z = p[2];
-        if (e + 3 >= skip && e + 3 < end) v.w = p[3];
-      }
-      v = make_float4(clean(v.x), clean(v.y), clean(v.z), clean(v.w));
-      mine4[st * 32 + lane] = v;
-      mx = fmaxf(fmaxf(fmaxf(mx, v.x), fmaxf(v.y, v.z)), v.w);
-    }
-  } else {
-    // 8 elements per lane and 16-byte piece (steps is even)
-#pragma unroll 4
-    for (int st = 0; st < steps / 2; ++st) {
-      const int e = w0 + (st * 32 + lane) * 8;
-      const uint16_t* p = reinterpret_cast<const uint16_t*>(row) + e;
-      uint32_t raw[4];
-      if (e >= skip && e + 8 <= end) {
-        const uint4 v = *reinterpret_cast<const uint4*>(p);
-        raw[0] = v.x;
-        raw[1] = v.y;
-        raw[2] = v.z;
-        raw[3] = v.w;
-      } else {
-        constexpr uint32_t kNone = kType == 1 ? 0xFF80u : 0xFC00u;  // -inf
+  // 16 bytes of the row from element e on, -inf where it has none
+  auto edge = [&](int e) {
+    uint32_t raw[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t l = e + 2 * j >= skip && e + 2 * j < end ? p[2 * j] : kNone;
-          const uint32_t h = e + 2 * j + 1 >= skip && e + 2 * j + 1 < end ? p[2 * j + 1] : kNone;
-          raw[j] = l | (h << 16);
-        }
+    for (int j = 0; j < 4; ++j) {
+      if (kType == 2) {
+        raw[j] = e + j >= skip && e + j < end ? reinterpret_cast<const uint32_t*>(row)[e + j] : 0xFF800000u;
+      } else {
+        constexpr uint32_t kNone = kType == 1 ? 0xFF80u : 0xFC00u;
+        const uint16_t* p = reinterpret_cast<const uint16_t*>(row);
+        const int m = e + 2 * j;
+        const uint32_t l = m >= skip && m < end ? p[m] : kNone;
+        const uint32_t h = m + 1 >= skip && m + 1 < end ? p[m + 1] : kNone;
+        raw[j] = l | (h << 16);
       }
+    }
+    return make_uint4(raw[0], raw[1], raw[2], raw[3]);
+  };
+  // load k of this lane: 16 bytes, 4 or 8 logits
+  auto keep = [&](int k, uint4 raw) {
+    if (kType == 2) {
+      const float4 v = make_float4(clean(__uint_as_float(raw.x)), clean(__uint_as_float(raw.y)),
+                                   clean(__uint_as_float(raw.z)), clean(__uint_as_float(raw.w)));
+      mine4[k * 32 + lane] = v;
+      mx = fmaxf(fmaxf(fmaxf(mx, v.x), fmaxf(v.y, v.z)), v.w);
+    } else {
+      const uint32_t r[4] = {raw.x, raw.y, raw.z, raw.w};
       float f[8];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float2 v = unpack2<kType == 1>(raw[j]);
+        const float2 v = unpack2<kType == 1>(r[j]);
         f[2 * j] = clean(v.x);
         f[2 * j + 1] = clean(v.y);
         mx = fmaxf(mx, fmaxf(f[2 * j], f[2 * j + 1]));
       }
-      mine4[(st * 32 + lane) * 2] = make_float4(f[0], f[1], f[2], f[3]);
-      mine4[(st * 32 + lane) * 2 + 1] = make_float4(f[4], f[5], f[6], f[7]);
+      mine4[(k * 32 + lane) * 2] = make_float4(f[0], f[1], f[2], f[3]);
+      mine4[(k * 32 + lane) * 2 + 1] = make_float4(f[4], f[5], f[6], f[7]);
     }
+  };
+  constexpr int kPer = 16 / kSize;  // logits per load
+  const int loads = steps * 128 / (32 * kPer);
+  int k = 0;
+  if (w0 >= skip && w0 + steps * 128 <= end) {  // (the warp alike) all inside the row: eight loads in flight
+    const uint4* src = reinterpret_cast<const uint4*>(row + static_cast<size_t>(w0) * kSize) + lane;
+    for (; k + 8 <= loads; k += 8) {
+      uint4 raw[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) raw[j] = src[(k + j) * 32];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) keep(k + j, raw[j]);
+    }
+    for (; k + 2 <= loads; k += 2) {
+      const uint4 r0 = src[k * 32], r1 = src[(k + 1) * 32];
+      keep(k, r0);
+      keep(k + 1, r1);
+    }
+  }
+  for (; k < loads; ++k) {
+    const int e = w0 + (k * 32 + lane) * kPer;
+    uint4 raw;
+    if (e >= skip && e + kPer <= end) raw = *reinterpret_cast<const uint4*>(row + static_cast<size_t>(e) * kSize);
+    else raw = edge(e);
+    keep(k, raw);
   }
   __syncwarp();
   // f(logit, token) for this lane's four tokens of a step; for all of them
@@ -256,11 +268,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
   // (the largest itself: 0, also where the product is NaN: of infinite logits, of a denormal T)
   auto dist = [&](float v) { return fmaxf((mx - v) * inv_t, 0.0f); };
   auto weight = [&](float d) { return __float2uint_rn(expf(-d) * 2147483648.0f); };
-  auto d_bin = [&](float d, int* bin) {  // false: past the bins
-    const float f = fmaf(d, kBinScale, 8388608.0f);  // d in bins, rounded, behind 2^23
-    *bin = __float_as_int(f) & 0x7FFFFF;
-    return f < 8388608.0f + kBins;
-  };
+  // the bin of d = dist(v): rounded to an integer behind 2^23 (the largest logit itself: 0, as in dist)
+  constexpr float kBinBase = 8388608.0f;
+  const float bin_scale = inv_t * kBinScale;
+  auto d_bin = [&](float v) { return fmaxf(fmaf(mx - v, bin_scale, kBinBase), kBinBase); };
   float cut_x = -INFINITY;  // the last kept token
   int cut_i = INT_MAX;
   auto keeps = [&](float v, int i) { return v >= cut_x && !(v == cut_x && i > cut_i); };
@@ -285,26 +296,40 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
         s.kmax = 0;
       }
       __syncthreads();
-      // the bin of a token (falling logits have rising bins), or false
-      auto bin_of = [&](float v, float d, int* bin) {
-        if (level == 0) return d_bin(d, bin);
+      // the bin of a token behind kBinBase's bit pattern (falling logits have rising bins); past the bins: larger
+      auto bin_of = [&](float v) -> int {
+        if (level == 0) return __float_as_int(d_bin(v));
         const uint32_t k = key_of(v);
-        *bin = static_cast<int>((key_hi - k) >> shift);
-        return k >= key_lo && k <= key_hi;
+        return k >= key_lo && k <= key_hi ? __float_as_int(kBinBase) + static_cast<int>((key_hi - k) >> shift) : INT_MAX;
       };
-      each([&](float v, int i) {
-        if (by_mass && !keeps(v, i)) return;
-        const float d = dist(v);
-        int bin;
-        if (!bin_of(v, d, &bin)) return;
-        if (by_mass) {
-          const uint32_t w = weight(d);
-          atomicAdd(&s.lo[bin], w & 0xFFFFu);
-          if (w >> 16) atomicAdd(&s.hi[bin], w >> 16);
-        } else {
-          atomicAdd(&s.lo[bin], 1u);
+#pragma unroll 2
+      for (int st = 0; st < steps; ++st) {
+        const float4 v4 = mine4[st * 32 + lane];
+        const float v[4] = {v4.x, v4.y, v4.z, v4.w};
+        uint32_t bin[4], w[4];
+        bool any = false;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          bin[j] = static_cast<uint32_t>(bin_of(v[j]) - __float_as_int(kBinBase));
+          if (by_mass && !keeps(v[j], i0 + st * 128 + j)) bin[j] = kBins;
+          any = any || bin[j] < kBins;
         }
-      });
+        if (!any) continue;
+        if (by_mass) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) w[j] = weight(dist(v[j]));
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (bin[j] >= kBins) continue;
+          if (by_mass) {
+            atomicAdd(&s.lo[bin[j]], w[j] & 0xFFFFu);
+            if (w[j] >> 16) atomicAdd(&s.hi[bin[j]], w[j] >> 16);
+          } else {
+            atomicAdd(&s.lo[bin[j]], 1u);
+          }
+        }
+      }
       __syncthreads();
       // sums of 32 bins each, to every CTA
 #pragma unroll
@@ -358,9 +383,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
       need = s.need;
       // The bin's tokens of this CTA; what it has before them.
       uint32_t kmin = 0xFFFFFFFFu, kmax = 0;
-      each([&](float v, int i) {
-        int bin;
-        const bool in = bin_of(v, dist(v), &bin) && bin == cut_bin && (!by_mass || keeps(v, i));
+      const int cut_bits = __float_as_int(kBinBase) + cut_bin;
+      auto collect = [&](float v, int i, bool in) {
+        in = in && (!by_mass || keeps(v, i));
         const uint32_t with = __ballot_sync(0xFFFFFFFFu, in);
         if (with == 0) return;
         uint32_t at = 0;
@@ -372,7 +397,19 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
           kmax = max(kmax, k);
           if (at < kOwn) s.own[at] = static_cast<u64>(k) << 32 | static_cast<uint32_t>(~i);
         }
-      });
+      };
+#pragma unroll 2
+      for (int st = 0; st < steps; ++st) {
+        const float4 v = mine4[st * 32 + lane];
+        const bool b0 = bin_of(v.x) == cut_bits, b1 = bin_of(v.y) == cut_bits, b2 = bin_of(v.z) == cut_bits,
+                   b3 = bin_of(v.w) == cut_bits;
+        if (!__any_sync(0xFFFFFFFFu, b0 || b1 || b2 || b3)) continue;
+        const int i = i0 + st * 128;
+        collect(v.x, i, b0);
+        collect(v.y, i + 1, b1);
+        collect(v.z, i + 2, b2);
+        collect(v.w, i + 3, b3);
+      }
       if (kmin <= kmax) {
         atomicMin(&s.kmin, kmin);
         atomicMax(&s.kmax, kmax);
@@ -490,6 +527,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
   // past d_max exp(-d) < min_p for certain (weights are 0 past 22.2)
   const float d_max = fminf(min_p > 0.0f ? 1e-5f - 1.000001f * logf(min_p) : 23.0f, 23.0f);
   auto kept = [&](float v, int i) -> uint32_t {  // the kept weight
+    if (v < cut_x) return 0u;
     const float d = dist(v);
     if (!(d <= d_max) || !keeps(v, i)) return 0u;
     const float e = expf(-d);
@@ -498,7 +536,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
   u64 mine = 0;  // of the warp
   auto add_warps = [&]() {
     u64 sum = 0;
-    each([&](float v, int i) { sum += kept(v, i); });
+    if (cut_x == -INFINITY && min_p == 0.0f) each([&](float v, int) { sum += weight(dist(v)); });
+    else each([&](float v, int i) { sum += kept(v, i); });
     mine = warp_add(sum);
     __syncthreads();  // (the sums of a scan before have been read)
     if (lane == 0) s.warp_sum[warp] = mine;
