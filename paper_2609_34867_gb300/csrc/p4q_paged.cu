@@ -5,8 +5,8 @@
 // query heads that share it (a group of more heads makes several units), cut
 // into tiles of positions. All units' tiles in one row, unit after unit, are
 // dealt to the CTAs in equal consecutive ranges, so a CTA's work does not
-// depend on how unequal the sequences are; a unit that several CTAs share is
-// joined by the one that finishes last.
+// depend on how unequal the sequences are (few tiles: one piece of a unit per
+// CTA). The units that several CTAs share are joined by a second kernel.
 //
 // A warp takes 16 positions at a time, straight from global memory into the
 // operands of m16n8k16 tensor-core products, without shared memory: the
@@ -23,7 +23,16 @@
 // p goes into the product as the sum of two 16-bit values (rounded, remainder):
 // rounded once it would add as much error as the output's own rounding does.
 // The new keys' loads are issued as soon as the old ones are in the first
-// product, and the values' behind the second.
+// product, and the values' behind the second: 8 KB in flight per warp, twelve
+// warps per SM. (Sixteen at 128 registers spilled: 757 us for 64 sequences of
+// 16384 x 8 heads, 631 this way. Copies into shared memory two tiles ahead left
+// room for eight warps, which their products' and exchanges' latencies bound: 907.)
+//
+// Bound: HBM. 64 x 16384 positions, 32 heads over 8 of 128, bf16 (4.3 GB): 631 us =
+// 6.8 TB/s, the measured copy; 24 sequences of up to 2048 x 40 heads 85 us = 0.91 of
+// it, 128 of up to 8190 (skewed) x 8 172 = 0.94; one of 32011 x 8 28 = 0.69, of 704 x
+// 40 10. What the short ones cost is a chain: lengths, page numbers, keys 4.6 us,
+// the end of a kernel and the second kernel 5.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -41,7 +50,7 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kMaxGrid = 640;    // CTAs of a launch at most (partial results of the workspace)
-constexpr int kMinTiles = 3;     // tiles per CTA at least, of one unit
+constexpr int kMinTiles = 2;     // tiles per CTA at least, of one unit
 constexpr int kUnitCost = 2;     // what a unit costs beside its tiles, in tiles
 constexpr float kShift = 7.0f;   // p = 2^(score - reference + 7): small p keep their bits in fp16
 constexpr float kMove = 8.0f;    // a reference moves when a score exceeds it by 2^8
@@ -130,7 +139,7 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 3 : 2) paged_attention_ke
   constexpr int kVc = kDh / 64;            // of a value row
   extern __shared__ __align__(16) float so[];  // [kWarps][kHeads][kDh]
   __shared__ float sm[kWarps][kHeads], sl[kWarps][kHeads];
-  __shared__ uint4 sq[kWarps][kNt][kKc][32];  // the query operand, lane by lane (in registers it made the loop spill)
+  __shared__ uint4 sq[kWarps][kNt][kKc][32];  // the query operand, lane by lane (the registers are for the loads)
   __shared__ unsigned long long scan[2][kWarps];
   __shared__ Plan plan;
 
@@ -259,19 +268,6 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 3 : 2) paged_attention_ke
       return page * c.page_stride + (j & slots) * c.token_stride;
     };
 
-    // Q: head g of each 8, dimensions 32 i + 8 t .. (each warp has its own copy)
-    __syncwarp();
-#pragma unroll
-    for (int n = 0; n < kNt; ++n)
-#pragma unroll
-      for (int i = 0; i < kKc; ++i) {
-        const int h = 8 * n + g;
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (h < heads) v = *reinterpret_cast<const uint4*>(a.q + b * a.ldq + static_cast<long long>(h0 + h) * kDh + 32 * i + 8 * t);
-        sq[warp][n][i][lane] = v;
-      }
-    __syncwarp();
-
     float o[kNt][kVc][4][4];  // O^T: [.][hh][j]: dimensions 64 hh + 8 g + 2 j (+ 1), heads 2 t, 2 t + 1
     float ref[kNt][2], l[kNt][2];
 #pragma unroll
@@ -366,9 +362,25 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 3 : 2) paged_attention_ke
     };
 
     look(tile);
+    // Q: head g of each 8, dimensions 32 i + 8 t .. (on its way beside the page numbers)
+    uint4 q[kNt][kKc];
+#pragma unroll
+    for (int n = 0; n < kNt; ++n)
+#pragma unroll
+      for (int i = 0; i < kKc; ++i) {
+        const int h = 8 * n + g;
+        q[n][i] = make_uint4(0u, 0u, 0u, 0u);
+        if (h < heads) q[n][i] = *reinterpret_cast<const uint4*>(a.q + b * a.ldq + static_cast<long long>(h0 + h) * kDh + 32 * i + 8 * t);
+      }
     load_k(tile);
     load_v(tile);
     look(tile + 1);
+    __syncwarp();
+#pragma unroll
+    for (int n = 0; n < kNt; ++n)
+#pragma unroll
+      for (int i = 0; i < kKc; ++i) sq[warp][n][i][lane] = q[n][i];
+    __syncwarp();
     for (int tl = tile; tl < tile_end; ++tl) {
       const bool more = tl + 1 < tile_end;
       float s[kRep][kNt][4];
@@ -380,9 +392,9 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 3 : 2) paged_attention_ke
           for (int e = 0; e < 4; ++e) s[r][n][e] = 0.0f;
 #pragma unroll
           for (int i = 0; i < kKc; ++i) {
-            const uint4 q = reload16(&sq[warp][n][i][lane]);
-            mma16816<kBf16>(s[r][n], kr[r][i][0].x, kr[r][i][1].x, kr[r][i][0].y, kr[r][i][1].y, q.x, q.y);
-            mma16816<kBf16>(s[r][n], kr[r][i][0].z, kr[r][i][1].z, kr[r][i][0].w, kr[r][i][1].w, q.z, q.w);
+            const uint4 f = reload16(&sq[warp][n][i][lane]);
+            mma16816<kBf16>(s[r][n], kr[r][i][0].x, kr[r][i][1].x, kr[r][i][0].y, kr[r][i][1].y, f.x, f.y);
+            mma16816<kBf16>(s[r][n], kr[r][i][0].z, kr[r][i][1].z, kr[r][i][0].w, kr[r][i][1].w, f.z, f.w);
           }
         }
       const uint32_t counts = live;
@@ -555,16 +567,16 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 3 : 2) paged_attention_ke
   }
 }
 
-// Joins the units that several CTAs share: CTA x the one that begins in CTA x of
-// the kernel before, from the parts of that one and the following; CTA (x, y)
-// its heads 4 y .. 4 y + 3. The parts of a head are divided among several warps,
-// which take kBatch at a time with their loads in flight together (one after the
-// other, 76 parts of 4 heads took 15 us).
-constexpr int kJoinWarps = 16, kJoinHeads = 4;
+// Joins the units that several CTAs share: CTA (x, y) head y of the unit that
+// begins in CTA x of the kernel before, from that one's part and those of the
+// following. Each warp takes every fourth part, kBatch at a time with their loads
+// in flight together (76 parts of 4 heads one after the other took 15 us; a CTA of
+// 16 warps for 4 heads 1.5 us more than this for 57).
+constexpr int kJoinWarps = 4;
 
 template <bool kBf16, int kDh, int kNt>
 __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const PagedAttnArgs a) {
-  constexpr int kHeads = 8 * kNt, kBatch = 8, kJd = kDh / 32;  // parts; dimensions per lane
+  constexpr int kHeads = 8 * kNt, kBatch = 16, kJd = kDh / 32;  // parts; dimensions per lane
   __shared__ __align__(16) float so[kJoinWarps][kDh];
   __shared__ float sm[kJoinWarps], sl[kJoinWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -574,83 +586,79 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const PagedAttnAr
   const int4* split = static_cast<const int4*>(a.ws);
   const float* partial = reinterpret_cast<const float*>(split + kMaxGrid);
   const int4 unit = split[blockIdx.x];
-  const int c0 = static_cast<int>(blockIdx.x), c1 = unit.z;
+  const int c0 = static_cast<int>(blockIdx.x), c1 = unit.z, h = static_cast<int>(blockIdx.y);
   if (c1 < 0) return;
   const int hk = unit.y / parts, h0 = hk * group + (unit.y % parts) * kHeads;
-  const int first = static_cast<int>(blockIdx.y) * kJoinHeads;
-  const int heads = min(kJoinHeads, min(kHeads, hk * group + group - h0) - first);  // of this CTA
-  if (heads <= 0) return;
-  const int ways = kJoinWarps / heads, k = warp / ways, way = warp % ways, h = first + k;
-  if (k < heads) {
-    float jm = -INFINITY, jl = 0.0f, jo[kJd];
+  if (h >= hk * group + group - h0) return;
+  float jm = -INFINITY, jl = 0.0f, jo[kJd];
 #pragma unroll
-    for (int e = 0; e < kJd; ++e) jo[e] = 0.0f;
-    for (int k0 = c0 + way; k0 <= c1; k0 += kBatch * ways) {
-      float mk[kBatch], lk[kBatch], z[kBatch][kJd];
+  for (int e = 0; e < kJd; ++e) jo[e] = 0.0f;
+  for (int k0 = c0 + warp; k0 <= c1; k0 += kBatch * kJoinWarps) {
+    float mk[kBatch], lk[kBatch], z[kBatch][kJd];
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
-        const int cta = k0 + i * ways;
-        const float* p = partial + static_cast<size_t>(2 * cta + (cta == c0)) * kPartFloats;
-        mk[i] = -INFINITY;
-        lk[i] = 0.0f;
+    for (int i = 0; i < kBatch; ++i) {
+      const int cta = k0 + i * kJoinWarps;
+      const float* p = partial + static_cast<size_t>(2 * cta + (cta == c0)) * kPartFloats;
+      mk[i] = -INFINITY;
+      lk[i] = 0.0f;
 #pragma unroll
-        for (int e = 0; e < kJd; ++e) z[i][e] = 0.0f;
-        if (cta <= c1) {
-          mk[i] = p[h];
-          lk[i] = p[16 + h];
-          if (kJd == 4) {
-            const float4 v = *(reinterpret_cast<const float4*>(p + 32 + h * kDh) + lane);
-            z[i][0] = v.x;
-            z[i][1] = v.y;
-            z[i][2 % kJd] = v.z;
-            z[i][3 % kJd] = v.w;
-          } else {
-            const float2 v = *(reinterpret_cast<const float2*>(p + 32 + h * kDh) + lane);
-            z[i][0] = v.x;
-            z[i][1] = v.y;
-          }
+      for (int e = 0; e < kJd; ++e) z[i][e] = 0.0f;
+      if (cta <= c1) {
+        mk[i] = p[h];
+        lk[i] = p[16 + h];
+        if (kJd == 4) {
+          const float4 v = *(reinterpret_cast<const float4*>(p + 32 + h * kDh) + lane);
+          z[i][0] = v.x;
+          z[i][1] = v.y;
+          z[i][2 % kJd] = v.z;
+          z[i][3 % kJd] = v.w;
+        } else {
+          const float2 v = *(reinterpret_cast<const float2*>(p + 32 + h * kDh) + lane);
+          z[i][0] = v.x;
+          z[i][1] = v.y;
         }
       }
-      float m = jm;
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) m = fmaxf(m, mk[i]);
-      const float of = jm == -INFINITY ? 0.0f : exp2_fast(jm - m);
-      jm = m;
-      jl *= of;
-#pragma unroll
-      for (int e = 0; e < kJd; ++e) jo[e] *= of;
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
-        const float f = mk[i] == -INFINITY ? 0.0f : exp2_fast(mk[i] - m);
-        jl += lk[i] * f;
-#pragma unroll
-        for (int e = 0; e < kJd; ++e) jo[e] += z[i][e] * f;
-      }
     }
-    if (lane == 0) {
-      sm[warp] = jm;
-      sl[warp] = jl;
-    }
+    float m = jm;
 #pragma unroll
-    for (int e = 0; e < kJd; ++e) so[warp][lane * kJd + e] = jo[e];
+    for (int i = 0; i < kBatch; ++i) m = fmaxf(m, mk[i]);
+    const float of = jm == -INFINITY ? 0.0f : exp2_fast(jm - m);
+    jm = m;
+    jl *= of;
+#pragma unroll
+    for (int e = 0; e < kJd; ++e) jo[e] *= of;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const float f = mk[i] == -INFINITY ? 0.0f : exp2_fast(mk[i] - m);
+      jl += lk[i] * f;
+#pragma unroll
+      for (int e = 0; e < kJd; ++e) jo[e] += z[i][e] * f;
+    }
   }
+  if (lane == 0) {
+    sm[warp] = jm;
+    sl[warp] = jl;
+  }
+#pragma unroll
+  for (int e = 0; e < kJd; ++e) so[warp][lane * kJd + e] = jo[e];
   __syncthreads();
-  for (int i = threadIdx.x; i < heads * (kDh / 4); i += 32 * kJoinWarps) {
-    const int n = i / (kDh / 4), d = (i % (kDh / 4)) * 4, w0 = n * ways;
-    float m = -INFINITY, sum = 0.0f;
-    for (int w = w0; w < w0 + ways; ++w) m = fmaxf(m, sm[w]);
-    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int w = w0; w < w0 + ways; ++w) {
-      const float f = sm[w] == -INFINITY ? 0.0f : exp2_fast(sm[w] - m);
-      const float4 z = *reinterpret_cast<const float4*>(&so[w][d]);
-      sum += sl[w] * f;
-      v.x += z.x * f;
-      v.y += z.y * f;
-      v.z += z.z * f;
-      v.w += z.w * f;
-    }
-    write_out<kBf16>(a, unit.x, h0 + first + n, d, m, sum, v);
+  const int d = static_cast<int>(threadIdx.x) * 4;
+  if (d >= kDh) return;
+  float m = sm[0], sum = 0.0f;
+#pragma unroll
+  for (int w = 1; w < kJoinWarps; ++w) m = fmaxf(m, sm[w]);
+  float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+  for (int w = 0; w < kJoinWarps; ++w) {
+    const float f = sm[w] == -INFINITY ? 0.0f : exp2_fast(sm[w] - m);
+    const float4 z = *reinterpret_cast<const float4*>(&so[w][d]);
+    sum += sl[w] * f;
+    v.x += z.x * f;
+    v.y += z.y * f;
+    v.z += z.z * f;
+    v.w += z.w * f;
   }
+  write_out<kBf16>(a, unit.x, h0 + h, d, m, sum, v);
 }
 
 template <bool kBf16, int kDh, int kNt, bool kSmallPage>
@@ -672,8 +680,8 @@ cudaError_t launch(const PagedAttnArgs& a, cudaStream_t stream, unsigned int* la
   ++*launches;
   // no unit can have more than one piece: nothing to join
   if (room <= kMinTiles && units <= grid) return cudaSuccess;
-  const unsigned slices = (std::min(group, 8 * kNt) + kJoinHeads - 1) / kJoinHeads;
-  e = launch_pdl(join_kernel<kBf16, kDh, kNt>, dim3(static_cast<unsigned>(grid), slices), dim3(32 * kJoinWarps), 0, stream,
+  const unsigned heads = static_cast<unsigned>(std::min(group, 8 * kNt));
+  e = launch_pdl(join_kernel<kBf16, kDh, kNt>, dim3(static_cast<unsigned>(grid), heads), dim3(32 * kJoinWarps), 0, stream,
                  a);
   if (e == cudaSuccess) ++*launches;
   return e;

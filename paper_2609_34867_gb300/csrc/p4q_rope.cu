@@ -91,12 +91,12 @@ __global__ void __launch_bounds__(kThreads, 6) rope_append_kernel(const RopeArgs
       y = make_uint4(yr[0], yr[1], yr[2], yr[3]);
     }
     uint16_t* d = is_q ? a.q_out + t * a.ldqo + hk * c.dh : (is_v ? c.v : c.k) + slot + hk * c.head_stride;
-    *reinterpret_cast<uint4*>(d + lo) = x;
-    *reinterpret_cast<uint4*>(d + hi) = y;
+    __stcs(reinterpret_cast<uint4*>(d + lo), x);
+    __stcs(reinterpret_cast<uint4*>(d + hi), y);
     if (!is_q && !is_v && a.k_out) {
       d = a.k_out + t * a.ldko + hk * c.dh;
-      *reinterpret_cast<uint4*>(d + lo) = x;
-      *reinterpret_cast<uint4*>(d + hi) = y;
+      __stcs(reinterpret_cast<uint4*>(d + lo), x);
+      __stcs(reinterpret_cast<uint4*>(d + hi), y);
     }
   }
 }
