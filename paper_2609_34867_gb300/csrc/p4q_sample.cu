@@ -19,6 +19,10 @@
 // of more tokens than the lists hold are
 // divided again by the logits' ordered bit patterns, at most three times (11 of 32
 // bits each); a bin of equal logits is cut by index.
+// Mostly few tokens can be kept at all: up to the bin of a top-k or top-p cut, or
+// those that pass a min-p. Up to 512 of them go to the cluster's first CTA, which
+// sorts them and makes the cuts and the draw on that list alone. What follows is
+// for the rest:
 // The draw: kept weights per CTA (behind a top-p cut they are known from the
 // histogram) and their prefix over the cluster; then the one CTA that contains the
 // drawn number finds the warp (a warp's tokens are consecutive), and that
@@ -46,20 +50,28 @@ constexpr int kList = 512;          // tokens of a bin that are ranked, at most
 constexpr int kOwn = 256;           // of one CTA
 
 constexpr int kGroups = kBins / 32;
+constexpr int kCand = 768;          // places for candidates, each CTA a part of them
+constexpr float kNear = 8.0f;       // a min-p of at least e^-8 mostly leaves few tokens
 
 struct Shared {
   uint32_t lo[kBins], hi[kBins];  // counts, or the weights' low and high 16 bits
-  u64 own[kOwn];                  // the CTA's tokens of the bin: key, complement of the index
-  u64 list[kList];                // the cluster's
-  uint32_t weight[kList];
+  u64 own[kOwn];      // the CTA's tokens of a bin: key, complement of the index
+  union {
+    u64 cand[kCand];  // (of the cluster's first CTA) candidates, each CTA's from its part's start
+    struct {
+      u64 list[kList];  // the cluster's tokens of the bin
+      uint32_t weight[kList];
+    };
+  };
   u64 warp_sum[kWarps];
   // values of each CTA of the cluster, written by it
   u64 group[kMaxCluster][kGroups];  // its sums over 32 bins
   u64 mass[kMaxCluster];
-  uint32_t max_key[kMaxCluster], first_max[kMaxCluster], own_n[kMaxCluster], key_min[kMaxCluster], key_max[kMaxCluster];
+  uint32_t max_key[kMaxCluster], first_max[kMaxCluster], cand_n[kMaxCluster], own_n[kMaxCluster], key_min[kMaxCluster],
+      key_max[kMaxCluster];
   u64 need, total, draw;
   u64 cut;                        // the last kept token
-  uint32_t bin, n, kmin, kmax;    // of the CTA's list: its length, smallest and largest key
+  uint32_t bin, sent, n, kmin, kmax;  // candidates sent; of the CTA's list: its length, smallest and largest key
   uint32_t red[kWarps];
 };
 
@@ -278,9 +290,140 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
   u64 cta_mass = 0;  // the kept weights of the CTA, where known
   bool known = false;
 
+  // Sends the tokens of a step's four logits with `in` to the first CTA's candidates
+  // (the CTA's own part of them, as far as it goes; s.sent counts all).
+  const int room = kCand / cs;
+  auto send = [&](const float (&v)[4], int i, const bool (&in)[4]) {
+    if (!__any_sync(0xFFFFFFFFu, in[0] || in[1] || in[2] || in[3])) return;
+    if (*reinterpret_cast<volatile uint32_t*>(&s.sent) > static_cast<uint32_t>(room)) return;  // too many already
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t with = __ballot_sync(0xFFFFFFFFu, in[j]);
+      if (with == 0) continue;
+      uint32_t at = 0;
+      if (lane == 0) at = atomicAdd(&s.sent, static_cast<uint32_t>(__popc(with)));
+      at = __shfl_sync(0xFFFFFFFFu, at, 0) + static_cast<uint32_t>(__popc(with & ((1u << lane) - 1u)));
+      if (in[j] && at < static_cast<uint32_t>(room))
+        st_shared_cluster_u64(mapa_shared(smem_u32(&s.cand[rank * room + at]), 0),
+                              static_cast<u64>(key_of(v[j])) << 32 | static_cast<uint32_t>(~(i + j)));
+    }
+  };
+  // How many candidates there are, or 0 if they do not all have a place (the counts are there).
+  auto candidates = [&]() -> uint32_t {
+    uint32_t all = 0, most = 0;
+    for (int r = 0; r < cs; ++r) {
+      all += s.cand_n[r];
+      most = max(most, s.cand_n[r]);
+    }
+    return all <= kList && most <= static_cast<uint32_t>(room) ? all : 0u;
+  };
+  const int top_k = a.top_k ? a.top_k[n] : 0;
+  const float top_p = a.top_p ? a.top_p[n] : 1.0f;
+  const float min_p = a.min_p && a.min_p[n] > 0.0f ? fminf(a.min_p[n], 1.0f) : 0.0f;
+  // past d_max exp(-d) < min_p for certain (weights are 0 past 22.2)
+  const float d_max = fminf(min_p > 0.0f ? 1e-5f - 1.000001f * logf(min_p) : 23.0f, 23.0f);
+  const bool by_k = top_k > 0 && top_k < V, by_p = top_p < 1.0f;
+  auto sum_cta = [&](u64 v) -> u64 {  // over the CTA's threads
+    v = warp_add(v);
+    __syncthreads();
+    if (lane == 0) s.warp_sum[warp] = v;
+    __syncthreads();
+    u64 all = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) all += s.warp_sum[w];
+    return all;
+  };
+  // Sorts a value of each of the first `size` threads (a power of two, 32 .. kList), falling, all threads calling.
+  auto sort = [&](u64 v, uint32_t size) -> u64 {
+    for (uint32_t k = 2; k <= size; k <<= 1)
+      for (uint32_t j = k >> 1; j > 0; j >>= 1) {
+        u64 other;
+        if (j >= 32) {
+          s.list[tid] = v;
+          __syncthreads();
+          other = s.list[tid ^ j];
+          __syncthreads();
+        } else {
+          other = __shfl_xor_sync(0xFFFFFFFFu, v, j);
+        }
+        const bool larger = ((tid & k) == 0) == ((tid & j) == 0);
+        v = larger == (other > v) ? other : v;
+      }
+    return v;
+  };
+  // Inclusive scan over the CTA's threads; *all: the sum.
+  auto scan_cta = [&](u64 v, u64* all) -> u64 {
+    u64 to = warp_scan(v);
+    __syncthreads();
+    if (lane == 31) s.warp_sum[warp] = to;
+    __syncthreads();
+    u64 sum = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      if (w < warp) to += s.warp_sum[w];
+      sum += s.warp_sum[w];
+    }
+    *all = sum;
+    return to;
+  };
+  static_assert(kList == kThreads, "a candidate per thread");
+  // The cuts and the draw on the `found` candidates, by the first CTA. with_k: they are the first top_k
+  // tokens and some after these; else `all` is the sum of the weights that a top-p is a share of.
+  auto finish = [&](uint32_t found, bool with_k, u64 all) {
+    uint32_t size = 32;
+    while (size < found) size <<= 1;
+    u64 t = 0;  // (no token: below every token)
+    if (tid < static_cast<int>(found)) {
+      int r = 0;
+      uint32_t j = static_cast<uint32_t>(tid);
+      while (j >= s.cand_n[r]) j -= s.cand_n[r++];
+      t = s.cand[r * room + j];
+    }
+    __syncthreads();  // (the sort's exchanges lie in the same place)
+    if (by_p || with_k) t = sort(t, size);
+    const bool real = tid < static_cast<int>(found) && !(with_k && tid >= top_k);
+    float e = 0.0f;
+    if (real) e = expf(-dist(float_of_key(static_cast<uint32_t>(t >> 32))));
+    const uint32_t w = __float2uint_rn(e * 2147483648.0f);
+    u64 to = 0;
+    if (by_p) {
+      u64 sum;
+      to = scan_cta(w, &sum);
+      if (tid == 0) {  // (64-bit floating point is slow: once)
+        const double part = ceil(static_cast<double>(top_p) * static_cast<double>(with_k ? sum : all));
+        s.need = part < 1.0 ? 1ull : static_cast<u64>(part);
+      }
+      __syncthreads();
+    }
+    const bool is_kept = real && w > 0 && !(e < min_p) && (!by_p || to - w < s.need);
+    // again by index: its complement, and the weight
+    u64 by_index = is_kept ? static_cast<u64>(static_cast<uint32_t>(t)) << 32 | w : 0ull;
+    by_index = sort(by_index, size);
+    const uint32_t kept_w = tid < static_cast<int>(size) ? static_cast<uint32_t>(by_index) : 0u;
+    u64 total;
+    const u64 upto = scan_cta(kept_w, &total);
+    if (tid == 0) {
+      const double want = floor(static_cast<double>(a.u[n]) * static_cast<double>(total));
+      const u64 r = want > 0.0 ? static_cast<u64>(fmin(want, 9.0e15)) : 0ull;
+      s.draw = min(r, total - 1);
+    }
+    __syncthreads();
+    const u64 r = s.draw;
+    if (upto - kept_w <= r && r < upto) {
+      const int i = static_cast<int>(~static_cast<uint32_t>(by_index >> 32));
+      a.token[n] = i;
+      if (a.logprob) {
+        const void* p = row + static_cast<size_t>(i + skip) * kSize;
+        const float v = kType == 2 ? *static_cast<const float*>(p) : from16<kType == 1>(*static_cast<const uint16_t*>(p));
+        a.logprob[n] = -dist(v) - logf(static_cast<float>(static_cast<double>(total) * 4.656612873077393e-10));
+      }
+    }
+  };
+
   // Shortens the kept head: to `need` tokens, or (by_mass) to the first tokens
-  // whose weights reach ceil(share * the kept weights' sum).
-  auto shorten = [&](auto mass_c, u64 need, float share) {
+  // whose weights reach ceil(share * the kept weights' sum). True: the kept tokens are few, and the
+  // first CTA has drawn one of them.
+  auto shorten = [&](auto mass_c, u64 need, float share) -> bool {
     constexpr bool by_mass = decltype(mass_c)::value;
     uint32_t key_lo = 0, key_hi = 0;
     int shift = 0;
@@ -291,6 +434,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
         if (by_mass) s.hi[i] = 0;
       }
       if (tid == 0) {
+        s.sent = 0;
         s.n = 0;
         s.kmin = 0xFFFFFFFFu;
         s.kmax = 0;
@@ -378,37 +522,41 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
         if (lane == 0) s.total = total;
       }
       __syncthreads();
-      if (!by_mass && level == 0 && s.total <= need) return;  // every token that may be drawn is among the first `need`
+      if (!by_mass && level == 0 && s.total <= need) return false;  // every token that may be drawn is among the first `need`
       const int cut_bin = static_cast<int>(s.bin);
+      const bool few = level == 0 && (by_mass || need <= kList);  // the tokens up to the bin may be few
       need = s.need;
-      // The bin's tokens of this CTA; what it has before them.
+      // The bin's tokens of this CTA; those up to it to the first CTA.
       uint32_t kmin = 0xFFFFFFFFu, kmax = 0;
       const int cut_bits = __float_as_int(kBinBase) + cut_bin;
-      auto collect = [&](float v, int i, bool in) {
-        in = in && (!by_mass || keeps(v, i));
-        const uint32_t with = __ballot_sync(0xFFFFFFFFu, in);
-        if (with == 0) return;
-        uint32_t at = 0;
-        if (lane == 0) at = atomicAdd(&s.n, static_cast<uint32_t>(__popc(with)));
-        at = __shfl_sync(0xFFFFFFFFu, at, 0) + static_cast<uint32_t>(__popc(with & ((1u << lane) - 1u)));
-        if (in) {
-          const uint32_t k = key_of(v);
-          kmin = min(kmin, k);
-          kmax = max(kmax, k);
-          if (at < kOwn) s.own[at] = static_cast<u64>(k) << 32 | static_cast<uint32_t>(~i);
-        }
-      };
 #pragma unroll 2
       for (int st = 0; st < steps; ++st) {
-        const float4 v = mine4[st * 32 + lane];
-        const bool b0 = bin_of(v.x) == cut_bits, b1 = bin_of(v.y) == cut_bits, b2 = bin_of(v.z) == cut_bits,
-                   b3 = bin_of(v.w) == cut_bits;
-        if (!__any_sync(0xFFFFFFFFu, b0 || b1 || b2 || b3)) continue;
-        const int i = i0 + st * 128;
-        collect(v.x, i, b0);
-        collect(v.y, i + 1, b1);
-        collect(v.z, i + 2, b2);
-        collect(v.w, i + 3, b3);
+        const float4 v4 = mine4[st * 32 + lane];
+        const float v[4] = {v4.x, v4.y, v4.z, v4.w};
+        bool in[4], at_cut[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int bits = bin_of(v[j]);
+          const bool may = !by_mass || keeps(v[j], i0 + st * 128 + j);
+          in[j] = may && bits <= cut_bits;
+          at_cut[j] = may && bits == cut_bits;
+        }
+        if (few) send(v, i0 + st * 128, in);
+        if (!__any_sync(0xFFFFFFFFu, at_cut[0] || at_cut[1] || at_cut[2] || at_cut[3])) continue;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t with = __ballot_sync(0xFFFFFFFFu, at_cut[j]);
+          if (with == 0) continue;
+          uint32_t at = 0;
+          if (lane == 0) at = atomicAdd(&s.n, static_cast<uint32_t>(__popc(with)));
+          at = __shfl_sync(0xFFFFFFFFu, at, 0) + static_cast<uint32_t>(__popc(with & ((1u << lane) - 1u)));
+          if (at_cut[j]) {
+            const uint32_t key = key_of(v[j]);
+            kmin = min(kmin, key);
+            kmax = max(kmax, key);
+            if (at < kOwn) s.own[at] = static_cast<u64>(key) << 32 | static_cast<uint32_t>(~(i0 + st * 128 + j));
+          }
+        }
       }
       if (kmin <= kmax) {
         atomicMin(&s.kmin, kmin);
@@ -426,11 +574,16 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
         for (int w = 0; w < kWarps; ++w) below += s.warp_sum[w];
       }
       if (warp == 0) {
+        put32_lanes(&s.cand_n[rank], s.sent);
         put32_lanes(&s.own_n[rank], s.n);
         put32_lanes(&s.key_min[rank], s.kmin);
         put32_lanes(&s.key_max[rank], s.kmax);
       }
       sync_all();
+      if (const uint32_t c = few ? candidates() : 0u) {
+        if (rank == 0) finish(c, !by_mass, s.total);
+        return true;
+      }
       uint32_t found = 0, most = 0;
       key_lo = 0xFFFFFFFFu;
       key_hi = 0;
@@ -474,7 +627,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
           cta_mass = below + warp_add(sum);
           known = true;
         }
-        return;
+        return false;
       }
       if (key_lo == key_hi) {  // equal logits: so many of them, by index
         const float v = float_of_key(key_lo);
@@ -511,21 +664,51 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
         sync_all();
         cut_x = v;
         cut_i = static_cast<int>(s.cut);
-        return;
+        return false;
       }
       const int bits = 32 - __clz(key_hi - key_lo);
       shift = max(0, bits - 11);
     }
   };
 
-  const int top_k = a.top_k ? a.top_k[n] : 0;
-  if (top_k > 0 && top_k < V) shorten(std::false_type{}, static_cast<u64>(top_k), 0.0f);
-  const float top_p = a.top_p ? a.top_p[n] : 1.0f;
-  if (top_p < 1.0f) shorten(std::true_type{}, 0, top_p);
+  if (by_k && shorten(std::false_type{}, static_cast<u64>(top_k), 0.0f)) return;
+  // (a top-k that cuts has set cut_x; beside one that does not, the other cuts are as without)
+  if (cut_x == -INFINITY && min_p > 0.0f && d_max <= kNear) {
+    __syncthreads();
+    if (tid == 0) s.sent = 0;
+    __syncthreads();
+    u64 all = 0;
+#pragma unroll 2
+    for (int st = 0; st < steps; ++st) {
+      const float4 v4 = mine4[st * 32 + lane];
+      const float v[4] = {v4.x, v4.y, v4.z, v4.w};
+      bool in[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float d = dist(v[j]);
+        in[j] = d <= d_max;
+        if (by_p) all += weight(d);
+      }
+      send(v, i0 + st * 128, in);
+    }
+    if (by_p) all = sum_cta(all);
+    else __syncthreads();
+    if (warp == 0) {
+      put32_lanes(&s.cand_n[rank], s.sent);
+      put64_lanes(&s.mass[rank], all);
+    }
+    sync_all();
+    const uint32_t found = candidates();
+    if (found > 0) {
+      all = 0;
+      for (int r = 0; r < cs; ++r) all += s.mass[r];
+      if (rank == 0) finish(found, false, all);
+      return;
+    }
+    sync_all();  // (the exchanged values have been read)
+  }
+  if (by_p && shorten(std::true_type{}, 0, top_p)) return;
 
-  const float min_p = a.min_p && a.min_p[n] > 0.0f ? fminf(a.min_p[n], 1.0f) : 0.0f;
-  // past d_max exp(-d) < min_p for certain (weights are 0 past 22.2)
-  const float d_max = fminf(min_p > 0.0f ? 1e-5f - 1.000001f * logf(min_p) : 23.0f, 23.0f);
   auto kept = [&](float v, int i) -> uint32_t {  // the kept weight
     if (v < cut_x) return 0u;
     const float d = dist(v);

@@ -124,6 +124,25 @@ def test_every_mode(p4q, dev, dt, V, ld):
             check_row(xs[n], float(u[n]), int(token[n]), float(lp[n]), **one)
 
 
+@pytest.mark.parametrize("spread", [0.3, 1.0, 6.0])
+@pytest.mark.parametrize("V", [700, 20001, 131071, 262143])
+def test_flat_and_peaked_rows(p4q, dev, V, spread):
+    """Many tokens within reach of a cut, and few; top-k and the filters of each size."""
+    rows = 12
+    x = logits(dev, rows, V, torch.float32, seed=V + int(10 * spread), spread=spread)
+    xs = x.cpu().numpy()
+    rng = np.random.default_rng(V)
+    u = rng.random(rows).astype(np.float32)
+    k = np.array([1, 2, 30, 400, 511, 512, 513, 690, 5, 60, 700, 100], np.int32)
+    p = np.array([0.05, 0.5, 0.9, 0.99, 0.999, 0.3, 0.8, 0.95, 0.7, 0.6, 0.9999, 0.2], np.float32)
+    m = np.array([0.5, 0.1, 1e-3, 1e-5, 0.9, 0.01, 3e-4, 0.2, 0.05, 1e-4, 0.3, 2e-3], np.float32)
+    for params in ({"top_k": k}, {"top_p": p}, {"min_p": m}, {"top_k": k, "top_p": p}, {"top_p": p, "min_p": m},
+                   {"top_k": k, "min_p": m}, {"top_k": k, "top_p": p, "min_p": m}):
+        token, lp = draw(p4q, dev, x, u, **params)
+        for n in range(rows):
+            check_row(xs[n], float(u[n]), int(token[n]), float(lp[n]), **{key: val[n] for key, val in params.items()})
+
+
 def test_parameters_at_and_past_their_ends(p4q, dev):
     V = 3001
     nan, inf = float("nan"), float("inf")
