@@ -369,39 +369,83 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
   static_assert(kList == kThreads, "a candidate per thread");
   // The cuts and the draw on the `found` candidates, by the first CTA. with_k: they are the first top_k
   // tokens and some after these; else `all` is the sum of the weights that a top-p is a share of.
+  // Up to 128 are compared pairwise (kThreads / size lanes per token), more are sorted: twice, for the
+  // cuts by logit and for the draw by index (64: 2.0 k cycles instead of 6.1 k).
   auto finish = [&](uint32_t found, bool with_k, u64 all) {
     uint32_t size = 32;
     while (size < found) size <<= 1;
+    const bool pairs = size <= 128;
+    const int ways = pairs ? kThreads / static_cast<int>(size) : 1;  // 4 .. 16 neighbouring lanes
+    const uint32_t at = static_cast<uint32_t>(tid / ways), way = static_cast<uint32_t>(tid % ways);
     u64 t = 0;  // (no token: below every token)
-    if (tid < static_cast<int>(found)) {
+    if (at < found) {
       int r = 0;
-      uint32_t j = static_cast<uint32_t>(tid);
+      uint32_t j = at;
       while (j >= s.cand_n[r]) j -= s.cand_n[r++];
       t = s.cand[r * room + j];
     }
-    __syncthreads();  // (the sort's exchanges lie in the same place)
-    if (by_p || with_k) t = sort(t, size);
-    const bool real = tid < static_cast<int>(found) && !(with_k && tid >= top_k);
-    float e = 0.0f;
-    if (real) e = expf(-dist(float_of_key(static_cast<uint32_t>(t >> 32))));
+    __syncthreads();  // (the list lies in the same place)
+    if (!pairs && (by_p || with_k)) t = sort(t, size);
+    const bool real = at < found;
+    float e = 0.0f, d = 0.0f;
+    if (real) {
+      d = dist(float_of_key(static_cast<uint32_t>(t >> 32)));
+      e = expf(-d);
+    }
     const uint32_t w = __float2uint_rn(e * 2147483648.0f);
-    u64 to = 0;
+    uint32_t place = at;  // among the candidates
+    u64 before = 0;       // the weights before it
+    auto sum_ways = [&](u64 v) {
+      for (int x = 1; x < ways; x <<= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, x);
+      return v;
+    };
+    if (pairs) {
+      if (way == 0) {
+        s.list[at] = t;
+        s.weight[at] = w;
+      }
+      __syncthreads();
+      uint32_t c = 0;
+      for (uint32_t j = way; j < found; j += ways)
+        if (s.list[j] > t) {
+          ++c;
+          before += s.weight[j];
+        }
+      place = static_cast<uint32_t>(sum_ways(c));
+      before = sum_ways(before);
+    }
+    const bool in_k = real && !(with_k && place >= static_cast<uint32_t>(top_k));
     if (by_p) {
       u64 sum;
-      to = scan_cta(w, &sum);
+      const u64 to = scan_cta(in_k && way == 0 ? w : 0u, &sum);
+      if (!pairs) before = to - w;
       if (tid == 0) {  // (64-bit floating point is slow: once)
         const double part = ceil(static_cast<double>(top_p) * static_cast<double>(with_k ? sum : all));
         s.need = part < 1.0 ? 1ull : static_cast<u64>(part);
       }
       __syncthreads();
     }
-    const bool is_kept = real && w > 0 && !(e < min_p) && (!by_p || to - w < s.need);
-    // again by index: its complement, and the weight
-    u64 by_index = is_kept ? static_cast<u64>(static_cast<uint32_t>(t)) << 32 | w : 0ull;
-    by_index = sort(by_index, size);
-    const uint32_t kept_w = tid < static_cast<int>(size) ? static_cast<uint32_t>(by_index) : 0u;
-    u64 total;
-    const u64 upto = scan_cta(kept_w, &total);
+    const bool is_kept = in_k && w > 0 && !(e < min_p) && (!by_p || before < s.need);
+    // by index: its complement, and the weight
+    u64 mine = is_kept ? static_cast<u64>(static_cast<uint32_t>(t)) << 32 | w : 0ull;
+    u64 upto, total;  // the kept weights up to this token, all
+    if (pairs) {
+      __syncthreads();  // (the tokens in the list have been read)
+      if (way == 0) s.list[at] = mine;
+      __syncthreads();
+      upto = 0;
+      u64 sum = 0;
+      for (uint32_t j = way; j < found; j += ways) {
+        const u64 x = s.list[j];
+        sum += static_cast<uint32_t>(x);
+        if (x >= mine) upto += static_cast<uint32_t>(x);
+      }
+      upto = sum_ways(upto);
+      total = sum_ways(sum);
+    } else {
+      mine = sort(mine, size);
+      upto = scan_cta(static_cast<uint32_t>(mine), &total);
+    }
     if (tid == 0) {
       const double want = floor(static_cast<double>(a.u[n]) * static_cast<double>(total));
       const u64 r = want > 0.0 ? static_cast<u64>(fmin(want, 9.0e15)) : 0ull;
@@ -409,13 +453,15 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
     }
     __syncthreads();
     const u64 r = s.draw;
-    if (upto - kept_w <= r && r < upto) {
-      const int i = static_cast<int>(~static_cast<uint32_t>(by_index >> 32));
+    if (way == 0 && upto - static_cast<uint32_t>(mine) <= r && r < upto) {
+      const int i = static_cast<int>(~static_cast<uint32_t>(mine >> 32));
       a.token[n] = i;
       if (a.logprob) {
-        const void* p = row + static_cast<size_t>(i + skip) * kSize;
-        const float v = kType == 2 ? *static_cast<const float*>(p) : from16<kType == 1>(*static_cast<const uint16_t*>(p));
-        a.logprob[n] = -dist(v) - logf(static_cast<float>(static_cast<double>(total) * 4.656612873077393e-10));
+        if (!pairs) {  // (sorted by index: the lane's d is another token's)
+          const void* p = row + static_cast<size_t>(i + skip) * kSize;
+          d = dist(kType == 2 ? *static_cast<const float*>(p) : from16<kType == 1>(*static_cast<const uint16_t*>(p)));
+        }
+        a.logprob[n] = -d - logf(static_cast<float>(static_cast<double>(total) * 4.656612873077393e-10));
       }
     }
   };
@@ -479,9 +525,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
 #pragma unroll
       for (int j = 0; j < kGroups / kWarps; ++j) {
         const int g = warp * (kGroups / kWarps) + j;
-        u64 v = s.lo[g * 32 + lane];
-        if (by_mass) v += static_cast<u64>(s.hi[g * 32 + lane]) << 16;
-        v = warp_add(v);
+        // (32 bits hold them: a CTA has at most 36864 tokens of less than 2^16 each)
+        u64 v = __reduce_add_sync(0xFFFFFFFFu, s.lo[g * 32 + lane]);
+        if (by_mass) v += static_cast<u64>(__reduce_add_sync(0xFFFFFFFFu, s.hi[g * 32 + lane])) << 16;
         put64_lanes(&s.group[rank][g], v);
       }
       sync_all();
@@ -533,13 +579,13 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
       for (int st = 0; st < steps; ++st) {
         const float4 v4 = mine4[st * 32 + lane];
         const float v[4] = {v4.x, v4.y, v4.z, v4.w};
+        const int bits[4] = {bin_of(v[0]), bin_of(v[1]), bin_of(v[2]), bin_of(v[3])};
+        if (!__any_sync(0xFFFFFFFFu, min(min(bits[0], bits[1]), min(bits[2], bits[3])) <= cut_bits)) continue;
         bool in[4], at_cut[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const int bits = bin_of(v[j]);
-          const bool may = !by_mass || keeps(v[j], i0 + st * 128 + j);
-          in[j] = may && bits <= cut_bits;
-          at_cut[j] = may && bits == cut_bits;
+          in[j] = bits[j] <= cut_bits && (!by_mass || keeps(v[j], i0 + st * 128 + j));
+          at_cut[j] = in[j] && bits[j] == cut_bits;
         }
         if (few) send(v, i0 + st * 128, in);
         if (!__any_sync(0xFFFFFFFFu, at_cut[0] || at_cut[1] || at_cut[2] || at_cut[3])) continue;
