@@ -555,8 +555,8 @@ p4q_status p4q_rope_append(const uint16_t* q, int ldq, const uint16_t* k, int ld
  * with key/value head h / (H / Hkv), and lse[b, h] = ln sum_j exp(scale q . k_j).
  * A sequence with lens[b] <= 0 has o = 0 and lse = -inf. Positions from lens[b]
  * on are not read. fp32 products, softmax and sums; o rounded once.
- * A length beyond the page table's columns is cut to them, and the positions of
- * a page outside the cache count as masked (both P4Q_ERR_INDEX).
+ * A length beyond the page table's columns (or 2^30) is cut to them, and the
+ * positions of a page outside the cache count as masked (both P4Q_ERR_INDEX).
  *   q, o  [kv->seqs, ldq / ldo] kv->dtype, H heads of dh (o written)
  *   lens  [kv->seqs] int32
  *   lse   [kv->seqs, H] fp32, written, or NULL

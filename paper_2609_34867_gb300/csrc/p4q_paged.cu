@@ -52,6 +52,7 @@ constexpr int kThreads = 32 * kWarps;
 constexpr int kMaxGrid = 640;    // CTAs of a launch at most (partial results of the workspace)
 constexpr int kMinTiles = 2;     // tiles per CTA at least, of one unit
 constexpr int kUnitCost = 2;     // what a unit costs beside its tiles, in tiles
+constexpr long long kMaxLen = 1ll << 30;  // positions (places of a sequence are counted in 32 bits)
 constexpr float kShift = 7.0f;   // p = 2^(score - reference + 7): small p keep their bits in fp16
 constexpr float kMove = 8.0f;    // a reference moves when a score exceeds it by 2^8
 
@@ -146,7 +147,7 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 3 : 2) paged_attention_ke
   const PagedCache& c = a.kv;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const int group = a.H / c.Hkv, parts = (group + kHeads - 1) / kHeads, units = c.Hkv * parts;
-  const long long room = static_cast<long long>(c.table_cols) << c.page_log2;
+  const long long room = min(static_cast<long long>(c.table_cols) << c.page_log2, kMaxLen);
   const float c2 = a.scale * 1.4426950408889634f;
   int4* split = static_cast<int4*>(a.ws);
   float* partial = reinterpret_cast<float*>(split + kMaxGrid);

@@ -113,8 +113,8 @@ cudaError_t launch_rope_append(const RopeArgs& a, cudaStream_t stream) {
   int tx_log2 = 3;
   while (tx_log2 < 8 && ((kItems << tx_log2) < items || ((1 << tx_log2) < items && a.T <= (num_sms() * kThreads) >> tx_log2)))
     ++tx_log2;
-  const int tokens = kThreads >> tx_log2;
-  return launch_pdl(kernel, dim3(static_cast<unsigned>((a.T + tokens - 1) / tokens)), dim3(kThreads), 0, stream, a,
+  const unsigned tokens = kThreads >> tx_log2;
+  return launch_pdl(kernel, dim3((static_cast<unsigned>(a.T) + tokens - 1) / tokens), dim3(kThreads), 0, stream, a,
                     tx_log2);
 }
 
