@@ -586,20 +586,38 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const PagedAttnAr
   pdl_launch_dependents();
   const int4* split = static_cast<const int4*>(a.ws);
   const float* partial = reinterpret_cast<const float*>(split + kMaxGrid);
+  const int c0 = static_cast<int>(blockIdx.x), h = static_cast<int>(blockIdx.y);
+  // A warp's first part beside the description, which says whether it is one (most units have few)
+  const int c_first = min(c0 + warp, kMaxGrid - 1);
+  const float* p0 = partial + static_cast<size_t>(2 * c_first + (warp == 0)) * kPartFloats;
+  const float m0 = p0[h], l0 = p0[16 + h];
+  float z0[kJd];
+#pragma unroll
+  for (int e = 0; e < kJd; e += 2) {
+    const float2 v = *reinterpret_cast<const float2*>(p0 + 32 + h * kDh + lane * kJd + e);
+    z0[e] = v.x;
+    z0[e + 1] = v.y;
+  }
   const int4 unit = split[blockIdx.x];
-  const int c0 = static_cast<int>(blockIdx.x), c1 = unit.z, h = static_cast<int>(blockIdx.y);
+  const int c1 = unit.z;
   if (c1 < 0) return;
   const int hk = unit.y / parts, h0 = hk * group + (unit.y % parts) * kHeads;
   if (h >= hk * group + group - h0) return;
   float jm = -INFINITY, jl = 0.0f, jo[kJd];
 #pragma unroll
   for (int e = 0; e < kJd; ++e) jo[e] = 0.0f;
-  for (int k0 = c0 + warp; k0 <= c1; k0 += kBatch * kJoinWarps) {
+  if (c0 + warp <= c1) {
+    jm = m0;
+    jl = l0;
+#pragma unroll
+    for (int e = 0; e < kJd; ++e) jo[e] = z0[e];
+  }
+  for (int k0 = c0 + warp + kJoinWarps; k0 <= c1; k0 += kBatch * kJoinWarps) {
     float mk[kBatch], lk[kBatch], z[kBatch][kJd];
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
       const int cta = k0 + i * kJoinWarps;
-      const float* p = partial + static_cast<size_t>(2 * cta + (cta == c0)) * kPartFloats;
+      const float* p = partial + static_cast<size_t>(2 * cta) * kPartFloats;
       mk[i] = -INFINITY;
       lk[i] = 0.0f;
 #pragma unroll
