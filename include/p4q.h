@@ -13,6 +13,8 @@
  *      symmetric round-to-nearest INT4 weights with one scale per output
  *      channel, INT4 activations with one scale per token, integer matmul and
  *      dequantization.
+ * Beside these, what an answer needs: a paged key/value cache, attention of one
+ * new token over it, and sampling (the last section).
  *
  * Conventions shared by every entry point
  *   - Pointers are DEVICE pointers unless a parameter says otherwise. The
@@ -28,8 +30,10 @@
  *     Device-side waits are bounded: a wait that runs out sets a device error
  *     word, the kernel returns, and the next p4q_device_status() call reports
  *     P4Q_ERR_TIMEOUT. No call aborts the process or traps the GPU.
- *   - Behaviour on non-finite inputs is unspecified (no fault, values undefined).
- *   - Alignment: every device pointer must be 16-byte aligned.
+ *   - Behaviour on non-finite inputs is unspecified (no fault, values undefined)
+ *     where a call does not say otherwise.
+ *   - Alignment: every device pointer must be 16-byte aligned, where a call does
+ *     not ask for less.
  */
 #ifndef P4Q_H_
 #define P4Q_H_
@@ -554,7 +558,10 @@ p4q_status p4q_rope_append(const uint16_t* q, int ldq, const uint16_t* k, int ld
  *   o[b, h] = sum_{j < lens[b]} p_j v_j,  p = softmax_j(scale q[b, h] . k_j),
  * with key/value head h / (H / Hkv), and lse[b, h] = ln sum_j exp(scale q . k_j).
  * A sequence with lens[b] <= 0 has o = 0 and lse = -inf. Positions from lens[b]
- * on are not read. fp32 products, softmax and sums; o rounded once.
+ * on do not count, whatever lies there. fp32 products, softmax and sums; the weights enter
+ * the product with v as two 16-bit values each; o rounded once. Non-finite q, k and v of
+ * counting positions act as in the formula (a score of -inf has no weight; if all have
+ * none, o = 0 and lse = -inf).
  * A length beyond the page table's columns (or 2^30) is cut to them, and the
  * positions of a page outside the cache count as masked (both P4Q_ERR_INDEX).
  *   q, o  [kv->seqs, ldq / ldo] kv->dtype, H heads of dh (o written)

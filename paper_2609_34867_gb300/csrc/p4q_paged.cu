@@ -29,10 +29,10 @@
 // room for eight warps, which their products' and exchanges' latencies bound: 907.)
 //
 // Bound: HBM. 64 x 16384 positions, 32 heads over 8 of 128, bf16 (4.3 GB): 631 us =
-// 6.8 TB/s, the measured copy; 24 sequences of up to 2048 x 40 heads 85 us = 0.91 of
-// it, 128 of up to 8190 (skewed) x 8 172 = 0.94; one of 32011 x 8 28 = 0.69, of 704 x
-// 40 10. What the short ones cost is a chain: lengths, page numbers, keys 4.6 us,
-// the end of a kernel and the second kernel 5.
+// 6.8 TB/s, the measured copy; 24 sequences of up to 2048 x 40 heads 84 us = 0.92 of
+// it, 128 of up to 8190 (skewed) x 8 170 = 0.96; one of 32011 x 8 28 = 0.69, of 704 x
+// 40 9.8. What the short ones cost is a chain: lengths, page numbers, keys 4.6 us,
+// the end of a kernel and the second kernel 4.
 #include <cuda_runtime.h>
 
 #include <algorithm>

@@ -27,6 +27,12 @@
 // histogram) and their prefix over the cluster; then the one CTA that contains the
 // drawn number finds the warp (a warp's tokens are consecutive), and that
 // warp walks its tokens.
+//
+// Bound: phases between barriers of the CTA and the cluster, at two CTAs of 512
+// threads per SM, and 31 (no cut) to 130 instructions per logit; HBM is at 2 TB/s at
+// most. us: 256 x 131072 fp32 without cuts 67, top-k 96, with top-p 99, largest logit only
+// 38, top-p of thousands of tokens 218; 64 x 32000 fp16 8.2, 11.4, 12.5, 3.8, 22; one row
+// 5.4, 8.8, 9.6, 2.8, 15.
 #include <climits>
 #include <cuda_runtime.h>
 
