@@ -21,8 +21,10 @@
 // bits each); a bin of equal logits is cut by index.
 // Mostly few tokens can be kept at all: up to the bin of a top-k or top-p cut, or
 // those that pass a min-p. Up to 512 of them go to the cluster's first CTA, which
-// sorts them and makes the cuts and the draw on that list alone. What follows is
-// for the rest:
+// sorts them and makes the cuts and the draw on that list alone. A top-k of up to 256
+// looks for them with a histogram of the threads' largest logits instead of all
+// (a thread then looks through its own if its largest is in reach: 256 x 131072 fp32
+// 96 us to 77, 64 x 32000 fp16 11.4 to 9.7). What follows is for the rest:
 // The draw: kept weights per CTA (behind a top-p cut they are known from the
 // histogram) and their prefix over the cluster; then the one CTA that contains the
 // drawn number finds the warp (a warp's tokens are consecutive), and that
@@ -30,9 +32,10 @@
 //
 // Bound: phases between barriers of the CTA and the cluster, at two CTAs of 512
 // threads per SM, and 31 (no cut) to 130 instructions per logit; HBM is at 2 TB/s at
-// most. us: 256 x 131072 fp32 without cuts 67, top-k 96, with top-p 99, largest logit only
-// 38, top-p of thousands of tokens 218; 64 x 32000 fp16 8.2, 11.4, 12.5, 3.8, 22; one row
-// 5.4, 8.8, 9.6, 2.8, 15.
+// most. us: 256 x 131072 fp32 without cuts 67, top-k 77, with top-p 79, largest logit only
+// 38, top-p of thousands of tokens 210; 64 x 32000 fp16 8.0, 9.7, 10.9, 3.9, 22; one row
+// 5.6, 7.9, 8.6, 2.9, 14. (The loops over a thread's logits are not unrolled: 150 KB of
+// code instead of 217, and no slower.)
 #include <climits>
 #include <cuda_runtime.h>
 
@@ -79,6 +82,7 @@ struct Shared {
   u64 cut;                        // the last kept token
   uint32_t bin, sent, n, kmin, kmax;  // candidates sent; of the CTA's list: its length, smallest and largest key
   uint32_t red[kWarps];
+  uint32_t param[5];              // the row's temperature, top-k, top-p, min-p and uniform number
 };
 
 __device__ __forceinline__ float float_of_key(uint32_t k) {
@@ -130,6 +134,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
   };
   // The variable in every CTA of the cluster: by one thread, or by a warp's lanes.
   auto put32 = [&](uint32_t* p, uint32_t v) {
+#pragma unroll 1
     for (int r = 0; r < cs; ++r) st_shared_cluster_u32(mapa_shared(smem_u32(p), r), v);
   };
   auto put64 = [&](u64* p, u64 v) {
@@ -154,6 +159,27 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
   const int end = V + skip;
   row -= skip * kSize;
   const int w0 = (rank * kWarps + warp) * steps * 128;  // the warp's first element
+  // What is needed later, while the row is under way: the row's parameters, an empty histogram
+  uint32_t param = 0;
+  if (tid < 5) {
+    const void* const from = tid == 0 ? static_cast<const void*>(a.temperature)
+                             : tid == 1 ? static_cast<const void*>(a.top_k)
+                             : tid == 2 ? static_cast<const void*>(a.top_p)
+                             : tid == 3 ? static_cast<const void*>(a.min_p)
+                                        : static_cast<const void*>(a.u);
+    param = from ? static_cast<const uint32_t*>(from)[n] : tid == 0 || tid == 2 ? 0x3F800000u : 0u;
+  }
+  auto empty = [&]() {  // the histogram and the lists
+    for (int i = tid; i < kBins; i += kThreads) s.lo[i] = s.hi[i] = 0;
+    if (tid == 0) {
+      s.sent = 0;
+      s.n = 0;
+      s.kmin = 0xFFFFFFFFu;
+      s.kmax = 0;
+    }
+  };
+  empty();
+  bool is_empty = true;
   float4* const mine4 = xs + warp * steps * 32;
   auto clean = [](float v) { return fmaxf(v, -INFINITY); };  // NaN counts as -inf
   float mx = -INFINITY;
@@ -221,6 +247,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
     else raw = edge(e);
     keep(k, raw);
   }
+  if (tid < 5) s.param[tid] = param;
+  const float own_mx = mx;  // this lane's
   __syncwarp();
   // f(logit, token) for this lane's four tokens of a step; for all of them
   const int i0 = w0 + lane * 4 - skip;
@@ -233,7 +261,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
     f(v.w, i + 3);
   };
   auto each = [&](auto&& f) {
-#pragma unroll 2
+#pragma unroll 1
     for (int st = 0; st < steps; ++st) four(st, f);
   };
   auto key_of = [](float v) { return float_order_key(v + 0.0f); };  // (-0 as +0)
@@ -259,7 +287,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
     }
     return;
   }
-  const float temp = a.temperature ? a.temperature[n] : 1.0f;
+  const float temp = __uint_as_float(s.param[0]);
   if (!(temp > 0.0f)) {  // the first of the largest
     uint32_t first = 0xFFFFFFFFu;
     each([&](float v, int i) {
@@ -323,9 +351,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
     }
     return all <= kList && most <= static_cast<uint32_t>(room) ? all : 0u;
   };
-  const int top_k = a.top_k ? a.top_k[n] : 0;
-  const float top_p = a.top_p ? a.top_p[n] : 1.0f;
-  const float min_p = a.min_p && a.min_p[n] > 0.0f ? fminf(a.min_p[n], 1.0f) : 0.0f;
+  const int top_k = static_cast<int>(s.param[1]);
+  const float top_p = __uint_as_float(s.param[2]);
+  float min_p = __uint_as_float(s.param[3]);
+  min_p = min_p > 0.0f ? fminf(min_p, 1.0f) : 0.0f;  // (NaN: none)
   // past d_max exp(-d) < min_p for certain (weights are 0 past 22.2)
   const float d_max = fminf(min_p > 0.0f ? 1e-5f - 1.000001f * logf(min_p) : 23.0f, 23.0f);
   const bool by_k = top_k > 0 && top_k < V, by_p = top_p < 1.0f;
@@ -341,7 +370,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
   };
   // Sorts a value of each of the first `size` threads (a power of two, 32 .. kList), falling, all threads calling.
   auto sort = [&](u64 v, uint32_t size) -> u64 {
+#pragma unroll 1
     for (uint32_t k = 2; k <= size; k <<= 1)
+#pragma unroll 1
       for (uint32_t j = k >> 1; j > 0; j >>= 1) {
         u64 other;
         if (j >= 32) {
@@ -374,10 +405,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
   };
   static_assert(kList == kThreads, "a candidate per thread");
   // The cuts and the draw on the `found` candidates, by the first CTA. with_k: they are the first top_k
-  // tokens and some after these; else `all` is the sum of the weights that a top-p is a share of.
+  // tokens and some after these; else s.total is the sum of the weights that a top-p is a share of.
   // Up to 128 are compared pairwise (kThreads / size lanes per token), more are sorted: twice, for the
   // cuts by logit and for the draw by index (64: 2.0 k cycles instead of 6.1 k).
-  auto finish = [&](uint32_t found, bool with_k, u64 all) {
+  auto finish = [&](uint32_t found, bool with_k) {
     uint32_t size = 32;
     while (size < found) size <<= 1;
     const bool pairs = size <= 128;
@@ -426,7 +457,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
       const u64 to = scan_cta(in_k && way == 0 ? w : 0u, &sum);
       if (!pairs) before = to - w;
       if (tid == 0) {  // (64-bit floating point is slow: once)
-        const double part = ceil(static_cast<double>(top_p) * static_cast<double>(with_k ? sum : all));
+        const double part = ceil(static_cast<double>(top_p) * static_cast<double>(with_k ? sum : s.total));
         s.need = part < 1.0 ? 1ull : static_cast<u64>(part);
       }
       __syncthreads();
@@ -453,7 +484,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
       upto = scan_cta(static_cast<uint32_t>(mine), &total);
     }
     if (tid == 0) {
-      const double want = floor(static_cast<double>(a.u[n]) * static_cast<double>(total));
+      const double want = floor(static_cast<double>(__uint_as_float(s.param[4])) * static_cast<double>(total));
       const u64 r = want > 0.0 ? static_cast<u64>(fmin(want, 9.0e15)) : 0ull;
       s.draw = min(r, total - 1);
     }
@@ -473,33 +504,36 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
   };
 
   // Shortens the kept head: to `need` tokens, or (by_mass) to the first tokens
-  // whose weights reach ceil(share * the kept weights' sum). True: the kept tokens are few, and the
-  // first CTA has drawn one of them.
-  auto shorten = [&](auto mass_c, u64 need, float share) -> bool {
+  // whose weights reach ceil(share * the kept weights' sum). Where the kept tokens are few, it only finds
+  // found_n candidates.
+  uint32_t found_n = 0;  // candidates that the first CTA draws one of
+  bool found_k = false;
+  auto shorten = [&](auto mass_c, u64 need, float share) {
     constexpr bool by_mass = decltype(mass_c)::value;
     uint32_t key_lo = 0, key_hi = 0;
     int shift = 0;
     u64 below = 0;  // (by_mass) the CTA's weights before the bin
-    for (int level = 0;; ++level) {
-      for (int i = tid; i < kBins; i += kThreads) {
-        s.lo[i] = 0;
-        if (by_mass) s.hi[i] = 0;
+    // Of the first `need` tokens mostly a histogram of the lanes' largest logits alone will do: up to the bin in
+    // which `need` lanes are reached there are as many tokens or more, and few more while the lanes are many.
+    bool lanes = !by_mass && need <= kList / 2 && need <= static_cast<u64>(cs) * (kThreads / 2);
+    for (int level = 0;;) {
+      if (!is_empty) {
+        empty();
+        __syncthreads();
       }
-      if (tid == 0) {
-        s.sent = 0;
-        s.n = 0;
-        s.kmin = 0xFFFFFFFFu;
-        s.kmax = 0;
-      }
-      __syncthreads();
+      is_empty = false;
       // the bin of a token behind kBinBase's bit pattern (falling logits have rising bins); past the bins: larger
       auto bin_of = [&](float v) -> int {
         if (level == 0) return __float_as_int(d_bin(v));
         const uint32_t k = key_of(v);
         return k >= key_lo && k <= key_hi ? __float_as_int(kBinBase) + static_cast<int>((key_hi - k) >> shift) : INT_MAX;
       };
-#pragma unroll 2
-      for (int st = 0; st < steps; ++st) {
+      if (lanes) {
+        const uint32_t bin = static_cast<uint32_t>(__float_as_int(d_bin(own_mx)) - __float_as_int(kBinBase));
+        if (bin < kBins) atomicAdd(&s.lo[bin], 1u);
+      }
+#pragma unroll 1
+      for (int st = lanes ? steps : 0; st < steps; ++st) {
         const float4 v4 = mine4[st * 32 + lane];
         const float v[4] = {v4.x, v4.y, v4.z, v4.w};
         uint32_t bin[4], w[4];
@@ -574,15 +608,48 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
         if (lane == 0) s.total = total;
       }
       __syncthreads();
-      if (!by_mass && level == 0 && s.total <= need) return false;  // every token that may be drawn is among the first `need`
       const int cut_bin = static_cast<int>(s.bin);
+      if (!by_mass && level == 0 && s.total <= need) {
+        sync_all();  // (the CTAs' bins and sums have been read)
+        if (!lanes) return;  // every token that may be drawn is among the first `need`
+        lanes = false;
+        continue;
+      }
       const bool few = level == 0 && (by_mass || need <= kList);  // the tokens up to the bin may be few
+      const int cut_bits = __float_as_int(kBinBase) + cut_bin;
+      if (lanes) {
+        if (__float_as_int(d_bin(own_mx)) <= cut_bits) {
+          for (int st = 0; st < steps; ++st) {  // the logits that this lane loaded
+            const int at4 = kType == 2 ? st * 32 + lane : ((st >> 1) * 32 + lane) * 2 + (st & 1);
+            const float4 v4 = mine4[at4];
+            const float v[4] = {v4.x, v4.y, v4.z, v4.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              if (__float_as_int(d_bin(v[j])) > cut_bits) continue;
+              const uint32_t at = atomicAdd(&s.sent, 1u);
+              if (at < static_cast<uint32_t>(room))
+                st_shared_cluster_u64(mapa_shared(smem_u32(&s.cand[rank * room + at]), 0),
+                                      static_cast<u64>(key_of(v[j])) << 32 |
+                                          static_cast<uint32_t>(~(w0 - skip + at4 * 4 + j)));
+            }
+          }
+        }
+        __syncthreads();
+        if (warp == 0) put32_lanes(&s.cand_n[rank], s.sent);
+        sync_all();
+        found_n = candidates();
+        found_k = true;
+        if (found_n > 0) return;
+        sync_all();  // (the counts have been read)
+        lanes = false;
+        continue;
+      }
       need = s.need;
       // The bin's tokens of this CTA; those up to it to the first CTA.
       uint32_t kmin = 0xFFFFFFFFu, kmax = 0;
-      const int cut_bits = __float_as_int(kBinBase) + cut_bin;
-#pragma unroll 2
-      for (int st = 0; st < steps; ++st) {
+      const bool none = level == 0 && !__any_sync(0xFFFFFFFFu, __float_as_int(d_bin(own_mx)) <= cut_bits);
+#pragma unroll 1
+      for (int st = none ? steps : 0; st < steps; ++st) {
         const float4 v4 = mine4[st * 32 + lane];
         const float v[4] = {v4.x, v4.y, v4.z, v4.w};
         const int bits[4] = {bin_of(v[0]), bin_of(v[1]), bin_of(v[2]), bin_of(v[3])};
@@ -633,8 +700,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
       }
       sync_all();
       if (const uint32_t c = few ? candidates() : 0u) {
-        if (rank == 0) finish(c, !by_mass, s.total);
-        return true;
+        found_n = c;
+        found_k = !by_mass;
+        return;
       }
       uint32_t found = 0, most = 0;
       key_lo = 0xFFFFFFFFu;
@@ -679,7 +747,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
           cta_mass = below + warp_add(sum);
           known = true;
         }
-        return false;
+        return;
       }
       if (key_lo == key_hi) {  // equal logits: so many of them, by index
         const float v = float_of_key(key_lo);
@@ -716,22 +784,25 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
         sync_all();
         cut_x = v;
         cut_i = static_cast<int>(s.cut);
-        return false;
+        return;
       }
       const int bits = 32 - __clz(key_hi - key_lo);
       shift = max(0, bits - 11);
+      ++level;
     }
   };
 
-  if (by_k && shorten(std::false_type{}, static_cast<u64>(top_k), 0.0f)) return;
+  if (by_k) shorten(std::false_type{}, static_cast<u64>(top_k), 0.0f);
   // (a top-k that cuts has set cut_x; beside one that does not, the other cuts are as without)
-  if (cut_x == -INFINITY && min_p > 0.0f && d_max <= kNear) {
+  if (found_n == 0 && cut_x == -INFINITY && min_p > 0.0f && d_max <= kNear) {
     __syncthreads();
     if (tid == 0) s.sent = 0;
+    is_empty = false;
     __syncthreads();
     u64 all = 0;
-#pragma unroll 2
-    for (int st = 0; st < steps; ++st) {
+    const bool none = !by_p && !__any_sync(0xFFFFFFFFu, dist(own_mx) <= d_max);
+#pragma unroll 1
+    for (int st = none ? steps : 0; st < steps; ++st) {
       const float4 v4 = mine4[st * 32 + lane];
       const float v[4] = {v4.x, v4.y, v4.z, v4.w};
       bool in[4];
@@ -752,14 +823,21 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
     sync_all();
     const uint32_t found = candidates();
     if (found > 0) {
-      all = 0;
-      for (int r = 0; r < cs; ++r) all += s.mass[r];
-      if (rank == 0) finish(found, false, all);
-      return;
+      found_n = found;
+      if (tid == 0) {
+        all = 0;
+        for (int r = 0; r < cs; ++r) all += s.mass[r];
+        s.total = all;
+      }
+    } else {
+      sync_all();  // (the exchanged values have been read)
     }
-    sync_all();  // (the exchanged values have been read)
   }
-  if (by_p && shorten(std::true_type{}, 0, top_p)) return;
+  if (found_n == 0 && by_p) shorten(std::true_type{}, 0, top_p);
+  if (found_n > 0) {
+    if (rank == 0) finish(found_n, found_k);
+    return;
+  }
 
   auto kept = [&](float v, int i) -> uint32_t {  // the kept weight
     if (v < cut_x) return 0u;
@@ -790,7 +868,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
   if (tid == 0) {  // (64-bit floating point is slow: once)
     u64 total = 0;
     for (int r = 0; r < cs; ++r) total += s.mass[r];
-    const double want = floor(static_cast<double>(a.u[n]) * static_cast<double>(total));
+    const double want = floor(static_cast<double>(__uint_as_float(s.param[4])) * static_cast<double>(total));
     const u64 r = want > 0.0 ? static_cast<u64>(fmin(want, 9.0e15)) : 0ull;
     s.draw = min(r, total - 1);
     s.total = total;

@@ -192,6 +192,33 @@ def test_equal_logits_go_by_index(p4q, dev, dt):
             assert abs(lp[n] + math.log(kept)) < 1e-5
 
 
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("V", [900, 32003, 131071])
+def test_the_largest_logits_lie_side_by_side(p4q, dev, dt, V):
+    """Rising rows, a heap of large logits in one place, and rows with fewer finite logits than a top-k asks for."""
+    rows = 8
+    x = logits(dev, rows, V, dt, seed=11).float()
+    x[0] = torch.linspace(-30, 0, V, device=dev)
+    x[1] = torch.linspace(0, -9, V, device=dev)
+    x[2, 300:556] = torch.linspace(11, 15, 256, device=dev)  # (seen by few of the threads that load the row)
+    x[3, V - 40:] = 20.0
+    x[4, :] = float("-inf")
+    x[4, 100:150] = torch.linspace(0, 3, 50, device=dev)
+    x[5, :] = -float("inf")
+    x[5, ::97] = 1.0
+    x[6, 7:] -= 500.0  # past the range of weights that are not 0
+    x = x.to(dt)
+    xs = x.float().cpu().numpy()
+    u = np.random.default_rng(V).random(rows).astype(np.float32)
+    for k in (1, 3, 40, 49, 50, 51, 130, 255, 256, 257, 600):
+        ks = np.full(rows, k, np.int32)
+        for params in ({"top_k": ks}, {"top_k": ks, "top_p": np.full(rows, 0.8, np.float32)},
+                       {"top_k": ks, "min_p": np.full(rows, 0.02, np.float32)}):
+            token, lp = draw(p4q, dev, x, u, **params)
+            for n in range(rows):
+                check_row(xs[n], float(u[n]), int(token[n]), float(lp[n]), **{key: val[n] for key, val in params.items()})
+
+
 def test_ties_at_the_cut_go_to_the_lower_index(p4q, dev):
     """Three levels of logits, far apart in index, in no order; the cut falls inside a level."""
     V = 40000
