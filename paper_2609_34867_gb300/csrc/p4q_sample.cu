@@ -14,8 +14,8 @@
 // no part). Every CTA gets the sums of all CTAs' groups of 32 bins, one warp of it
 // finds the group and, from the CTAs' bins of that, the bin in which the wanted
 // sum is reached. The bin's tokens, mostly a few, are gathered in every CTA and
-// ranked. (Two barriers of the cluster per cut; a scan divided among the CTAs and
-// a ranking by one thread per token took 30 k cycles where this takes 7.) Bins
+// ranked, a share of them by each. (A scan divided among the CTAs and a ranking by
+// one thread per token took 30 k cycles where this takes 7.) Bins
 // of more tokens than the lists hold are
 // divided again by the logits' ordered bit patterns, at most three times (11 of 32
 // bits each); a bin of equal logits is cut by index.
@@ -24,7 +24,7 @@
 // sorts them and makes the cuts and the draw on that list alone. A top-k of up to 256
 // looks for them with a histogram of the threads' largest logits instead of all
 // (a thread then looks through its own if its largest is in reach: 256 x 131072 fp32
-// 96 us to 77, 64 x 32000 fp16 11.4 to 9.7). What follows is for the rest:
+// 96 us to 77, 64 x 32000 fp16 11.4 to 9.5). What follows is for the rest:
 // The draw: kept weights per CTA (behind a top-p cut they are known from the
 // histogram) and their prefix over the cluster; then the one CTA that contains the
 // drawn number finds the warp (a warp's tokens are consecutive), and that
@@ -33,8 +33,8 @@
 // Bound: phases between barriers of the CTA and the cluster, at two CTAs of 512
 // threads per SM, and 31 (no cut) to 130 instructions per logit; HBM is at 2 TB/s at
 // most. us: 256 x 131072 fp32 without cuts 67, top-k 77, with top-p 79, largest logit only
-// 38, top-p of thousands of tokens 210; 64 x 32000 fp16 8.0, 9.7, 10.9, 3.9, 22; one row
-// 5.6, 7.9, 8.6, 2.9, 14. (The loops over a thread's logits are not unrolled: 150 KB of
+// 38, top-p of thousands of tokens 189; 64 x 32000 fp16 8.0, 9.5, 10.6, 3.9, 22; one row
+// 5.6, 7.8, 8.5, 2.9, 14. (The loops over a thread's logits are not unrolled: 150 KB of
 // code instead of 217, and no slower.)
 #include <climits>
 #include <cuda_runtime.h>
@@ -713,7 +713,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
         key_lo = min(key_lo, s.key_min[r]);
         key_hi = max(key_hi, s.key_max[r]);
       }
-      if (found <= kList && most <= kOwn) {  // every CTA ranks them for itself
+      if (found <= kList && most <= kOwn) {  // every CTA ranks its share of them (all in each: 256 x 131072 210 us, so 189)
         for (uint32_t i = tid; i < found; i += kThreads) {
           int r = 0;
           uint32_t j = i;
@@ -723,7 +723,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
           if (by_mass) s.weight[i] = weight(dist(float_of_key(static_cast<uint32_t>(t >> 32))));
         }
         __syncthreads();
-        for (uint32_t i = warp; i < found; i += kWarps) {  // a warp per token: what comes before it
+        for (uint32_t i = rank * kWarps + warp; i < found; i += cs * kWarps) {  // a warp per token: what comes before it
           const u64 t = s.list[i];
           u64 before = 0;
           if (by_mass) {
@@ -734,9 +734,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
             for (uint32_t j = lane; j < found; j += 32) c += s.list[j] > t ? 1u : 0u;
             before = __reduce_add_sync(0xFFFFFFFFu, c);
           }
-          if (before < need && need <= before + (by_mass ? s.weight[i] : 1u) && lane == 0) s.cut = t;
+          if (before < need && need <= before + (by_mass ? s.weight[i] : 1u)) put64_lanes(&s.cut, t);
         }
-        __syncthreads();
+        sync_all();
         const u64 last = s.cut;
         cut_x = float_of_key(static_cast<uint32_t>(last >> 32));
         cut_i = static_cast<int>(~static_cast<uint32_t>(last));
