@@ -32,9 +32,9 @@
 //
 // Bound: phases between barriers of the CTA and the cluster, at two CTAs of 512
 // threads per SM, and 31 (no cut) to 130 instructions per logit; HBM is at 2 TB/s at
-// most. us: 256 x 131072 fp32 without cuts 67, top-k 77, with top-p 79, largest logit only
-// 38, top-p of thousands of tokens 189; 64 x 32000 fp16 8.0, 9.5, 10.6, 3.9, 22; one row
-// 5.6, 7.8, 8.5, 2.9, 14. (The loops over a thread's logits are not unrolled: 150 KB of
+// most. us: 256 x 131072 fp32 without cuts 67, top-k 76, with top-p 77, largest logit only
+// 38, top-p of thousands of tokens 189; 64 x 32000 fp16 7.9, 9.5, 9.7, 3.9, 22; one row
+// 5.7, 7.8, 8.1, 2.9, 13. (The loops over a thread's logits are not unrolled: 150 KB of
 // code instead of 217, and no slower.)
 #include <climits>
 #include <cuda_runtime.h>
@@ -453,10 +453,13 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
     }
     const bool in_k = real && !(with_k && place >= static_cast<uint32_t>(top_k));
     if (by_p) {
-      u64 sum;
-      const u64 to = scan_cta(in_k && way == 0 ? w : 0u, &sum);
-      if (!pairs) before = to - w;
-      if (tid == 0) {  // (64-bit floating point is slow: once)
+      u64 sum = before + w;  // (of the last of the first top_k: theirs)
+      bool last = way == 0 && place == min(static_cast<uint32_t>(top_k), found) - 1;
+      if (!pairs) {
+        before = scan_cta(in_k ? w : 0u, &sum) - w;
+        last = tid == 0;
+      }
+      if (with_k ? last : tid == 0) {  // (64-bit floating point is slow: once)
         const double part = ceil(static_cast<double>(top_p) * static_cast<double>(with_k ? sum : s.total));
         s.need = part < 1.0 ? 1ull : static_cast<u64>(part);
       }
