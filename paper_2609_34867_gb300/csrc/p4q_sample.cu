@@ -59,6 +59,7 @@ constexpr int kList = 512;          // tokens of a bin that are ranked, at most
 constexpr int kOwn = 256;           // of one CTA
 
 constexpr int kGroups = kBins / 32;
+constexpr int kPairs = 128;         // candidates that are compared pairwise, at most
 constexpr int kCand = 768;          // places for candidates, each CTA a part of them
 constexpr float kNear = 8.0f;       // a min-p of at least e^-8 mostly leaves few tokens
 
@@ -406,12 +407,12 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
   static_assert(kList == kThreads, "a candidate per thread");
   // The cuts and the draw on the `found` candidates, by the first CTA. with_k: they are the first top_k
   // tokens and some after these; else s.total is the sum of the weights that a top-p is a share of.
-  // Up to 128 are compared pairwise (kThreads / size lanes per token), more are sorted: twice, for the
-  // cuts by logit and for the draw by index (64: 2.0 k cycles instead of 6.1 k).
+  // Up to 128 are compared pairwise (kThreads / size lanes per token; 64: 2.0 k cycles instead of 6.1 k), more
+  // are sorted (200 of 64 x 32000 fp16 pairwise 21.5 us instead of 16.4). Likewise the kept ones, for the draw by index.
   auto finish = [&](uint32_t found, bool with_k) {
     uint32_t size = 32;
     while (size < found) size <<= 1;
-    const bool pairs = size <= 128;
+    const bool pairs = size <= kPairs;
     const int ways = pairs ? kThreads / static_cast<int>(size) : 1;  // 4 .. 16 neighbouring lanes
     const uint32_t at = static_cast<uint32_t>(tid / ways), way = static_cast<uint32_t>(tid % ways);
     u64 t = 0;  // (no token: below every token)
@@ -422,18 +423,15 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
       t = s.cand[r * room + j];
     }
     __syncthreads();  // (the list lies in the same place)
-    if (!pairs && (by_p || with_k)) t = sort(t, size);
+    if (!pairs) t = sort(t, size);
     const bool real = at < found;
-    float e = 0.0f, d = 0.0f;
-    if (real) {
-      d = dist(float_of_key(static_cast<uint32_t>(t >> 32)));
-      e = expf(-d);
-    }
+    const float e = real ? expf(-dist(float_of_key(static_cast<uint32_t>(t >> 32)))) : 0.0f;
     const uint32_t w = __float2uint_rn(e * 2147483648.0f);
     uint32_t place = at;  // among the candidates
     u64 before = 0;       // the weights before it
-    auto sum_ways = [&](u64 v) {
-      for (int x = 1; x < ways; x <<= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, x);
+    auto sum_lanes = [](u64 v, int lanes) {  // over neighbouring lanes
+#pragma unroll 1
+      for (int x = 1; x < lanes; x <<= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, x);
       return v;
     };
     if (pairs) {
@@ -448,8 +446,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
           ++c;
           before += s.weight[j];
         }
-      place = static_cast<uint32_t>(sum_ways(c));
-      before = sum_ways(before);
+      place = static_cast<uint32_t>(sum_lanes(c, ways));
+      before = sum_lanes(before, ways);
     }
     const bool in_k = real && !(with_k && place >= static_cast<uint32_t>(top_k));
     if (by_p) {
@@ -466,22 +464,31 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
       __syncthreads();
     }
     const bool is_kept = in_k && w > 0 && !(e < min_p) && (!by_p || before < s.need);
-    // by index: its complement, and the weight
+    // The draw: the kept tokens are the first ones; by index: its complement, and the weight.
+    const uint32_t kept = static_cast<uint32_t>(__syncthreads_count(is_kept && way == 0));  // (the list has been read)
     u64 mine = is_kept ? static_cast<u64>(static_cast<uint32_t>(t)) << 32 | w : 0ull;
-    u64 upto, total;  // the kept weights up to this token, all
-    if (pairs) {
-      __syncthreads();  // (the tokens in the list have been read)
-      if (way == 0) s.list[at] = mine;
+    u64 upto = 0, total = 0;  // the kept weights up to this token, all
+    uint32_t key = 0;         // this token's logit
+    bool leader = true;
+    if (kept <= kPairs) {
+      if (is_kept && way == 0) {
+        s.list[place] = mine;
+        s.own[place] = t;
+      }
+      int per = kThreads / 32;  // lanes per token
+      while (kThreads / per < static_cast<int>(kept)) per >>= 1;
       __syncthreads();
-      upto = 0;
-      u64 sum = 0;
-      for (uint32_t j = way; j < found; j += ways) {
+      const uint32_t to = static_cast<uint32_t>(tid / per), first = static_cast<uint32_t>(tid % per);
+      mine = to < kept ? s.list[to] : 0ull;
+      key = to < kept ? static_cast<uint32_t>(s.own[to] >> 32) : 0u;
+      leader = first == 0;
+      for (uint32_t j = first; j < kept; j += per) {
         const u64 x = s.list[j];
-        sum += static_cast<uint32_t>(x);
+        total += static_cast<uint32_t>(x);
         if (x >= mine) upto += static_cast<uint32_t>(x);
       }
-      upto = sum_ways(upto);
-      total = sum_ways(sum);
+      upto = sum_lanes(upto, per);
+      total = sum_lanes(total, per);
     } else {
       mine = sort(mine, size);
       upto = scan_cta(static_cast<uint32_t>(mine), &total);
@@ -493,15 +500,16 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
     }
     __syncthreads();
     const u64 r = s.draw;
-    if (way == 0 && upto - static_cast<uint32_t>(mine) <= r && r < upto) {
+    if (leader && upto - static_cast<uint32_t>(mine) <= r && r < upto) {
       const int i = static_cast<int>(~static_cast<uint32_t>(mine >> 32));
       a.token[n] = i;
       if (a.logprob) {
-        if (!pairs) {  // (sorted by index: the lane's d is another token's)
+        float x = float_of_key(key);
+        if (kept > kPairs) {  // (sorted without it)
           const void* p = row + static_cast<size_t>(i + skip) * kSize;
-          d = dist(kType == 2 ? *static_cast<const float*>(p) : from16<kType == 1>(*static_cast<const uint16_t*>(p)));
+          x = kType == 2 ? *static_cast<const float*>(p) : from16<kType == 1>(*static_cast<const uint16_t*>(p));
         }
-        a.logprob[n] = -d - logf(static_cast<float>(static_cast<double>(total) * 4.656612873077393e-10));
+        a.logprob[n] = -dist(x) - logf(static_cast<float>(static_cast<double>(total) * 4.656612873077393e-10));
       }
     }
   };
