@@ -369,25 +369,36 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
     for (int w = 0; w < kWarps; ++w) all += s.warp_sum[w];
     return all;
   };
-  // Sorts a value of each of the first `size` threads (a power of two, 32 .. kList), falling, all threads calling.
-  auto sort = [&](u64 v, uint32_t size) -> u64 {
+  // Sorts a value of each of the first `size` threads (a multiple of 32, up to kList), falling, all threads calling;
+  // `count` values are not 0, and no two of these alike. The warps sort theirs, then each value's place is its own
+  // warp's and what searches in the others' find larger.
+  auto sort = [&](u64 v, uint32_t size, uint32_t count) -> u64 {
 #pragma unroll 1
-    for (uint32_t k = 2; k <= size; k <<= 1)
+    for (uint32_t k = 2; k <= 32; k <<= 1)
 #pragma unroll 1
       for (uint32_t j = k >> 1; j > 0; j >>= 1) {
-        u64 other;
-        if (j >= 32) {
-          s.list[tid] = v;
-          __syncthreads();
-          other = s.list[tid ^ j];
-          __syncthreads();
-        } else {
-          other = __shfl_xor_sync(0xFFFFFFFFu, v, j);
-        }
-        const bool larger = ((tid & k) == 0) == ((tid & j) == 0);
+        const u64 other = __shfl_xor_sync(0xFFFFFFFFu, v, j);
+        const bool larger = ((lane & k) == 0) == ((lane & j) == 0);
         v = larger == (other > v) ? other : v;
       }
-    return v;
+    s.list[tid] = v;
+    __syncthreads();
+    uint32_t place = static_cast<uint32_t>(lane);
+    if (v != 0) {
+#pragma unroll 4
+      for (uint32_t w = 0; w < size; w += 32) {
+        const u64* const in = s.list + w;
+        uint32_t more = 0;
+#pragma unroll
+        for (uint32_t step = 16; step > 0; step >>= 1) more += in[more + step - 1] > v ? step : 0u;
+        more += in[more] > v ? 1u : 0u;
+        place += w == static_cast<uint32_t>(warp) * 32 ? 0u : more;
+      }
+    }
+    __syncthreads();
+    if (v != 0) s.list[place] = v;
+    __syncthreads();
+    return static_cast<uint32_t>(tid) < count ? s.list[tid] : 0ull;
   };
   // Inclusive scan over the CTA's threads; *all: the sum.
   auto scan_cta = [&](u64 v, u64* all) -> u64 {
@@ -407,8 +418,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
   static_assert(kList == kThreads, "a candidate per thread");
   // The cuts and the draw on the `found` candidates, by the first CTA. with_k: they are the first top_k
   // tokens and some after these; else s.total is the sum of the weights that a top-p is a share of.
-  // Up to 128 are compared pairwise (kThreads / size lanes per token; 64: 2.0 k cycles instead of 6.1 k), more
-  // are sorted (200 of 64 x 32000 fp16 pairwise 21.5 us instead of 16.4). Likewise the kept ones, for the draw by index.
+  // Up to 128 are compared pairwise (kThreads / size lanes per token), more are sorted (200 of 64 x 32000 fp16
+  // 14.2 us, pairwise 21.5, by a bitonic sort of all 16.4; 400: 22.6 and 21.7). Likewise the kept ones, for the
+  // draw by index.
   auto finish = [&](uint32_t found, bool with_k) {
     uint32_t size = 32;
     while (size < found) size <<= 1;
@@ -423,7 +435,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
       t = s.cand[r * room + j];
     }
     __syncthreads();  // (the list lies in the same place)
-    if (!pairs) t = sort(t, size);
+    if (!pairs) t = sort(t, size, found);
     const bool real = at < found;
     const float e = real ? expf(-dist(float_of_key(static_cast<uint32_t>(t >> 32)))) : 0.0f;
     const uint32_t w = __float2uint_rn(e * 2147483648.0f);
@@ -490,7 +502,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
       upto = sum_lanes(upto, per);
       total = sum_lanes(total, per);
     } else {
-      mine = sort(mine, size);
+      mine = sort(mine, size, kept);
       upto = scan_cta(static_cast<uint32_t>(mine), &total);
     }
     if (tid == 0) {
