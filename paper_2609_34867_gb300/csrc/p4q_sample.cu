@@ -225,9 +225,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
   };
   constexpr int kPer = 16 / kSize;  // logits per load
   const int loads = steps * 128 / (32 * kPer);
-  int k = 0;
+  const uint4* const src = reinterpret_cast<const uint4*>(row + static_cast<size_t>(w0) * kSize) + lane;
   if (w0 >= skip && w0 + steps * 128 <= end) {  // (the warp alike) all inside the row: eight loads in flight
-    const uint4* src = reinterpret_cast<const uint4*>(row + static_cast<size_t>(w0) * kSize) + lane;
+    int k = 0;
     for (; k + 8 <= loads; k += 8) {
       uint4 raw[8];
 #pragma unroll
@@ -240,13 +240,27 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
       keep(k, r0);
       keep(k + 1, r1);
     }
-  }
-  for (; k < loads; ++k) {
-    const int e = w0 + (k * 32 + lane) * kPer;
-    uint4 raw;
-    if (e >= skip && e + kPer <= end) raw = *reinterpret_cast<const uint4*>(row + static_cast<size_t>(e) * kSize);
-    else raw = edge(e);
-    keep(k, raw);
+    for (; k < loads; ++k) keep(k, src[k * 32]);
+  } else {  // four, then the 16 bytes that the row begins or ends in (one load after the other, with those
+            // in their places: 256 x 131071 fp32 58 us instead of 41, of 131072 38)
+    constexpr uint32_t kNone = kType == 2 ? 0xFF800000u : kType == 1 ? 0xFF80FF80u : 0xFC00FC00u;
+    for (int k = 0; k < loads; k += 4) {
+      uint4 raw[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int e = w0 + ((k + j) * 32 + lane) * kPer;
+        raw[j] = make_uint4(kNone, kNone, kNone, kNone);
+        if (k + j < loads && e >= skip && e + kPer <= end) raw[j] = src[(k + j) * 32];
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (k + j < loads) keep(k + j, raw[j]);
+    }
+#pragma unroll 1
+    for (int x = 0; x < 2; ++x) {
+      const int e = x == 0 ? 0 : (end - 1) / kPer * kPer, at = (e - w0) / kPer;
+      if (e >= w0 && at < loads * 32 && at % 32 == lane && (e < skip || e + kPer > end)) keep(at / 32, edge(e));
+    }
   }
   if (tid < 5) s.param[tid] = param;
   const float own_mx = mx;  // this lane's
