@@ -961,14 +961,17 @@ cudaError_t launch_type(const SampleArgs& a, cudaStream_t stream) {
     const int unit = 128 * kStep * kWarps * cs;
     return (elements + unit - 1) / unit * kStep;
   };
-  // CTAs per row: so that every SM has one and no slice is longer than 16384 (if
-  // a larger cluster can be had). Plain draws / top-p with clusters of 1, 2, 4, 8,
+  // CTAs per row: so that every SM has one, eight only while no SM gets two, and no
+  // slice is longer than 16384 (if a larger cluster can be had). Eight and four at 32 x
+  // 32000 fp16: plain 6.9, 6.8, top-k 14.3, 8.3, top-p 17.8, 17.4; at 16 x 32000 6.6, 6.7,
+  // 9.3, 8.3, 16.5, 17.3; at 8 x 65536 fp32 6.8, 8.7, 8.7, 9.0, 17.2, 23.0. Plain draws / top-p with clusters of 1, 2, 4, 8,
   // us: 1 x 32000 fp16 10.9, 7.5, 5.6, 5.2 / 27.6, 21.4, 15.0, 13.8; 64 x 32000
   // 14.1, 9.5, 8.2, 11.9 / 32.0, 21.6, 18.9, 30.0; 256 x 32000 bf16 25.0, 20.3,
   // 24.7, 39.0 / 60.8, 49.1, 62.2, 106; 256 x 131072 fp32 (4 and 8) 76.0, 64.8 /
   // 218, 193.
   int cs = 1;
-  while (cs < kMaxCluster && (a.rows * cs < num_sms() || steps_of(cs) > 8)) cs *= 2;
+  while (cs < kMaxCluster && ((2 * cs < kMaxCluster ? a.rows * cs < num_sms() : a.rows * 2 * cs <= num_sms()) || steps_of(cs) > 8))
+    cs *= 2;
   const int steps = steps_of(cs);
   if (steps > kMaxSteps) return cudaErrorInvalidValue;
   static SmemLimit limit;
