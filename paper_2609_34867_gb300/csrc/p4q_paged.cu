@@ -3,10 +3,11 @@
 //
 // Work: a unit is one key/value head of one sequence with up to 8 NT of the
 // query heads that share it (a group of more heads makes several units), cut
-// into tiles of positions. All units' tiles in one row, unit after unit, are
-// dealt to the CTAs in equal consecutive ranges, so a CTA's work does not
-// depend on how unequal the sequences are (few tiles: one piece of a unit per
-// CTA). The units that several CTAs share are joined by a second kernel.
+// into tiles of positions. Few units: each is a cluster's, and its CTAs'
+// parts are added up in the first one's shared memory. Else all units' tiles in one
+// row, unit after unit, are dealt to the CTAs in equal consecutive ranges, so a
+// CTA's work does not depend on how unequal the sequences are (few tiles: one piece
+// of a unit per CTA); the units that several CTAs share are joined by a second kernel.
 //
 // A warp takes 16 positions at a time, straight from global memory into the
 // operands of m16n8k16 tensor-core products, without shared memory: the
@@ -30,12 +31,14 @@
 //
 // Bound: HBM. 64 x 16384 positions, 32 heads over 8 of 128, bf16 (4.3 GB): 631 us =
 // 6.8 TB/s, the measured copy; 24 sequences of up to 2048 x 40 heads 84 us = 0.92 of
-// it, 128 of up to 8190 (skewed) x 8 170 = 0.96; one of 32011 x 8 28 = 0.69, of 704 x
-// 40 9.8. What the short ones cost is a chain: lengths, page numbers, keys 4.6 us,
-// the end of a kernel and the second kernel 4.
+// it, 128 of up to 8190 (skewed) x 8 170 = 0.96; one of 32011 x 8 28 = 0.69. Short ones
+// cost a chain: lengths, page numbers, keys 4.6 us, then the end of a kernel and the second
+// kernel 4, or the cluster's exchange 1.5: one of 704 x 40 6.2 us (by ranges 9.2), of 512 x 8
+// 4.1 (6.9), 10 of 1024 x 8 11.4 (15.8).
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "p4q_device.cuh"
 #include "p4q_elem.cuh"
@@ -52,6 +55,8 @@ constexpr int kThreads = 32 * kWarps;
 constexpr int kMaxGrid = 640;    // CTAs of a launch at most (partial results of the workspace)
 constexpr int kMinTiles = 2;     // tiles per CTA at least, of one unit
 constexpr int kUnitCost = 2;     // what a unit costs beside its tiles, in tiles
+constexpr int kMaxCluster = 8;   // CTAs that share a unit as a cluster
+constexpr int kJoinTiles = 6;    // what the second kernel costs, in tiles of a CTA
 constexpr long long kMaxLen = 1ll << 30;  // positions (places of a sequence are counted in 32 bits)
 constexpr float kShift = 7.0f;   // p = 2^(score - reference + 7): small p keep their bits in fp16
 constexpr float kMove = 8.0f;    // a reference moves when a score exceeds it by 2^8
@@ -87,6 +92,14 @@ __device__ __forceinline__ uint4 reload16(const uint4* p) {
   uint4 v;
   asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(smem_u32(p)));
   return v;
+}
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ void st_shared_cluster_v4(uint32_t a, float4 v) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(a), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -131,7 +144,7 @@ __device__ __forceinline__ unsigned long long quotient(unsigned long long a, uns
   return a / b;
 }
 
-template <bool kBf16, int kDh, int kNt, bool kSmallPage>
+template <bool kBf16, int kDh, int kNt, bool kSmallPage, bool kCluster>
 __global__ void __launch_bounds__(kThreads, kNt == 1 ? 3 : 2) paged_attention_kernel(const PagedAttnArgs a) {
   constexpr int kHeads = 8 * kNt;
   constexpr int kRep = 128 / kDh;          // blocks of 16 positions per warp and tile: 8 KB of keys and values
@@ -152,6 +165,7 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 3 : 2) paged_attention_ke
   int4* split = static_cast<int4*>(a.ws);
   float* partial = reinterpret_cast<float*>(split + kMaxGrid);
 
+  if (kCluster) cluster_arrive();  // (waited for before the first CTA's shared memory is written)
   pdl_wait();
   pdl_launch_dependents();
 
@@ -161,16 +175,24 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 3 : 2) paged_attention_ke
   };
   auto tiles_of = [&](int n) { return n <= kTile ? 1 : (n + kTile - 1) / kTile; };
 
-  // The tiles before this thread's sequences, their sum, and from these the
-  // CTA's range and where it begins. Few tiles: a CTA for each kMinTiles of a
-  // unit, so that none has two units one after the other; else equal ranges.
-  {
+  unsigned long long x = 0, last = 1;
+  int b, u, tile = 0;
+  const int cs = kCluster ? static_cast<int>(cluster_nctarank()) : 1, rank = kCluster ? static_cast<int>(cluster_ctarank()) : 0;
+  if (kCluster) {
+    const int unit = static_cast<int>(blockIdx.x) / cs;
+    b = unit / units;
+    u = unit % units;
+    if (a.lens[b] > room && rank == 0 && u == 0 && tid == 0) atomicOr(&g_paged_err, kErrIndex);
+  } else {
+    // The tiles before this thread's sequences, their sum, and from these the
+    // CTA's range and where it begins. Few tiles: a CTA for each kMinTiles of a
+    // unit, so that none has two units one after the other; else equal ranges.
     typedef unsigned long long u64;
     const int per = (c.seqs + kThreads - 1) / kThreads, b0 = min(c.seqs, tid * per), b1 = min(c.seqs, b0 + per);
     u64 mine = 0, padded = 0;
-    for (int b = b0; b < b1; ++b) {
-      const int n = tiles_of(length(b));
-      if (a.lens[b] > room && blockIdx.x == 0) atomicOr(&g_paged_err, kErrIndex);
+    for (int i = b0; i < b1; ++i) {
+      const int n = tiles_of(length(i));
+      if (a.lens[i] > room && blockIdx.x == 0) atomicOr(&g_paged_err, kErrIndex);
       mine += span_of(n, 0);
       padded += span_of(n, 1);
     }
@@ -210,10 +232,10 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 3 : 2) paged_attention_ke
     if (first >= total) return;  // (the whole CTA)
     if (first >= (upto - mine) * units && first < upto * units) {
       u64 at = (upto - mine) * units;
-      for (int b = b0; b < b1; ++b) {
-        const u64 n = static_cast<u64>(span_of(tiles_of(length(b)), pieces)) * units;
+      for (int i = b0; i < b1; ++i) {
+        const u64 n = static_cast<u64>(span_of(tiles_of(length(i)), pieces)) * units;
         if (first < at + n) {
-          plan.b = b;
+          plan.b = i;
           break;
         }
         at += n;
@@ -225,20 +247,23 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 3 : 2) paged_attention_ke
       plan.pieces = pieces;
     }
     __syncthreads();
-  }
-
-  unsigned long long x = plan.first;
-  const unsigned long long last = x + plan.q + (blockIdx.x < plan.r ? 1 : 0);
-  int b = plan.b, u, tile;
-  {
+    x = plan.first;
+    last = x + plan.q + (blockIdx.x < plan.r ? 1 : 0);
+    b = plan.b;
     const int span = span_of(tiles_of(length(b)), plan.pieces);
     u = static_cast<int>(quotient(x - plan.at, span));
     tile = static_cast<int>(x - plan.at - static_cast<unsigned long long>(u) * span);
   }
   while (x < last && b < c.seqs) {
-    const int len = length(b), tiles = tiles_of(len), span = span_of(tiles, plan.pieces);
-    const int stop = static_cast<int>(min(static_cast<unsigned long long>(span), tile + (last - x)));
-    const int tile_end = min(tiles, stop);
+    const int len = length(b), tiles = tiles_of(len);
+    int stop, tile_end;
+    if (kCluster) {  // the CTA's share of the unit (none: a part of no weight)
+      tile = rank * tiles / cs;
+      stop = tile_end = (rank + 1) * tiles / cs;
+    } else {
+      stop = static_cast<int>(min(static_cast<unsigned long long>(span_of(tiles, plan.pieces)), tile + (last - x)));
+      tile_end = min(tiles, stop);
+    }
     auto next_unit = [&]() {
       x += stop - tile;
       tile = 0;
@@ -247,7 +272,7 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 3 : 2) paged_attention_ke
         ++b;
       }
     };
-    if (tile >= tile_end) {  // none of its tiles are in the range
+    if (!kCluster && tile >= tile_end) {  // none of its tiles are in the range
       next_unit();
       continue;
     }
@@ -362,7 +387,7 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 3 : 2) paged_attention_ke
       }
     };
 
-    look(tile);
+    if (!kCluster || tile < tile_end) look(tile);
     // Q: head g of each 8, dimensions 32 i + 8 t .. (on its way beside the page numbers)
     uint4 q[kNt][kKc];
 #pragma unroll
@@ -373,9 +398,11 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 3 : 2) paged_attention_ke
         q[n][i] = make_uint4(0u, 0u, 0u, 0u);
         if (h < heads) q[n][i] = *reinterpret_cast<const uint4*>(a.q + b * a.ldq + static_cast<long long>(h0 + h) * kDh + 32 * i + 8 * t);
       }
-    load_k(tile);
-    load_v(tile);
-    look(tile + 1);
+    if (!kCluster || tile < tile_end) {
+      load_k(tile);
+      load_v(tile);
+      look(tile + 1);
+    }
     __syncwarp();
 #pragma unroll
     for (int n = 0; n < kNt; ++n)
@@ -545,6 +572,39 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 3 : 2) paged_attention_ke
         done(h, d, m, sum, v);
       }
     };
+    if (kCluster) {  // the CTAs' parts to the first of them, and their sum there
+      constexpr int kPart = kHeads * kDh + 2 * kHeads;
+      float* const all = so + kWarps * kHeads * kDh;  // [cs][kPart]
+      cluster_wait();
+      add_warps([&](int h, int d, float m, float sum, float4 v) {
+        const uint32_t at = mapa_shared(smem_u32(all + rank * kPart), 0);
+        st_shared_cluster_v4(at + 4 * (h * kDh + d), v);
+        if (d == 0) {
+          st_shared_cluster_u32(at + 4 * (kHeads * kDh + h), __float_as_uint(m));
+          st_shared_cluster_u32(at + 4 * (kHeads * kDh + kHeads + h), __float_as_uint(sum));
+        }
+      });
+      cluster_sync();
+      if (rank != 0) return;
+      for (int i = tid; i < heads * (kDh / 4); i += kThreads) {
+        const int h = i / (kDh / 4), d = (i % (kDh / 4)) * 4;
+        float m = -INFINITY, sum = 0.0f;
+        for (int r = 0; r < cs; ++r) m = fmaxf(m, all[r * kPart + kHeads * kDh + h]);
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int r = 0; r < cs; ++r) {
+          const float* const part = all + r * kPart;
+          const float mr = part[kHeads * kDh + h], f = mr == -INFINITY ? 0.0f : exp2_fast(mr - m);
+          const float4 z = *reinterpret_cast<const float4*>(part + h * kDh + d);
+          sum += part[kHeads * kDh + kHeads + h] * f;
+          v.x += z.x * f;
+          v.y += z.y * f;
+          v.z += z.z * f;
+          v.w += z.w * f;
+        }
+        write_out<kBf16>(a, b, h0 + h, d, m, sum, v);
+      }
+      return;
+    }
     if (tile == 0 && tile_end == tiles) {
       add_warps([&](int h, int d, float m, float sum, float4 v) { write_out<kBf16>(a, b, h0 + h, d, m, sum, v); });
     } else {
@@ -680,11 +740,63 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const PagedAttnAr
   write_out<kBf16>(a, unit.x, h0 + h, d, m, sum, v);
 }
 
+template <int kDh, int kNt>
+constexpr size_t cluster_smem(int cs) {
+  return (static_cast<size_t>(kWarps + cs) * 8 * kNt * kDh + static_cast<size_t>(cs) * 2 * 8 * kNt) * sizeof(float);
+}
+
+struct ClusterLaunch {
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[2];
+  ClusterLaunch(int units, int cs, size_t smem, cudaStream_t stream) {
+    cfg.gridDim = dim3(static_cast<unsigned>(units * cs));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = static_cast<unsigned>(cs);
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+  }
+};
+
+// Clusters of cs CTAs that the GPU holds at once (asked once).
+template <bool kBf16, int kDh, int kNt, bool kSmallPage>
+int clusters_at_once(int cs) {
+  static std::atomic<int> known[kMaxCluster + 1];  // one more than the number
+  int n = known[cs].load(std::memory_order_relaxed);
+  if (n == 0) {
+    static SmemLimit limit;
+    auto* kernel = paged_attention_kernel<kBf16, kDh, kNt, kSmallPage, true>;
+    ClusterLaunch l(1, cs, cluster_smem<kDh, kNt>(cs), nullptr);
+    l.cfg.numAttrs = 1;
+    if (limit.allow(kernel, cluster_smem<kDh, kNt>(kMaxCluster)) != cudaSuccess || cudaOccupancyMaxActiveClusters(&n, kernel, &l.cfg) != cudaSuccess) {
+      cudaGetLastError();
+      n = 0;
+    }
+    known[cs].store(++n, std::memory_order_relaxed);
+  }
+  return n - 1;
+}
+
+// A cluster of cs CTAs for each unit.
+template <bool kBf16, int kDh, int kNt, bool kSmallPage>
+cudaError_t launch_clusters(const PagedAttnArgs& a, int units, int cs, cudaStream_t stream, unsigned int* launches) {
+  const ClusterLaunch l(units, cs, cluster_smem<kDh, kNt>(cs), stream);
+  const cudaError_t e = cudaLaunchKernelEx(&l.cfg, paged_attention_kernel<kBf16, kDh, kNt, kSmallPage, true>, a);
+  if (e == cudaSuccess) ++*launches;
+  return e;
+}
+
 template <bool kBf16, int kDh, int kNt, bool kSmallPage>
 cudaError_t launch(const PagedAttnArgs& a, cudaStream_t stream, unsigned int* launches) {
   constexpr size_t smem = static_cast<size_t>(kWarps) * 8 * kNt * kDh * sizeof(float);
   static SmemLimit limit;
-  auto* kernel = paged_attention_kernel<kBf16, kDh, kNt, kSmallPage>;
+  auto* kernel = paged_attention_kernel<kBf16, kDh, kNt, kSmallPage, false>;
   const cudaError_t le = limit.allow(kernel, smem);
   if (le != cudaSuccess) return le;
   // CTAs for every tile that the table has room for, at most a wave
@@ -693,12 +805,21 @@ cudaError_t launch(const PagedAttnArgs& a, cudaStream_t stream, unsigned int* la
   constexpr int kTile = 16 * (128 / kDh) * kWarps;
   const long long room = std::max(1ll, ((static_cast<long long>(a.kv.table_cols) << a.kv.page_log2) + kTile - 1) / kTile);
   const int wave = std::min(kMaxGrid, num_sms() * (kNt == 1 ? 3 : 2));
+  // A cluster for each unit, if all have room at once (an eighth is left over: behind another kernel's last
+  // CTAs 144 clusters of 3 took 23 us, of 2 17.7) and none of its CTAs has so many tiles more than equal ranges give
+  // it, of sequences half as long as the table, that the second kernel costs less. us, with it and without: one
+  // sequence of 704 x 40 heads 6.2, 9.3, of 2048 x 8 6.5, 9.0, of 4096 x 8 10.7 both; 16 of up to 768 x 8 10.3, 13.8.
+  if (units <= wave) {
+    const bool spread = units * room <= num_sms();  // a tile each (256 x 32 heads 3.9, of two 4.8; 4 of 512 x 8 5.5, 4.9)
+    int cs = static_cast<int>(std::min<long long>(kMaxCluster, spread ? room : (room + kMinTiles - 1) / kMinTiles));
+    while (cs > 1 && units * 8 > clusters_at_once<kBf16, kDh, kNt, kSmallPage>(cs) * 7) --cs;
+    if (units <= clusters_at_once<kBf16, kDh, kNt, kSmallPage>(cs) && (room + cs - 1) / cs <= units * room / (2 * wave) + kJoinTiles)
+      return launch_clusters<kBf16, kDh, kNt, kSmallPage>(a, static_cast<int>(units), cs, stream, launches);
+  }
   const int grid = room >= wave || units >= wave ? wave : static_cast<int>(std::min<long long>(wave, units * room));
   cudaError_t e = launch_pdl(kernel, dim3(static_cast<unsigned>(grid)), dim3(kThreads), smem, stream, a);
   if (e != cudaSuccess) return e;
   ++*launches;
-  // no unit can have more than one piece: nothing to join
-  if (room <= kMinTiles && units <= grid) return cudaSuccess;
   const unsigned heads = static_cast<unsigned>(std::min(group, 8 * kNt));
   e = launch_pdl(join_kernel<kBf16, kDh, kNt>, dim3(static_cast<unsigned>(grid), heads), dim3(32 * kJoinWarps), 0, stream,
                  a);

@@ -124,6 +124,17 @@ def test_long_and_many(p4q, dev, n, longest, H, Hkv, dh, page, dt):
     check(c, *run(p4q, dev, c))
 
 
+@pytest.mark.parametrize("H,Hkv", [(40, 40), (32, 8), (24, 2), (8, 1)])
+@pytest.mark.parametrize("longest", [1, 63, 65, 129, 250, 500, 704, 1100, 2300])
+def test_few_sequences(p4q, dev, H, Hkv, longest):
+    """One to a few sequences, as long as the table and much shorter, of each number of CTAs per key/value head."""
+    for lens, dh, page, dt in (([longest], 128, 16, "fp16"), ([longest], 64, 8, "bf16"), ([longest, 0, 1], 128, 64, "bf16"),
+                               ([longest, longest // 2, longest // 9, 66, 0], 64, 16, "fp16"),
+                               ([longest // 3] * 9 + [longest], 128, 16, "fp16")):
+        c = make(dev, [min(n, longest) for n in lens], H, Hkv, dh, page, dt, seed=longest)
+        check(c, *run(p4q, dev, c))
+
+
 @pytest.mark.parametrize("qscale,scale", [(30.0, None), (0.01, None), (1.0, 0.7), (1.0, -0.3), (1.0, 0.0)])
 def test_peaked_flat_and_scaled(p4q, dev, qscale, scale):
     """One position dominates (its place varies), equal weights, other scales."""
