@@ -56,7 +56,7 @@ constexpr int kMaxGrid = 640;    // CTAs of a launch at most (partial results of
 constexpr int kMinTiles = 2;     // tiles per CTA at least, of one unit
 constexpr int kUnitCost = 2;     // what a unit costs beside its tiles, in tiles
 constexpr int kMaxCluster = 8;   // CTAs that share a unit as a cluster
-constexpr int kJoinTiles = 6;    // what the second kernel costs, in tiles of a CTA
+constexpr int kJoinTiles = 8;    // what the second kernel costs, in tiles of a CTA
 constexpr long long kMaxLen = 1ll << 30;  // positions (places of a sequence are counted in 32 bits)
 constexpr float kShift = 7.0f;   // p = 2^(score - reference + 7): small p keep their bits in fp16
 constexpr float kMove = 8.0f;    // a reference moves when a score exceeds it by 2^8
@@ -807,13 +807,15 @@ cudaError_t launch(const PagedAttnArgs& a, cudaStream_t stream, unsigned int* la
   const int wave = std::min(kMaxGrid, num_sms() * (kNt == 1 ? 3 : 2));
   // A cluster for each unit, if all have room at once (an eighth is left over: behind another kernel's last
   // CTAs 144 clusters of 3 took 23 us, of 2 17.7) and none of its CTAs has so many tiles more than equal ranges give
-  // it, of sequences half as long as the table, that the second kernel costs less. us, with it and without: one
-  // sequence of 704 x 40 heads 6.2, 9.3, of 2048 x 8 6.5, 9.0, of 4096 x 8 10.7 both; 16 of up to 768 x 8 10.3, 13.8.
-  if (units <= wave) {
+  // it, of sequences a third as long as the table, that the second kernel costs less. us, with it and without: one
+  // sequence of 704 x 40 heads 6.2, 9.2, of 2048 x 8 6.5, 9.0, of 4096 x 8 11.0, 10.7, half as long as the table 4.1,
+  // 7.9; 16 of up to 768 x 8 10.3, 13.7, 12 of up to 768 x 32 (12 tiles) 21.2, 19.6. A CTA for each of up to twice as many units of few tiles: 25 of 128 x 32
+  // 14.2, 15.9, of 256 22.0, 23.5 (of five waves: 100 of 200 x 32 73, 66).
+  if (units <= wave || (units <= 2 * wave && room <= 2 * kMinTiles)) {
     const bool spread = units * room <= num_sms();  // a tile each (256 x 32 heads 3.9, of two 4.8; 4 of 512 x 8 5.5, 4.9)
     int cs = static_cast<int>(std::min<long long>(kMaxCluster, spread ? room : (room + kMinTiles - 1) / kMinTiles));
     while (cs > 1 && units * 8 > clusters_at_once<kBf16, kDh, kNt, kSmallPage>(cs) * 7) --cs;
-    if (units <= clusters_at_once<kBf16, kDh, kNt, kSmallPage>(cs) && (room + cs - 1) / cs <= units * room / (2 * wave) + kJoinTiles)
+    if ((room + cs - 1) / cs <= units * room / (3 * wave) + kJoinTiles)
       return launch_clusters<kBf16, kDh, kNt, kSmallPage>(a, static_cast<int>(units), cs, stream, launches);
   }
   const int grid = room >= wave || units >= wave ? wave : static_cast<int>(std::min<long long>(wave, units * room));
