@@ -31,10 +31,10 @@
 // warp walks its tokens.
 //
 // Bound: phases between barriers of the CTA and the cluster, at two CTAs of 512
-// threads per SM, and 31 (no cut) to 130 instructions per logit; HBM is at 2 TB/s at
-// most. us: 256 x 131072 fp32 without cuts 67, top-k 76, with top-p 77, largest logit only
-// 38, top-p of thousands of tokens 189; 64 x 32000 fp16 7.9, 9.5, 9.7, 3.9, 22; one row
-// 5.7, 7.8, 8.1, 2.9, 13. (The loops over a thread's logits are not unrolled: 150 KB of
+// threads per SM, and 24 (a small top-k) to 110 instructions per logit; HBM is at 2 TB/s at
+// most. us: 256 x 131072 fp32 without cuts 67, top-k 77, with top-p 78, largest logit only
+// 38, top-p of thousands of tokens 189; 64 x 32000 fp16 8.1, 9.9, 10.0, 4.0, 22; one row
+// 5.7, 8.2, 8.4, 2.9, 13. (The loops over a thread's logits are not unrolled: 150 KB of
 // code instead of 217, and no slower.)
 #include <climits>
 #include <cuda_runtime.h>
