@@ -21,8 +21,11 @@
 //      into the second one's operand.
 // The reference maximum of the softmax moves only when a score exceeds it by
 // 2^8 (p stays below 2^15), so that most tiles need no exchange between lanes.
-// p goes into the product as the sum of two 16-bit values (rounded, remainder):
-// rounded once it would add as much error as the output's own rounding does.
+// p goes into the product as the sum of 16-bit values, each the rounded remainder of
+// those before it: two in fp16 (22 bits), three in bf16 (24 bits, all of p). Rounded
+// once it would add as much error as the output's own rounding does. (Two of bf16: 0.24 %
+// of the outputs of 128 sequences of up to 8190 lay a rounding away from fp32 arithmetic's,
+// of three 0.10 %; 170.9 and 171.6 us.)
 // The new keys' loads are issued as soon as the old ones are in the first
 // product, and the values' behind the second: 8 KB in flight per warp, twelve
 // warps per SM. (Sixteen at 128 registers spilled: 757 us for 64 sequences of
@@ -58,7 +61,9 @@ constexpr int kUnitCost = 2;     // what a unit costs beside its tiles, in tiles
 constexpr int kMaxCluster = 8;   // CTAs that share a unit as a cluster
 constexpr int kJoinTiles = 8;    // what the second kernel costs, in tiles of a CTA
 constexpr long long kMaxLen = 1ll << 30;  // positions (places of a sequence are counted in 32 bits)
-constexpr float kShift = 7.0f;   // p = 2^(score - reference + 7): small p keep their bits in fp16
+// p = 2^(score - reference + kShift): small p keep their bits in fp16 (bf16 has the range of fp32)
+template <bool kBf16>
+constexpr float kShift = kBf16 ? 0.0f : 7.0f;
 constexpr float kMove = 8.0f;    // a reference moves when a score exceeds it by 2^8
 
 // Workspace: for each CTA the unit that begins in it and goes on in others
@@ -108,6 +113,21 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return y;
 }
 
+// p of two heads as `kParts` pairs of 16-bit values (p0 in the low halves) whose sums they are.
+template <bool kBf16>
+constexpr int kParts = kBf16 ? 3 : 2;
+
+template <bool kBf16>
+__device__ __forceinline__ void split2(float p0, float p1, uint32_t (&w)[kParts<kBf16>]) {
+#pragma unroll
+  for (int i = 0; i < kParts<kBf16>; ++i) {
+    w[i] = pack2<kBf16>(p0, p1);
+    const float2 back = unpack2<kBf16>(w[i]);
+    p0 -= back.x;
+    p1 -= back.y;
+  }
+}
+
 // Output of head h (dimensions d .. d + 3) and its logarithm of the sum, from
 // the reference maximum, the sum and the values against it.
 template <bool kBf16>
@@ -118,7 +138,7 @@ __device__ __forceinline__ void write_out(const PagedAttnArgs& a, int b, int h, 
   w.y = pack2<kBf16>(v.z * inv, v.w * inv);
   *reinterpret_cast<uint2*>(a.o + b * a.ldo + static_cast<long long>(h) * a.kv.dh + d) = w;
   if (d == 0 && a.lse)
-    a.lse[static_cast<long long>(b) * a.H + h] = sum == 0.0f ? -INFINITY : (m - kShift) * 0.6931471805599453f + logf(sum);
+    a.lse[static_cast<long long>(b) * a.H + h] = sum == 0.0f ? -INFINITY : (m - kShift<kBf16>) * 0.6931471805599453f + logf(sum);
 }
 
 // How the tiles of all units in one row are dealt: CTA c has q of them from
@@ -487,10 +507,10 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 3 : 2) paged_attention_ke
 #pragma unroll
       for (int n = 0; n < kNt; ++n)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) from[n][e] = ref[n][e] == -INFINITY ? 0.0f : ref[n][e] - kShift;
+        for (int e = 0; e < 2; ++e) from[n][e] = ref[n][e] == -INFINITY ? 0.0f : ref[n][e] - kShift<kBf16>;
 #pragma unroll
       for (int r = 0; r < kRep; ++r) {
-        uint32_t bh[kNt][2], bl[kNt][2];
+        uint32_t pw[kNt][kParts<kBf16>][2];
 #pragma unroll
         for (int n = 0; n < kNt; ++n)
 #pragma unroll
@@ -498,10 +518,10 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 3 : 2) paged_attention_ke
             const float p0 = exp2_fast(s[r][n][2 * e] - from[n][0]), p1 = exp2_fast(s[r][n][2 * e + 1] - from[n][1]);
             l[n][0] += p0;
             l[n][1] += p1;
-            const uint32_t hi = pack2<kBf16>(p0, p1);
-            const float2 back = unpack2<kBf16>(hi);
-            bh[n][e] = transpose8x8(hi);
-            bl[n][e] = transpose8x8(pack2<kBf16>(p0 - back.x, p1 - back.y));
+            uint32_t w[kParts<kBf16>];
+            split2<kBf16>(p0, p1, w);
+#pragma unroll
+            for (int i = 0; i < kParts<kBf16>; ++i) pw[n][i][e] = transpose8x8(w[i]);
           }
 #pragma unroll
         for (int hh = 0; hh < kVc; ++hh) {
@@ -513,10 +533,9 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 3 : 2) paged_attention_ke
             const uint32_t a0 = __byte_perm(w0[j], w1[j], 0x5410), a1 = __byte_perm(w0[j], w1[j], 0x7632);
             const uint32_t a2 = __byte_perm(w2[j], w3[j], 0x5410), a3 = __byte_perm(w2[j], w3[j], 0x7632);
 #pragma unroll
-            for (int n = 0; n < kNt; ++n) {
-              mma16816<kBf16>(o[n][hh][j], a0, a1, a2, a3, bh[n][0], bh[n][1]);
-              mma16816<kBf16>(o[n][hh][j], a0, a1, a2, a3, bl[n][0], bl[n][1]);
-            }
+            for (int n = 0; n < kNt; ++n)
+#pragma unroll
+              for (int i = 0; i < kParts<kBf16>; ++i) mma16816<kBf16>(o[n][hh][j], a0, a1, a2, a3, pw[n][i][0], pw[n][i][1]);
           }
         }
       }

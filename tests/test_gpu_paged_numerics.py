@@ -1,0 +1,84 @@
+"""What the paged attention's numbers hold beyond the general bounds: the softmax
+weights keep the precision of fp32 in the product with the values."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"fp16": torch.float16, "bf16": torch.bfloat16}
+
+
+def _rounded_twice(w, dtype):
+    """w (fp64) as the sum of two values of dtype, each rounded to nearest."""
+    hi = w.to(dtype).double()
+    return hi + (w - hi).to(dtype).double()
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("page", [4, 16])
+@pytest.mark.parametrize("H,Hkv,dh", [(2, 2, 128), (8, 1, 128), (2, 1, 64), (16, 1, 64)])
+def test_weights_keep_24_bits(p4q, dev, dt, page, H, Hkv, dh):
+    """Scores are chosen so that their weights are the furthest from two values of
+    bf16, half of them above and half below, and the values so that the sum is all but 0 in
+    64 bits: what is left is the weights' error.
+
+    Blocks of 16 positions begin with a score of 0, so that every warp's weights are the
+    exponentials times a power of two. The scores are single products and exact. Error of a
+    weight, relative: exponent's product and scale 3 * 2^-24 * 1.45, exponent's difference
+    2^-22 (its range is below 8), both times ln 2, and the exponential 2^-22: below 2^-21. Products with v
+    are exact in fp32 (of p's parts); a sum of 17 addends in each of three products per block is
+    off by 17 * 2^-23 of its largest partial sum, which is below 2 p v as signs alternate:
+    four blocks, three products, divided by the weights' sum L (> 40): 408 * 2^-23 / L vmax.
+    Output: rounded once, u |o| + 2^-25 for an fp16 value below its normal range. Weights of 16
+    bits are off by 2^-18 and more, all in one direction."""
+    dtype, u = TYPES[dt], {"fp16": 2.0 ** -11, "bf16": 2.0 ** -8}[dt]
+    s = torch.arange(-256, -64, dtype=torch.float64) / 256  # -1 .. -1/4 in steps that bf16 and fp16 hold
+    s = torch.cat((s, torch.arange(-127, -16, dtype=torch.float64) / 512))
+    s = s[s == s.to(torch.bfloat16).double()]
+    w = torch.exp(s)
+    off = w - _rounded_twice(w, torch.bfloat16)
+    order = torch.argsort(off)
+    low, high = order[:30], order.flip(0)[:30]
+    assert float(off[low].mean()) < -2.0 ** -20 and float(off[high].mean()) > 2.0 ** -20
+    # by weight, so that neighbours of both signs all but cancel
+    low, high = low[torch.argsort(w[low])], high[torch.argsort(w[high])]
+    tested = torch.stack((high, low), 1).reshape(-1)
+    score = torch.zeros((64,), dtype=torch.float64)
+    value = torch.zeros((64,), dtype=torch.float64)
+    at = torch.tensor([j for j in range(64) if j % 16])
+    score[at] = s[tested]
+    value[at] = torch.tensor([1.0, -1.0], dtype=torch.float64).repeat(30)
+    weight = torch.exp(score)
+    for j in (0, 16, 32, 48):  # the rest of the sum, rounded and again what is left
+        value[j] = (-(weight * value).sum()).to(dtype).double()
+    scale_v = (1.0 + torch.arange(dh, dtype=torch.float64) / 128)  # exact products of few bits
+    scale_v = (scale_v * 8).round() / 8
+    v = (value[:, None] * scale_v).to(dtype)
+    k = torch.zeros((64, dh), dtype=dtype)
+    k[:, 1:] = torch.randn((64, dh - 1), generator=torch.Generator().manual_seed(1)).to(dtype)
+    k[:, 0] = score.to(dtype)
+    assert torch.equal(k[:, 0].double(), score)
+    pages = 64 // page
+    table = torch.randperm(pages, generator=torch.Generator().manual_seed(2))
+    kc, vc = (torch.zeros((pages, page, Hkv, dh), dtype=dtype) for _ in range(2))
+    kc[table] = k.view(pages, page, 1, dh).expand(-1, -1, Hkv, -1)
+    vc[table] = v.view(pages, page, 1, dh).expand(-1, -1, Hkv, -1)
+    q = torch.zeros((1, H * dh), dtype=dtype)
+    q[:, ::dh] = 1.0
+    o = torch.empty((1, H * dh), dtype=dtype, device=dev)
+    lse = torch.empty((1, H), device=dev)
+    p4q.p4q_paged_attention(q.to(dev), kc.to(dev), vc.to(dev), table.to(torch.int32)[None].to(dev),
+                            torch.tensor([64], dtype=torch.int32, device=dev), o, p4q.paged_attention_workspace(dev),
+                            scale=1.0, lse=lse)
+    torch.cuda.synchronize()
+    assert p4q.p4q_device_status() == 0
+    L = float(weight.sum())
+    want = (weight[:, None] * v.double()).sum(0) / L
+    vmax = v.double().abs().amax(0)
+    size = (weight[:, None] * v.double().abs()).sum(0) / L
+    bound = u * want.abs() + (2.0 ** -25 if dt == "fp16" else 0.0) + 2.0 ** -21 * size + 408 * 2.0 ** -23 / L * vmax
+    err = (o.cpu().double().view(H, dh) - want).abs()
+    assert bool((err <= bound).all()), f"largest {float((err / bound).max()):.2f} of the bound, {float(err.max()):.3g}"
+    assert abs(float(lse.cpu().double()[0, 0]) - math.log(L)) <= 2.0 ** -20
