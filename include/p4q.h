@@ -559,9 +559,11 @@ p4q_status p4q_rope_append(const uint16_t* q, int ldq, const uint16_t* k, int ld
  * with key/value head h / (H / Hkv), and lse[b, h] = ln sum_j exp(scale q . k_j).
  * A sequence with lens[b] <= 0 has o = 0 and lse = -inf. Positions from lens[b]
  * on do not count, whatever lies there. fp32 products, softmax and sums; the weights enter
- * the product with v as the sum of 16-bit values (22 bits with fp16, 24 with bf16); o rounded once. Non-finite q, k and v of
- * counting positions act as in the formula (a score of -inf has no weight; if all have
- * none, o = 0 and lse = -inf).
+ * the product with v as the sum of 16-bit values (22 bits with fp16, 24 with bf16); o rounded once.
+ * Non-finite q, k and v of counting positions act as in the formula: an infinite v_j makes its
+ * dimension of o infinite, NaN beside one of the other sign; a score of -inf has no weight (0,
+ * which makes NaN of an infinite v_j), and if all have none, o = 0 and lse = -inf. Weights below
+ * 2^-126 of the largest may count as 0.
  * A length beyond the page table's columns (or 2^30) is cut to them, and the
  * positions of a page outside the cache count as masked (both P4Q_ERR_INDEX).
  *   q, o  [kv->seqs, ldq / ldo] kv->dtype, H heads of dh (o written)

@@ -20,12 +20,12 @@
 //   P: S^T leaves the first product with positions as rows; movmatrix turns it
 //      into the second one's operand.
 // The reference maximum of the softmax moves only when a score exceeds it by
-// 2^8 (p stays below 2^15), so that most tiles need no exchange between lanes.
-// p goes into the product as the sum of 16-bit values, each the rounded remainder of
-// those before it: two in fp16 (22 bits), three in bf16 (24 bits, all of p). Rounded
-// once it would add as much error as the output's own rounding does. (Two of bf16: 0.24 %
-// of the outputs of 128 sequences of up to 8190 lay a rounding away from fp32 arithmetic's,
-// of three 0.10 %; 170.9 and 171.6 us.)
+// 2^8 (fp16 2^4: p stays below 2^15), so that most tiles need no exchange between lanes.
+// p goes into the product as the sum of 16-bit values: two in fp16 (22 bits), three in
+// bf16 (24 bits, all of p). Rounded once it would add as much error as the output's own
+// rounding does. (Two of bf16: 0.24 % of the outputs of 128 sequences of up to 8190 lay a
+// rounding away from fp32 arithmetic's, of three 0.10 %; 170.9 and 171.6 us.) None of the
+// values of a p > 0 is negative or 0, so that an infinite value in V stays infinite.
 // The new keys' loads are issued as soon as the old ones are in the first
 // product, and the values' behind the second: 8 KB in flight per warp, twelve
 // warps per SM. (Sixteen at 128 registers spilled: 757 us for 64 sequences of
@@ -61,10 +61,12 @@ constexpr int kUnitCost = 2;     // what a unit costs beside its tiles, in tiles
 constexpr int kMaxCluster = 8;   // CTAs that share a unit as a cluster
 constexpr int kJoinTiles = 8;    // what the second kernel costs, in tiles of a CTA
 constexpr long long kMaxLen = 1ll << 30;  // positions (places of a sequence are counted in 32 bits)
-// p = 2^(score - reference + kShift): small p keep their bits in fp16 (bf16 has the range of fp32)
+// p = 2^(score - reference + kShift), and a reference moves when a score exceeds it by
+// 2^kMove. fp16: p up to 2^15, and small ones keep their bits (bf16 has fp32's range).
 template <bool kBf16>
-constexpr float kShift = kBf16 ? 0.0f : 7.0f;
-constexpr float kMove = 8.0f;    // a reference moves when a score exceeds it by 2^8
+constexpr float kShift = kBf16 ? 0.0f : 11.0f;
+template <bool kBf16>
+constexpr float kMove = kBf16 ? 8.0f : 4.0f;
 
 // Workspace: for each CTA the unit that begins in it and goes on in others
 // (batch index, unit, last CTA; last CTA -1: none), then two partial results per
@@ -113,18 +115,37 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return y;
 }
 
-// p of two heads as `kParts` pairs of 16-bit values (p0 in the low halves) whose sums they are.
+// p of two heads as `kParts` pairs of 16-bit values (p0 in the low halves) whose sums
+// they are: cut off towards 0, the last of fp16 rounded. Where p > 0 all of them are: 0 would
+// make NaN of an infinite value in V, and so would values of both signs. The least value
+// instead of 0 adds to p no more than 2^-126 in bf16, and in fp16 2^-23 where p is below
+// 2^-11 of the weight at the reference (2^-34 of that weight).
 template <bool kBf16>
 constexpr int kParts = kBf16 ? 3 : 2;
 
+__device__ __forceinline__ uint32_t cut_bf16x2(float p0, float p1) {
+  return __byte_perm(__float_as_uint(p0), __float_as_uint(p1), 0x7632);
+}
+
 template <bool kBf16>
 __device__ __forceinline__ void split2(float p0, float p1, uint32_t (&w)[kParts<kBf16>]) {
+  const uint32_t top = cut_bf16x2(p0, p1);
+  if constexpr (kBf16) {
+    const uint32_t least = __vminu2(top, 0x00800080u);  // 2^-126, or 0
+    w[0] = top;
 #pragma unroll
-  for (int i = 0; i < kParts<kBf16>; ++i) {
-    w[i] = pack2<kBf16>(p0, p1);
-    const float2 back = unpack2<kBf16>(w[i]);
-    p0 -= back.x;
-    p1 -= back.y;
+    for (int i = 1; i < kParts<kBf16>; ++i) {
+      p0 -= __uint_as_float(__float_as_uint(p0) & 0xFFFF0000u);
+      p1 -= __uint_as_float(__float_as_uint(p1) & 0xFFFF0000u);
+      w[i] = __vmaxu2(cut_bf16x2(p0, p1), least);
+    }
+  } else {
+    const uint32_t least = __vminu2(top, 0x00010001u);  // 2^-24, or 0
+    uint32_t hi;
+    asm("cvt.rz.f16x2.f32 %0, %1, %2;" : "=r"(hi) : "f"(p1), "f"(p0));
+    const float2 back = unpack2<false>(hi);
+    w[0] = __vmaxu2(hi, least);
+    w[1] = __vmaxu2(pack2<false>(p0 - back.x, p1 - back.y), least);
   }
 }
 
@@ -136,6 +157,7 @@ __device__ __forceinline__ void write_out(const PagedAttnArgs& a, int b, int h, 
   uint2 w;
   w.x = pack2<kBf16>(v.x * inv, v.y * inv);
   w.y = pack2<kBf16>(v.z * inv, v.w * inv);
+  if (sum == 0.0f) w = make_uint2(0u, 0u);  // (0 times an infinite value was NaN)
   *reinterpret_cast<uint2*>(a.o + b * a.ldo + static_cast<long long>(h) * a.kv.dh + d) = w;
   if (d == 0 && a.lse)
     a.lse[static_cast<long long>(b) * a.H + h] = sum == 0.0f ? -INFINITY : (m - kShift<kBf16>) * 0.6931471805599453f + logf(sum);
@@ -480,7 +502,7 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 3 : 2) paged_attention_ke
 #pragma unroll
         for (int n = 0; n < kNt; ++n)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) move = move || s[r][n][e] > ref[n][e & 1] + kMove;
+          for (int e = 0; e < 4; ++e) move = move || s[r][n][e] > ref[n][e & 1] + kMove<kBf16>;
       if (__any_sync(0xFFFFFFFFu, move)) {
 #pragma unroll
         for (int n = 0; n < kNt; ++n)
