@@ -805,17 +805,24 @@ struct ClusterLaunch {
   }
 };
 
+// The shared memory that a cluster's CTAs ask for, whatever their number.
+template <bool kBf16, int kDh, int kNt, bool kSmallPage>
+cudaError_t allow_clusters() {
+  static SmemLimit limit;
+  return limit.allow(paged_attention_kernel<kBf16, kDh, kNt, kSmallPage, true>, cluster_smem<kDh, kNt>(kMaxCluster));
+}
+
 // Clusters of cs CTAs that the GPU holds at once (asked once).
 template <bool kBf16, int kDh, int kNt, bool kSmallPage>
 int clusters_at_once(int cs) {
   static std::atomic<int> known[kMaxCluster + 1];  // one more than the number
   int n = known[cs].load(std::memory_order_relaxed);
   if (n == 0) {
-    static SmemLimit limit;
     auto* kernel = paged_attention_kernel<kBf16, kDh, kNt, kSmallPage, true>;
     ClusterLaunch l(1, cs, cluster_smem<kDh, kNt>(cs), nullptr);
     l.cfg.numAttrs = 1;
-    if (limit.allow(kernel, cluster_smem<kDh, kNt>(kMaxCluster)) != cudaSuccess || cudaOccupancyMaxActiveClusters(&n, kernel, &l.cfg) != cudaSuccess) {
+    if (allow_clusters<kBf16, kDh, kNt, kSmallPage>() != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, kernel, &l.cfg) != cudaSuccess) {
       cudaGetLastError();
       n = 0;
     }
@@ -827,8 +834,10 @@ int clusters_at_once(int cs) {
 // A cluster of cs CTAs for each unit.
 template <bool kBf16, int kDh, int kNt, bool kSmallPage>
 cudaError_t launch_clusters(const PagedAttnArgs& a, int units, int cs, cudaStream_t stream, unsigned int* launches) {
+  cudaError_t e = allow_clusters<kBf16, kDh, kNt, kSmallPage>();
+  if (e != cudaSuccess) return e;
   const ClusterLaunch l(units, cs, cluster_smem<kDh, kNt>(cs), stream);
-  const cudaError_t e = cudaLaunchKernelEx(&l.cfg, paged_attention_kernel<kBf16, kDh, kNt, kSmallPage, true>, a);
+  e = cudaLaunchKernelEx(&l.cfg, paged_attention_kernel<kBf16, kDh, kNt, kSmallPage, true>, a);
   if (e == cudaSuccess) ++*launches;
   return e;
 }

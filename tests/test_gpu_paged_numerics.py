@@ -21,7 +21,7 @@ def _rounded_twice(w, dtype):
 
 @pytest.mark.parametrize("dt", ["fp16", "bf16"])
 @pytest.mark.parametrize("page", [4, 16])
-@pytest.mark.parametrize("H,Hkv,dh", [(2, 2, 128), (8, 1, 128), (2, 1, 64), (16, 1, 64)])
+@pytest.mark.parametrize("H,Hkv,dh", [(2, 2, 128), (8, 1, 128), (12, 1, 128), (2, 1, 64), (16, 1, 64)])
 def test_weights_keep_24_bits(p4q, dev, dt, page, H, Hkv, dh):
     """Scores are chosen so that their weights are the furthest from two values of
     bf16, half of them above and half below, and the values so that the sum is all but 0 in
