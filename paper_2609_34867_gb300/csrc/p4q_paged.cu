@@ -41,7 +41,6 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
-#include <atomic>
 
 #include "p4q_device.cuh"
 #include "p4q_elem.cuh"
@@ -812,23 +811,21 @@ cudaError_t allow_clusters() {
   return limit.allow(paged_attention_kernel<kBf16, kDh, kNt, kSmallPage, true>, cluster_smem<kDh, kNt>(kMaxCluster));
 }
 
-// Clusters of cs CTAs that the GPU holds at once (asked once).
+// Clusters of cs CTAs that the GPU holds at once; 0 where it does not say.
 template <bool kBf16, int kDh, int kNt, bool kSmallPage>
 int clusters_at_once(int cs) {
-  static std::atomic<int> known[kMaxCluster + 1];  // one more than the number
-  int n = known[cs].load(std::memory_order_relaxed);
-  if (n == 0) {
-    auto* kernel = paged_attention_kernel<kBf16, kDh, kNt, kSmallPage, true>;
+  static DeviceNumber known[kMaxCluster + 1];
+  int n = 0;
+  const cudaError_t e = known[cs].get(&n, [cs](int* number) {
+    const cudaError_t le = allow_clusters<kBf16, kDh, kNt, kSmallPage>();
+    if (le != cudaSuccess) return le;
     ClusterLaunch l(1, cs, cluster_smem<kDh, kNt>(cs), nullptr);
     l.cfg.numAttrs = 1;
-    if (allow_clusters<kBf16, kDh, kNt, kSmallPage>() != cudaSuccess ||
-        cudaOccupancyMaxActiveClusters(&n, kernel, &l.cfg) != cudaSuccess) {
-      cudaGetLastError();
-      n = 0;
-    }
-    known[cs].store(++n, std::memory_order_relaxed);
-  }
-  return n - 1;
+    return cudaOccupancyMaxActiveClusters(number, paged_attention_kernel<kBf16, kDh, kNt, kSmallPage, true>, &l.cfg);
+  });
+  if (e == cudaSuccess) return n;
+  cudaGetLastError();
+  return 0;
 }
 
 // A cluster of cs CTAs for each unit.

@@ -1,5 +1,6 @@
-// Dynamic shared memory past 48 KB has to be allowed for a kernel before it is
-// launched with it, on each device.
+// What a launch needs of its device, asked or set once on each: dynamic shared
+// memory past 48 KB has to be allowed for a kernel before it is launched with it,
+// and what fits at once is the device's to say.
 #pragma once
 
 #include <atomic>
@@ -28,6 +29,34 @@ class SmemLimit {
 
  private:
   std::atomic<uint64_t> done_{0};
+};
+
+// A number that the runtime tells about the current device (clusters that fit at
+// once), asked the first time that it is wanted there. A question that failed is
+// asked again the next time.
+class DeviceNumber {
+ public:
+  template <class Ask>  // cudaError_t ask(int* number)
+  cudaError_t get(int* number, Ask&& ask) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const bool kept = dev >= 0 && dev < kDevices;  // further devices: asked on every call
+    if (kept) {
+      const int known = known_[dev].load(std::memory_order_relaxed);
+      if (known > 0) {
+        *number = known - 1;
+        return cudaSuccess;
+      }
+    }
+    e = ask(number);
+    if (e == cudaSuccess && kept) known_[dev].store(*number + 1, std::memory_order_relaxed);
+    return e;
+  }
+
+ private:
+  static constexpr int kDevices = 64;
+  std::atomic<int> known_[kDevices] = {};  // one more than the number; 0: not asked yet
 };
 
 }  // namespace p4q
