@@ -100,10 +100,6 @@ __device__ __forceinline__ uint4 reload16(const uint4* p) {
   return v;
 }
 
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
-
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-
 __device__ __forceinline__ void st_shared_cluster_v4(uint32_t a, float4 v) {
   asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(a), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
@@ -206,7 +202,7 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 3 : 2) paged_attention_ke
   int4* split = static_cast<int4*>(a.ws);
   float* partial = reinterpret_cast<float*>(split + kMaxGrid);
 
-  if (kCluster) cluster_arrive();  // (waited for before the first CTA's shared memory is written)
+  if (kCluster) cluster_begun_arrive();
   pdl_wait();
   pdl_launch_dependents();
 
@@ -615,7 +611,7 @@ __global__ void __launch_bounds__(kThreads, kNt == 1 ? 3 : 2) paged_attention_ke
     if (kCluster) {  // the CTAs' parts to the first of them, and their sum there
       constexpr int kPart = kHeads * kDh + 2 * kHeads;
       float* const all = so + kWarps * kHeads * kDh;  // [cs][kPart]
-      cluster_wait();
+      cluster_begun_wait();
       add_warps([&](int h, int d, float m, float sum, float4 v) {
         const uint32_t at = mapa_shared(smem_u32(all + rank * kPart), 0);
         st_shared_cluster_v4(at + 4 * (h * kDh + d), v);

@@ -149,6 +149,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
     if (lane < cs) st_shared_cluster_u32(mapa_shared(smem_u32(p), lane), v);
   };
 
+  if (cs > 1) cluster_begun_arrive();
   pdl_wait();
   pdl_launch_dependents();
 
@@ -286,6 +287,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
     const uint32_t k = __reduce_max_sync(0xFFFFFFFFu, key_of(mx));
     if (lane == 0) s.red[warp] = k;
     __syncthreads();
+    if (cs > 1) cluster_begun_wait();
     if (warp == 0) {
       const uint32_t all = __reduce_max_sync(0xFFFFFFFFu, s.red[lane & (kWarps - 1)]);
       put32_lanes(&s.max_key[rank], all);
