@@ -346,7 +346,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
   const int room = kCand / cs;
   auto send = [&](const float (&v)[4], int i, const bool (&in)[4]) {
     if (!__any_sync(0xFFFFFFFFu, in[0] || in[1] || in[2] || in[3])) return;
-    if (*reinterpret_cast<volatile uint32_t*>(&s.sent) > static_cast<uint32_t>(room)) return;  // too many already
+    // too many already (by one lane's reading, as other warps count on)
+    if (__shfl_sync(0xFFFFFFFFu, *reinterpret_cast<volatile uint32_t*>(&s.sent), 0) > static_cast<uint32_t>(room)) return;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const uint32_t with = __ballot_sync(0xFFFFFFFFu, in[j]);
