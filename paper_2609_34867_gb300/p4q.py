@@ -7,6 +7,7 @@ no fallback path.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import struct
@@ -134,6 +135,25 @@ def _stream(stream):
             torch.cuda.init()
         return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream.cuda_stream
+
+
+def _empty(shape, dtype, device, stream):
+    """An output of a wrapper whose kernels run on `stream`. Its memory comes from
+    that stream's pool (what was freed on the current stream may still be in use there), and
+    is not handed out again before the current stream, where the caller goes on, has
+    done with it either."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(t.device))
+    return t
+
+
+def _on(stream):
+    """Where a wrapper's workspace is allocated: on the stream that uses it, so that it is not
+    handed out again, when the wrapper drops it, before that use."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
 def _check(status: int, what: str):
@@ -379,7 +399,7 @@ def p4q_cls_saliency(q_cls, k_cls, k, A_cls, stream=None):
 
 def cls_saliency(q_cls, k_cls, k, stream=None):
     """Allocating wrapper of p4q_cls_saliency."""
-    A = torch.empty((q_cls.shape[0], k.shape[1]), dtype=torch.float32, device=k.device)
+    A = _empty((q_cls.shape[0], k.shape[1]), torch.float32, k.device, stream)
     p4q_cls_saliency(q_cls, k_cls, k, A, stream)
     return A
 
@@ -519,8 +539,9 @@ def p4q_paged_attention(q, k_cache, v_cache, table, lens, o, ws, scale=None, lse
 def paged_attention(q, k_cache, v_cache, table, lens, ws=None, scale=None, stream=None):
     """Allocating wrapper of p4q_paged_attention: returns o."""
     if ws is None:
-        ws = paged_attention_workspace(q.device)
-    o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        with _on(stream):
+            ws = paged_attention_workspace(q.device)
+    o = _empty(q.shape, q.dtype, q.device, stream)
     p4q_paged_attention(q, k_cache, v_cache, table, lens, o, ws, scale, None, stream)
     return o
 
@@ -550,8 +571,8 @@ def p4q_sample(logits, u, token, logprob=None, temperature=None, top_k=None, top
 
 def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
     """Allocating wrapper of p4q_sample: returns (token, logprob)."""
-    token = torch.empty((logits.shape[0],), dtype=torch.int32, device=logits.device)
-    logprob = torch.empty((logits.shape[0],), dtype=torch.float32, device=logits.device)
+    token = _empty((logits.shape[0],), torch.int32, logits.device, stream)
+    logprob = _empty((logits.shape[0],), torch.float32, logits.device, stream)
     p4q_sample(logits, u, token, logprob, temperature, top_k, top_p, min_p, stream)
     return token, logprob
 
@@ -560,22 +581,22 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, stre
 def quant_act(X, stream=None):
     """Allocating wrapper of p4q_quant_act: returns (Xq, s_a)."""
     M, K = X.shape
-    Xq = torch.empty((M, K // 2), dtype=torch.uint8, device=X.device)
-    s = torch.empty((M,), dtype=torch.float32, device=X.device)
+    Xq = _empty((M, K // 2), torch.uint8, X.device, stream)
+    s = _empty((M,), torch.float32, X.device, stream)
     p4q_quant_act(X, Xq, s, stream)
     return Xq, s
 
 
 def quant_weight(W, stream=None):
     N, K = W.shape
-    Wq = torch.empty((N, K // 2), dtype=torch.uint8, device=W.device)
-    s = torch.empty((N,), dtype=torch.float32, device=W.device)
+    Wq = _empty((N, K // 2), torch.uint8, W.device, stream)
+    s = _empty((N,), torch.float32, W.device, stream)
     p4q_quant_weight(W, Wq, s, stream)
     return Wq, s
 
 
 def w4a4_linear(Xq, s_a, Wq, s_w, stream=None):
-    Y = torch.empty((Xq.shape[0], Wq.shape[0]), dtype=torch.float16, device=Xq.device)
+    Y = _empty((Xq.shape[0], Wq.shape[0]), torch.float16, Xq.device, stream)
     p4q_w4a4_linear(Xq, s_a, Wq, s_w, Y, stream)
     return Y
 
@@ -602,7 +623,7 @@ def w4a4_gemm_s32_ws(Xq, Wq, ws, stream=None):
     """Allocating wrapper of p4q_w4a4_gemm_s32_ws: returns the int32 accumulators."""
     M, K = Xq.shape[0], Xq.shape[1] * 2
     N = Wq.shape[0]
-    acc = torch.empty((M, N), dtype=torch.int32, device=Xq.device)
+    acc = _empty((M, N), torch.int32, Xq.device, stream)
     wp, wn = (None, 0) if ws is None else (_ptr(ws), ws.numel() * ws.element_size())
     _check(lib().p4q_w4a4_gemm_s32_ws(_ptr(Xq), M, K, _ptr(Wq), N, _ptr(acc), wp, wn, _stream(stream)),
            "p4q_w4a4_gemm_s32_ws")
@@ -618,8 +639,8 @@ def p4q_expand_codes(q, u, sum_u, stream=None):
 
 def expand_codes(q, stream=None):
     """Allocating wrapper of p4q_expand_codes: returns (u, sum_u)."""
-    u = torch.empty((q.shape[0], q.shape[1] * 2), dtype=torch.uint8, device=q.device)
-    s = torch.empty((q.shape[0],), dtype=torch.int32, device=q.device)
+    u = _empty((q.shape[0], q.shape[1] * 2), torch.uint8, q.device, stream)
+    s = _empty((q.shape[0],), torch.int32, q.device, stream)
     p4q_expand_codes(q, u, s, stream)
     return u, s
 
@@ -674,7 +695,7 @@ def p4q_quant_act_expanded_rowmax(Y, blocks, rowmax, Xq, s_a, Xu, sum_xu, stream
 
 
 def w4a4_gemm_s32(Xq, Wq, stream=None):
-    acc = torch.empty((Xq.shape[0], Wq.shape[0]), dtype=torch.int32, device=Xq.device)
+    acc = _empty((Xq.shape[0], Wq.shape[0]), torch.int32, Xq.device, stream)
     p4q_w4a4_gemm_s32(Xq, Wq, acc, stream)
     return acc
 
@@ -690,8 +711,9 @@ def select(V, Q, A_cls, K, ws=None, alpha_permille=300, beta_permille=200, strea
     B, N, d = V.shape
     J = 0 if Q is None else Q.shape[1]
     if ws is None:
-        ws = select_workspace(B, N, d, J, K, V.device, alpha_permille, beta_permille)
-    idx = torch.empty((B, K), dtype=torch.int32, device=V.device)
+        with _on(stream):
+            ws = select_workspace(B, N, d, J, K, V.device, alpha_permille, beta_permille)
+    idx = _empty((B, K), torch.int32, V.device, stream)
     p4q_select(V, Q, A_cls, K, idx, ws, alpha_permille, beta_permille, stream)
     return idx
 
@@ -701,10 +723,11 @@ def select_gather_quant(V, Q, A_cls, text, K, ws=None, alpha_permille=300, beta_
     J = 0 if Q is None else Q.shape[1]
     T = 0 if text is None else text.shape[1]
     if ws is None:
-        ws = select_workspace(B, N, d, J, K, V.device, alpha_permille, beta_permille)
-    idx = torch.empty((B, K), dtype=torch.int32, device=V.device)
-    X = torch.empty((B, K + T, d), dtype=torch.float16, device=V.device)
-    Xq = torch.empty((B * (K + T), d // 2), dtype=torch.uint8, device=V.device)
-    s_a = torch.empty((B * (K + T),), dtype=torch.float32, device=V.device)
+        with _on(stream):
+            ws = select_workspace(B, N, d, J, K, V.device, alpha_permille, beta_permille)
+    idx = _empty((B, K), torch.int32, V.device, stream)
+    X = _empty((B, K + T, d), torch.float16, V.device, stream)
+    Xq = _empty((B * (K + T), d // 2), torch.uint8, V.device, stream)
+    s_a = _empty((B * (K + T),), torch.float32, V.device, stream)
     p4q_select_gather_quant(V, Q, A_cls, text, K, idx, X, Xq, s_a, ws, alpha_permille, beta_permille, stream)
     return idx, X, Xq, s_a
