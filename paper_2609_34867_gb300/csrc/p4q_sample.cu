@@ -333,7 +333,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
   auto weight = [&](float d) { return __float2uint_rn(expf(-d) * 2147483648.0f); };
   // the bin of d = dist(v): rounded to an integer behind 2^23 (the largest logit itself: 0, as in dist)
   constexpr float kBinBase = 8388608.0f;
-  const float bin_scale = inv_t * kBinScale;
+  // (finite, so that differences as small as a tiny T have bins: smaller steps of d then)
+  const float bin_scale = fminf(inv_t * kBinScale, 3.402823466e38f);
   auto d_bin = [&](float v) { return fmaxf(fmaf(mx - v, bin_scale, kBinBase), kBinBase); };
   float cut_x = -INFINITY;  // the last kept token
   int cut_i = INT_MAX;
