@@ -44,3 +44,15 @@ def test_first_call(first, dt):
     """Pages of 16 and of 8, groups of 16 and of 4 heads, dh 128 and 64: eight instances in one process."""
     _fresh([(lens, H, 1, dh, page, dt) for H in (16, 4) for dh in (128, 64) for page in (16, 8)
             for lens in (first, [33], [500, 20])])
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("H,Hkv,dh,page", [(40, 40, 128, 16), (32, 8, 128, 8), (12, 1, 64, 64), (16, 1, 128, 16)])
+@pytest.mark.parametrize("cols", [1, 44, 200, 4000])
+def test_tables_wider_than_the_lengths(p4q, dev, dt, H, Hkv, dh, page, cols):
+    """The table's width decides how a call is split: the same sequences in tables of each width."""
+    from test_gpu_paged_attention import check, make, run
+    for lens in ([704], [1, 0, 65], [300, 704, 12, 500]):
+        need = max((n + page - 1) // page for n in lens)
+        c = make(dev, lens, H, Hkv, dh, page, dt, seed=cols, cols=max(cols, need))
+        check(c, *run(p4q, dev, c))
