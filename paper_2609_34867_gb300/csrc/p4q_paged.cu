@@ -23,21 +23,25 @@
 // 2^8 (fp16 2^4: p stays below 2^15), so that most tiles need no exchange between lanes.
 // p goes into the product as the sum of 16-bit values: two in fp16 (22 bits), three in
 // bf16 (24 bits, all of p). Rounded once it would add as much error as the output's own
-// rounding does. (Two of bf16: 0.24 % of the outputs of 128 sequences of up to 8190 lay a
-// rounding away from fp32 arithmetic's, of three 0.10 %; 170.9 and 171.6 us.) None of the
-// values of a p > 0 is negative or 0, so that an infinite value in V stays infinite.
+// rounding does. Two of bf16 leave 0.24 % of the outputs of 128 sequences of up to 8190 a
+// rounding away from fp32 arithmetic's, three 0.10 %, for 0.4 % of the time (165.8 and 166.4
+// us; 3 - 9 % where instructions are the bound: 12 and 16 heads per key/value head, pages of
+// 1 and 8). None of the values of a p > 0 is negative or 0, so that an
+// infinite value in V stays infinite.
 // The new keys' loads are issued as soon as the old ones are in the first
 // product, and the values' behind the second: 8 KB in flight per warp, twelve
 // warps per SM. (Sixteen at 128 registers spilled: 757 us for 64 sequences of
 // 16384 x 8 heads, 631 this way. Copies into shared memory two tiles ahead left
 // room for eight warps, which their products' and exchanges' latencies bound: 907.)
 //
-// Bound: HBM. 64 x 16384 positions, 32 heads over 8 of 128, bf16 (4.3 GB): 631 us =
-// 6.8 TB/s, the measured copy; 24 sequences of up to 2048 x 40 heads 84 us = 0.92 of
-// it, 128 of up to 8190 (skewed) x 8 170 = 0.96; one of 32011 x 8 28 = 0.69. Short ones
+// Bound: HBM. Times among other calls, on the GPU. 64 x 16384 positions, 32 heads over 8 of
+// 128, bf16, pages of 16 (4.3 GB): 606 - 628 us = 6.8 - 7.1 TB/s, the measured copy (6.78); of
+// 8 the same, of 1 727; of 64 dimensions 314 - 348 (pages of 8 381 - 390); 12 or 16 heads per key/value
+// head, 4 of these, 353 (pages of 8 414: instructions). 24 sequences of up to 2048 x 40 heads 82 - 85 us
+// = 0.92 of the copy, 128 of up to 8190 (skewed) x 8 167 - 171 = 0.96; one of 32011 x 8 28.4 = 0.68. Short ones
 // cost a chain: lengths, page numbers, keys 4.6 us, then the end of a kernel and the second
-// kernel 4, or the cluster's exchange 1.5: one of 704 x 40 6.2 us (by ranges 9.2), of 512 x 8
-// 4.1 (6.9), 10 of 1024 x 8 11.4 (15.8).
+// kernel 4, or the cluster's exchange 1.5: one of 704 x 40 6.2 us (by ranges 9.4), of 512 x 8
+// 3.9 (6.9), 10 of 1024 x 8 11.0 (15.8).
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -850,8 +854,9 @@ cudaError_t launch(const PagedAttnArgs& a, cudaStream_t stream, unsigned int* la
   const int wave = std::min(kMaxGrid, num_sms() * (kNt == 1 ? 3 : 2));
   // A cluster for each unit, if all have room at once (an eighth is left over: behind another kernel's last
   // CTAs 144 clusters of 3 took 23 us, of 2 17.7) and none of its CTAs has so many tiles more than equal ranges give
-  // it, of sequences a third as long as the table, that the second kernel costs less. us, with it and without: one
-  // sequence of 704 x 40 heads 6.2, 9.2, of 2048 x 8 6.5, 9.0, of 4096 x 8 11.0, 10.7, half as long as the table 4.1,
+  // it, of sequences a third as long as the table, that the second kernel costs less. The table's width stands for the
+  // lengths here, which the host does not know: 704 positions x 40 heads take 6.2 us in tables of up to 4096, 9.4 in
+  // wider ones (8 heads 4.7, 8.7). us, with it and without: one sequence of 704 x 40 heads 6.2, 9.4, of 2048 x 8 6.5, 9.0, of 4096 x 8 11.0, 10.7, half as long as the table 4.1,
   // 7.9; 16 of up to 768 x 8 10.3, 13.7, 12 of up to 768 x 32 (12 tiles) 21.2, 19.6. A CTA for each of up to twice as many units of few tiles: 25 of 128 x 32
   // 14.2, 15.9, of 256 22.0, 23.5 (of five waves: 100 of 200 x 32 73, 66).
   if (units <= wave || (units <= 2 * wave && room <= 2 * kMinTiles)) {

@@ -10,9 +10,10 @@
 // a CTA as many tokens as its threads cover with about four items each. Many
 // threads with little in flight each are faster than few with much: 22528 tokens
 // of 40 heads with the rotated key rows kept too (1.63 GB) take 244 us (0.98 of the
-// measured copy) at 40 registers, 308 with four items loaded at once and the
-// angles in registers (98). Stores are marked evict-first (249 without, in the same
-// call): nothing here is read again, and what the next kernel reads is new.
+// measured copy) at 40 registers (8 - 12 bytes of them spilled), 308 with four items
+// loaded at once and the angles in registers (98). Stores are marked evict-first (249
+// without, in the same call); of so many rows of q_out and k_out most have left L2 either
+// way before the next kernel reads them.
 #include <cuda_runtime.h>
 
 #include "p4q_device.cuh"

@@ -24,17 +24,17 @@
 // sorts them and makes the cuts and the draw on that list alone. A top-k of up to 256
 // looks for them with a histogram of the threads' largest logits instead of all
 // (a thread then looks through its own if its largest is in reach: 256 x 131072 fp32
-// 96 us to 77, 64 x 32000 fp16 11.4 to 9.5). What follows is for the rest:
+// 96 us to 78, 64 x 32000 fp16 11.4 to 10.0). What follows is for the rest:
 // The draw: kept weights per CTA (behind a top-p cut they are known from the
 // histogram) and their prefix over the cluster; then the one CTA that contains the
 // drawn number finds the warp (a warp's tokens are consecutive), and that
 // warp walks its tokens.
 //
 // Bound: phases between barriers of the CTA and the cluster, at two CTAs of 512
-// threads per SM, and 24 (a small top-k) to 110 instructions per logit; HBM is at 2 TB/s at
-// most. us: 256 x 131072 fp32 without cuts 67, top-k 77, with top-p 78, largest logit only
-// 38, top-p of thousands of tokens 189; 64 x 32000 fp16 8.1, 9.9, 10.0, 4.0, 22; one row
-// 5.7, 8.2, 8.4, 2.9, 13. (The loops over a thread's logits are not unrolled: 150 KB of
+// threads per SM, and 25 (a small top-k) to 110 instructions per logit; HBM is at 2 TB/s at
+// most. us: 256 x 131072 fp32 without cuts 68, top-k 78, with top-p 78, min-p 65, largest logit only
+// 38, top-p of thousands of tokens 190; 64 x 32000 fp16 8.2, 10.0, 10.1, 11.8, 3.9, 20 - 22; one row
+// 5.7, 8.2, 8.4, 6.9, 2.9, 13.7. (The loops over a thread's logits are not unrolled: 150 KB of
 // code instead of 217, and no slower.)
 #include <climits>
 #include <cuda_runtime.h>
@@ -754,7 +754,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
         key_lo = min(key_lo, s.key_min[r]);
         key_hi = max(key_hi, s.key_max[r]);
       }
-      if (found <= kList && most <= kOwn) {  // every CTA ranks its share of them (all in each: 256 x 131072 210 us, so 189)
+      if (found <= kList && most <= kOwn) {  // every CTA ranks its share of them (all in each: 256 x 131072 210 us, so 190)
         for (uint32_t i = tid; i < found; i += kThreads) {
           int r = 0;
           uint32_t j = i;
