@@ -29,8 +29,9 @@ def test_weights_keep_24_bits(p4q, dev, dt, page, H, Hkv, dh):
 
     Blocks of 16 positions begin with a score of 0, so that every warp's weights are the
     exponentials times a power of two. The scores are single products and exact. Error of a
-    weight, relative: exponent's product and scale 3 * 2^-24 * 1.45, exponent's difference
-    2^-22 (its range is below 8), both times ln 2, and the exponential 2^-22: below 2^-21. Products with v
+    weight, relative: exponent's product and scale 3 * 2^-24 * 1.45, exponent's difference half a
+    place of its range, both times ln 2, and the exponential 2^-22. The range is below 2 in bf16 (2^-24), below
+    16 in fp16 (2^-21), whose weights are 2^11 times as large: below 2^-21 and 2^-20. Products with v
     are exact in fp32 (of p's parts); a sum of 17 addends in each of three products per block is
     off by 17 * 2^-23 of its largest partial sum, which is below 2 p v as signs alternate:
     four blocks, three products, divided by the weights' sum L (> 40): 408 * 2^-23 / L vmax.
@@ -81,7 +82,8 @@ def test_weights_keep_24_bits(p4q, dev, dt, page, H, Hkv, dh):
     want = (weight[:, None] * v.double()).sum(0) / L
     vmax = v.double().abs().amax(0)
     size = (weight[:, None] * v.double().abs()).sum(0) / L
-    bound = u * want.abs() + (2.0 ** -25 if dt == "fp16" else 0.0) + 2.0 ** -21 * size + 408 * 2.0 ** -23 / L * vmax
+    d = {"fp16": 2.0 ** -20, "bf16": 2.0 ** -21}[dt]
+    bound = u * want.abs() + (2.0 ** -25 if dt == "fp16" else 0.0) + d * size + 408 * 2.0 ** -23 / L * vmax
     err = (o.cpu().double().view(H, dh) - want).abs()
     assert bool((err <= bound).all()), f"largest {float((err / bound).max()):.2f} of the bound, {float(err.max()):.3g}"
     assert abs(float(lse.cpu().double()[0, 0]) - math.log(L)) <= 2.0 ** -20
