@@ -572,8 +572,8 @@ p4q_status p4q_rope_append(const uint16_t* q, int ldq, const uint16_t* k, int ld
  *   ws    device workspace of p4q_paged_attention_workspace_bytes() bytes,
  *         16-byte aligned; its contents are scratch. Calls that may overlap on
  *         the GPU (on different streams) need a workspace each.
- * Requires H % Hkv == 0, H <= 65535, |scale| < 2^127, ld % 8 == 0 and >= H * dh,
- * 16-byte aligned rows. kv->seqs == 0 is a no-op. */
+ * Requires H % Hkv == 0, H <= 65535, scale log2 e finite in fp32 (|scale| < 2.358e38),
+ * ld % 8 == 0 and >= H * dh, 16-byte aligned rows. kv->seqs == 0 is a no-op. */
 size_t p4q_paged_attention_workspace_bytes(void);
 p4q_status p4q_paged_attention(const uint16_t* q, int ldq, int H, const p4q_paged_kv* kv, const int32_t* lens,
                                float scale, uint16_t* o, int ldo, float* lse, void* ws, size_t ws_bytes,

@@ -443,8 +443,8 @@ p4q_status p4q_paged_attention(const uint16_t* q, int ldq, int H, const p4q_page
   PagedAttnArgs a;
   p4q_status st = check_paged(kv, kv && kv->seqs > 0, &a.kv);
   if (st != P4Q_OK) return st;
-  // (the kernels hold scale log2 e; neither NaN nor so large that this overflows)
-  if (H < 1 || H % kv->Hkv != 0 || !(fabsf(scale) < 1.70141183e38f)) return P4Q_ERR_INVALID_ARG;
+  // (the kernels hold scale log2 e)
+  if (H < 1 || H % kv->Hkv != 0 || !std::isfinite(scale * 1.4426950408889634f)) return P4Q_ERR_INVALID_ARG;
   if (H > 65535) return P4Q_ERR_UNSUPPORTED_SHAPE;
   if (ldq < H * kv->dh || ldo < H * kv->dh) return P4Q_ERR_INVALID_ARG;
   if (kv->seqs > 0 && (!q || !lens || !o)) return P4Q_ERR_INVALID_ARG;
