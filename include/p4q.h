@@ -579,6 +579,60 @@ p4q_status p4q_paged_attention(const uint16_t* q, int ldq, int H, const p4q_page
                                float scale, uint16_t* o, int ldo, float* lse, void* ws, size_t ws_bytes,
                                p4q_stream_t stream);
 
+/* A paged cache of codes: keys and values as whole numbers of 8 or 4 bits with
+ * one fp32 scale per position and key/value head, a value being code * scale.
+ * Pages, slots and table as in p4q_paged_kv; the dh codes of a head are
+ * contiguous, int8 with bits 8, and with bits 4 two to a byte (two's complement,
+ * the even dimension in the low half), from
+ *   k (v) + page * page_stride + slot * token_stride + h * head_stride   (bytes),
+ * its scale at k_scale (v_scale) + page * scale_page_stride + slot *
+ * scale_token_stride + h * scale_head_stride (elements; a page's scales of one
+ * head side by side, scale_token_stride 1, are read fastest).
+ * Limits: bits 4 or 8; dh 64 or 128; page_size a power of two up to 65536; the
+ * codes' strides multiples of 16 bytes and at least a row's dh * bits / 8, the
+ * scales' positive; k and v 16-byte, the others 4-byte aligned. */
+typedef struct {
+  void* k;               /* [pages] pages of the keys' codes */
+  void* v;               /* [pages] pages of the values' codes */
+  float* k_scale;
+  float* v_scale;
+  const int32_t* table;  /* [seqs, table_ld] page numbers, columns 0 .. table_cols - 1 */
+  int64_t page_stride, token_stride, head_stride;                    /* bytes, alike for k and v */
+  int64_t scale_page_stride, scale_token_stride, scale_head_stride;  /* elements, alike for both */
+  int32_t bits;
+  int32_t pages, page_size, Hkv, dh;
+  int32_t seqs, table_ld, table_cols;
+} p4q_paged_kvq;
+
+/* p4q_rope_append into a cache of codes. The rows that a 16-bit cache would take
+ * (k rotated, v as it is, both of type dtype) are quantised per token and head:
+ *   a = max |x_d|, s = fl32(a / m), m = 127 (bits 8) or 7 (bits 4),
+ *   code_d = round_half_even(fl32(x_d / s))   (all 0 where a = 0),
+ * the quantiser of p4q_quant_act for one head. A row with a value that is not
+ * finite has codes 0 and the scale NaN: it reads back as NaN. Unlike in
+ * p4q_rope_append each product and the sum of the rotation is rounded to fp32
+ * (then once to dtype), so that codes and scales are defined bit for bit.
+ *   k_out, v_out [T, ldko / ldvo]  dtype, or NULL: fl32(code * scale) rounded to dtype,
+ *         the values that attention over the cache will see (for a prompt's own
+ *         attention); each may be its input with its input's pitch
+ * dtype P4Q_F16 or P4Q_BF16. Other arguments and rules as p4q_rope_append. */
+p4q_status p4q_rope_append_quant(const uint16_t* q, int ldq, const uint16_t* k, int ldk, const uint16_t* v, int ldv,
+                                 int T, int H, const float* cos, const float* sin, int max_pos, int rot,
+                                 int interleaved, const int32_t* pos, const int32_t* rot_pos, const int32_t* seq,
+                                 const p4q_paged_kvq* kv, int dtype, uint16_t* q_out, int ldqo, uint16_t* k_out,
+                                 int ldko, uint16_t* v_out, int ldvo, p4q_stream_t stream);
+
+/* p4q_paged_attention over a cache of codes; q and o of type dtype, P4Q_F16 or
+ * P4Q_BF16. Scores are (scale log2 e s_j) (q . c_j) with whole codes c_j; the
+ * weights times the values' scales enter the product with the codes in 22 bits.
+ * fp32 products, softmax and sums; o rounded once. Scales may have any sign; one
+ * of v that is not finite counts as NaN. Finite q of bf16 below 2^-32 of the largest of
+ * their head lose bits (2^-39 of that one at most). Other arguments, rules and the workspace
+ * (p4q_paged_attention_workspace_bytes()) as p4q_paged_attention. */
+p4q_status p4q_paged_attention_quant(const uint16_t* q, int ldq, int H, const p4q_paged_kvq* kv, int dtype,
+                                     const int32_t* lens, float scale, uint16_t* o, int ldo, float* lse, void* ws,
+                                     size_t ws_bytes, p4q_stream_t stream);
+
 /* Draws one token from each row of logits with a given uniform number. With
  * x_max the row's largest logit and T its temperature:
  *   d_i = 0 where x_i = x_max, else (x_max - x_i) * (1 / T)    (fp32)

@@ -252,6 +252,45 @@ p4q_status check_paged(const p4q_paged_kv* kv, bool used, PagedCache* out) {
   return P4Q_OK;
 }
 
+// check_paged for a cache of codes.
+p4q_status check_paged_quant(const p4q_paged_kvq* kv, bool used, int dtype, PagedCodes* out) {
+  if (!kv || kv->pages < 0 || kv->page_size < 1 || kv->Hkv < 1 || kv->dh < 1 || kv->seqs < 0 || kv->table_cols < 0 ||
+      kv->table_ld < kv->table_cols)
+    return P4Q_ERR_INVALID_ARG;
+  if (used && (!kv->k || !kv->v || !kv->k_scale || !kv->v_scale || !kv->table)) return P4Q_ERR_INVALID_ARG;
+  if ((kv->bits != 4 && kv->bits != 8) || (dtype != P4Q_F16 && dtype != P4Q_BF16) || (kv->dh != 64 && kv->dh != 128) ||
+      kv->Hkv > 65535 || kv->page_size > 65536 || (kv->page_size & (kv->page_size - 1)) != 0)
+    return P4Q_ERR_UNSUPPORTED_SHAPE;
+  const int row = kv->dh * kv->bits / 8;
+  if (kv->page_stride < row || kv->token_stride < row || kv->head_stride < row || kv->scale_page_stride < 1 ||
+      kv->scale_token_stride < 1 || kv->scale_head_stride < 1)
+    return P4Q_ERR_INVALID_ARG;
+  if (kv->page_stride % 16 != 0 || kv->token_stride % 16 != 0 || kv->head_stride % 16 != 0 || !aligned16(kv->k) ||
+      !aligned16(kv->v) || !aligned4(kv->k_scale) || !aligned4(kv->v_scale) || !aligned4(kv->table))
+    return P4Q_ERR_MISALIGNED;
+  out->k = static_cast<uint8_t*>(kv->k);
+  out->v = static_cast<uint8_t*>(kv->v);
+  out->k_scale = kv->k_scale;
+  out->v_scale = kv->v_scale;
+  out->table = kv->table;
+  out->page_stride = kv->page_stride;
+  out->token_stride = kv->token_stride;
+  out->head_stride = kv->head_stride;
+  out->scale_page_stride = kv->scale_page_stride;
+  out->scale_token_stride = kv->scale_token_stride;
+  out->scale_head_stride = kv->scale_head_stride;
+  out->bits = kv->bits;
+  out->pages = kv->pages;
+  out->page_log2 = 0;
+  while ((1 << out->page_log2) < kv->page_size) ++out->page_log2;
+  out->Hkv = kv->Hkv;
+  out->dh = kv->dh;
+  out->seqs = kv->seqs;
+  out->table_ld = kv->table_ld;
+  out->table_cols = kv->table_cols;
+  return P4Q_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -298,7 +337,8 @@ p4q_status p4q_device_status(p4q_stream_t stream) {
   const unsigned int g = gemm_read_and_clear_error() | gemm8_read_and_clear_error() | quant_read_and_clear_error() |
                          attn_read_and_clear_error() | fewrows_read_and_clear_error() | peak_read_and_clear_error() |
                          diverse_read_and_clear_error();
-  const unsigned int i = rope_read_and_clear_error() | paged_read_and_clear_error();
+  const unsigned int i = rope_read_and_clear_error() | paged_read_and_clear_error() |
+                         rope_quant_read_and_clear_error() | paged_quant_read_and_clear_error();
   if (cudaGetLastError() != cudaSuccess) return P4Q_ERR_CUDA;
   return g ? P4Q_ERR_TIMEOUT : i ? P4Q_ERR_INDEX : P4Q_OK;
 }
@@ -465,6 +505,87 @@ p4q_status p4q_paged_attention(const uint16_t* q, int ldq, int H, const p4q_page
   a.ws = ws;
   unsigned int launches = 0;
   const cudaError_t e = launch_paged_attention(a, reinterpret_cast<cudaStream_t>(stream), &launches);
+  counted(cudaSuccess, launches);
+  return from_cuda(e);
+}
+
+p4q_status p4q_rope_append_quant(const uint16_t* q, int ldq, const uint16_t* k, int ldk, const uint16_t* v, int ldv,
+                                 int T, int H, const float* cos, const float* sin, int max_pos, int rot,
+                                 int interleaved, const int32_t* pos, const int32_t* rot_pos, const int32_t* seq,
+                                 const p4q_paged_kvq* kv, int dtype, uint16_t* q_out, int ldqo, uint16_t* k_out,
+                                 int ldko, uint16_t* v_out, int ldvo, p4q_stream_t stream) {
+  RopeQuantArgs a;
+  p4q_status st = check_paged_quant(kv, T > 0, dtype, &a.kv);
+  if (st != P4Q_OK) return st;
+  if (T < 0 || H < 1 || max_pos < 1 || rot < 1) return P4Q_ERR_INVALID_ARG;
+  if (rot % 16 != 0 || rot > kv->dh || H > 65535) return P4Q_ERR_UNSUPPORTED_SHAPE;
+  const int nq = H * kv->dh, nk = kv->Hkv * kv->dh;
+  if (ldq < nq || ldk < nk || ldv < nk || ldqo < nq || (k_out && ldko < nk) || (v_out && ldvo < nk))
+    return P4Q_ERR_INVALID_ARG;
+  if (T > 0 && (!q || !k || !v || !cos || !sin || !pos || !q_out)) return P4Q_ERR_INVALID_ARG;
+  if (!seq && T > kv->seqs) return P4Q_ERR_INVALID_ARG;
+  if (ldq % 8 != 0 || ldk % 8 != 0 || ldv % 8 != 0 || ldqo % 8 != 0 || (k_out && ldko % 8 != 0) ||
+      (v_out && ldvo % 8 != 0))
+    return P4Q_ERR_MISALIGNED;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(cos) || !aligned16(sin) || !aligned16(q_out) ||
+      !aligned16(k_out) || !aligned16(v_out) || !aligned4(pos) || !aligned4(rot_pos) || !aligned4(seq))
+    return P4Q_ERR_MISALIGNED;
+  if (T == 0) return P4Q_OK;
+  if ((st = check_device()) != P4Q_OK) return st;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.q_out = q_out;
+  a.k_out = k_out;
+  a.v_out = v_out;
+  a.cos = cos;
+  a.sin = sin;
+  a.pos = pos;
+  a.rot_pos = rot_pos;
+  a.seq = seq;
+  a.ldq = ldq;
+  a.ldk = ldk;
+  a.ldv = ldv;
+  a.ldqo = ldqo;
+  a.ldko = ldko;
+  a.ldvo = ldvo;
+  a.T = T;
+  a.H = H;
+  a.max_pos = max_pos;
+  a.rot = rot;
+  a.interleaved = interleaved != 0;
+  a.bf16 = dtype == P4Q_BF16;
+  return from_cuda(counted(launch_rope_append_quant(a, reinterpret_cast<cudaStream_t>(stream))));
+}
+
+p4q_status p4q_paged_attention_quant(const uint16_t* q, int ldq, int H, const p4q_paged_kvq* kv, int dtype,
+                                     const int32_t* lens, float scale, uint16_t* o, int ldo, float* lse, void* ws,
+                                     size_t ws_bytes, p4q_stream_t stream) {
+  QuantAttnArgs a;
+  p4q_status st = check_paged_quant(kv, kv && kv->seqs > 0, dtype, &a.kv);
+  if (st != P4Q_OK) return st;
+  if (H < 1 || H % kv->Hkv != 0 || !std::isfinite(scale * 1.4426950408889634f)) return P4Q_ERR_INVALID_ARG;
+  if (H > 65535) return P4Q_ERR_UNSUPPORTED_SHAPE;
+  if (ldq < H * kv->dh || ldo < H * kv->dh) return P4Q_ERR_INVALID_ARG;
+  if (kv->seqs > 0 && (!q || !lens || !o)) return P4Q_ERR_INVALID_ARG;
+  if (ldq % 8 != 0 || ldo % 8 != 0 || !aligned16(q) || !aligned16(o) || !aligned4(lens) || !aligned4(lse))
+    return P4Q_ERR_MISALIGNED;
+  if (kv->seqs == 0) return P4Q_OK;
+  if (!ws || ws_bytes < paged_attention_workspace_bytes()) return P4Q_ERR_WORKSPACE_TOO_SMALL;
+  if (!aligned16(ws)) return P4Q_ERR_MISALIGNED;
+  if ((st = check_device()) != P4Q_OK) return st;
+  a.q = q;
+  a.o = o;
+  a.lse = lse;
+  a.lens = lens;
+  a.ldq = ldq;
+  a.ldo = ldo;
+  a.H = H;
+  a.scale = scale;
+  a.ws = ws;
+  a.bf16 = dtype == P4Q_BF16;
+  unsigned int launches = 0;
+  const cudaError_t e = launch_paged_attention_quant(a, reinterpret_cast<cudaStream_t>(stream), &launches);
   counted(cudaSuccess, launches);
   return from_cuda(e);
 }

@@ -52,12 +52,12 @@ __device__ __forceinline__ QRow quant_row(float a) {
 // they differ for some value (a quotient within about 2^-21 of a .5 boundary)
 // is recomputed with exact quotients fl(x / s).
 struct QRowF {
-  float s, ip, im;  // scale a / 7 and the two bracketing reciprocals (0 when a == 0)
+  float s, ip, im;  // scale a / most and the two bracketing reciprocals (0 when a == 0)
 };
 
-__device__ __forceinline__ QRowF quant_row_f(float a) {
+__device__ __forceinline__ QRowF quant_row_f(float a, float most = 7.0f) {
   QRowF r;
-  r.s = __fdiv_rn(a, 7.0f);
+  r.s = __fdiv_rn(a, most);
   const float inv = (a != 0.0f) ? __frcp_rn(r.s) : 0.0f;
   r.ip = __fmul_rn(inv, 1.0f + 0x1p-21f);
   r.im = __fmul_rn(inv, 1.0f - 0x1p-21f);
@@ -76,8 +76,9 @@ __device__ __forceinline__ uint32_t packed4(Codes8 c) { return (c.e & 0x0F0F0F0F
 __device__ __forceinline__ uint32_t expanded_even(Codes8 c) { return (c.e & 0x0F0F0F0Fu) ^ 0x08080808u; }
 __device__ __forceinline__ uint32_t expanded_odd(Codes8 c) { return (c.o & 0x0F0F0F0Fu) ^ 0x08080808u; }
 
-// The magic-biased codes tb of eight fp32 values f (pairs in order).
-__device__ __forceinline__ void quant_values(const float2 (&f)[4], const QRowF& q, uint32_t (&tb)[8]) {
+// The magic-biased codes tb of eight fp32 values f (pairs in order). divide: exact
+// quotients whatever the products say (where 1 / s is near the end of fp32's range).
+__device__ __forceinline__ void quant_values(const float2 (&f)[4], const QRowF& q, uint32_t (&tb)[8], bool divide = false) {
   const float2 ip2 = make_float2(q.ip, q.ip), im2 = make_float2(q.im, q.im);
   const float2 mg = make_float2(12582912.0f, 12582912.0f);
   uint32_t diff = 0;
@@ -89,7 +90,7 @@ __device__ __forceinline__ void quant_values(const float2 (&f)[4], const QRowF& 
     tb[2 * k + 1] = __float_as_uint(tp.y);
     diff |= (tb[2 * k] ^ __float_as_uint(tm.x)) | (tb[2 * k + 1] ^ __float_as_uint(tm.y));
   }
-  if (diff != 0) {
+  if (diff != 0 || divide) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       tb[2 * k] = __float_as_uint(rintf(__fdiv_rn(f[k].x, q.s)) + 12582912.0f);

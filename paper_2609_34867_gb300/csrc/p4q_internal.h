@@ -230,6 +230,53 @@ size_t paged_attention_workspace_bytes();
 cudaError_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t stream, unsigned int* launches);
 unsigned int paged_read_and_clear_error();
 
+// A cache of codes: strides of the codes in bytes, of the scales in elements. Copied from p4q_paged_kvq.
+struct PagedCodes {
+  uint8_t* k = nullptr;
+  uint8_t* v = nullptr;
+  float* k_scale = nullptr;
+  float* v_scale = nullptr;
+  const int32_t* table = nullptr;
+  long long page_stride = 0, token_stride = 0, head_stride = 0;
+  long long scale_page_stride = 0, scale_token_stride = 0, scale_head_stride = 0;
+  int bits = 0, pages = 0, page_log2 = 0, Hkv = 0, dh = 0, seqs = 0, table_ld = 0, table_cols = 0;
+};
+
+struct RopeQuantArgs {
+  PagedCodes kv;
+  const uint16_t* q = nullptr;
+  const uint16_t* k = nullptr;
+  const uint16_t* v = nullptr;
+  uint16_t* q_out = nullptr;
+  uint16_t* k_out = nullptr;  // may be null
+  uint16_t* v_out = nullptr;  // may be null
+  const float* cos = nullptr;
+  const float* sin = nullptr;
+  const int32_t* pos = nullptr;
+  const int32_t* rot_pos = nullptr;  // null: pos
+  const int32_t* seq = nullptr;      // null: the token's own number
+  long long ldq = 0, ldk = 0, ldv = 0, ldqo = 0, ldko = 0, ldvo = 0;
+  int T = 0, H = 0, max_pos = 0, rot = 0;
+  bool interleaved = false, bf16 = false;
+};
+cudaError_t launch_rope_append_quant(const RopeQuantArgs& a, cudaStream_t stream);
+unsigned int rope_quant_read_and_clear_error();
+
+struct QuantAttnArgs {
+  PagedCodes kv;
+  const uint16_t* q = nullptr;
+  uint16_t* o = nullptr;
+  float* lse = nullptr;  // may be null
+  const int32_t* lens = nullptr;
+  long long ldq = 0, ldo = 0;
+  int H = 0;
+  float scale = 0.0f;
+  void* ws = nullptr;  // as for a 16-bit cache
+  bool bf16 = false;
+};
+cudaError_t launch_paged_attention_quant(const QuantAttnArgs& a, cudaStream_t stream, unsigned int* launches);
+unsigned int paged_quant_read_and_clear_error();
+
 struct SampleArgs {
   const void* logits = nullptr;
   long long ld = 0;

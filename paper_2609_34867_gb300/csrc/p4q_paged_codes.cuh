@@ -1,0 +1,435 @@
+// Attention over a paged cache of 8- or 4-bit codes with one scale per position and head: a
+// warp's way through the tiles of a unit.
+//   x_j = (scale log2 e) sk_j (q . c_j),  p_j = 2^(x_j - ref),  o = sum_j (p_j sv_j) c'_j / sum_j p_j
+// with codes c_j, c'_j and scales sk_j, sv_j of key and value: the codes enter the products as
+// they are (whole numbers, exact in fp16) and the scales are factors of the positions' scores
+// and weights, four multiplications per 16 positions and lane.
+//
+// As with 16-bit rows a warp takes 16 positions at a time straight from global memory into the
+// operands of m16n8k16 products, positions the rows of S^T = K Q^T and the inner axis of
+// O^T = V^T P^T. Codes become fp16 in registers: a byte or nibble is the low mantissa bits of
+// 1024 (nibbles in the high half of a byte: of 1024 / 16 = 64, undone by the multiplication that
+// takes the offset away), one logical operation and one packed addition for two codes. Which
+// dimensions an MMA's k-th ones are is free as long as q has the same order, so the nibbles
+// {0, 4}, {1, 5}, {2, 6}, {3, 7} of a word are pairs as they lie.
+//
+// q of fp16 enters the product as it is; q of bf16 times the power of two that brings its head's
+// largest finite value below 2^15, in fp16: exact where |q| >= 2^-32 of that one, and off by
+// less than 2^-39 of it elsewhere. The weights p sv enter theirs as two fp16 values (22 bits)
+// times a power of two per head that moves like the softmax's reference, so scales
+// of any size count against the largest p sv seen and not against fp16's range.
+#pragma once
+
+#include "p4q_paged.cuh"
+
+namespace p4q {
+namespace paged {
+
+// Two codes as fp16 pairs. Bytes 2 half, 2 half + 1 of a word whose sign bits are flipped.
+template <int kHalf>
+__device__ __forceinline__ uint32_t codes8(uint32_t flipped) {
+  const uint32_t v = __byte_perm(flipped, 0x64646464u, kHalf ? 0x4342 : 0x4140);  // 1024 + 128 + c
+  const uint32_t bias = 0x64806480u;
+  const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&v), *reinterpret_cast<const __half2*>(&bias));
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// Nibbles kOdd of both 16-bit halves (0: bits 0 - 3, 1: bits 4 - 7).
+template <int kOdd>
+__device__ __forceinline__ uint32_t codes4(uint32_t w) {
+  __half2 h;
+  if (kOdd) {
+    const uint32_t v = (w & 0x00F000F0u) ^ 0x64806480u, f = 0x2C002C00u, bias = 0xD480D480u;  // 1024 + 16 (8 + c); 1/16; -72
+    h = __hfma2(*reinterpret_cast<const __half2*>(&v), *reinterpret_cast<const __half2*>(&f),
+                *reinterpret_cast<const __half2*>(&bias));
+  } else {
+    const uint32_t v = (w & 0x000F000Fu) ^ 0x64086408u, bias = 0x64086408u;  // 1024 + 8 + c
+    h = __hsub2(*reinterpret_cast<const __half2*>(&v), *reinterpret_cast<const __half2*>(&bias));
+  }
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+template <int kWords>
+__device__ __forceinline__ void load_words(uint32_t (&w)[kWords], const uint8_t* p, int piece_stride) {
+  if constexpr (kWords >= 4) {
+#pragma unroll
+    for (int i = 0; i < kWords; i += 4) {
+      const uint4 v = ldg_stream16(p + (i / 4) * piece_stride);
+      w[i] = v.x;
+      w[i + 1] = v.y;
+      w[i + 2] = v.z;
+      w[i + 3] = v.w;
+    }
+  } else if constexpr (kWords == 2) {
+    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
+  } else {
+    asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(w[0]) : "l"(p));
+  }
+}
+
+template <int kBits, int kDhRows, bool kSmallPage>
+struct Codes {
+  typedef QuantAttnArgs Args;
+  static constexpr bool kOwnOnly = false;
+  static constexpr int kDh = kDhRows;
+  static constexpr int kRep = kSmallPage ? 2 : kDh * kBits == 1024 ? 2 : 4;  // blocks of 16 positions per warp and tile
+  static constexpr int kTile = 16 * kRep * kWarps;
+  static constexpr int kKc = kDh / 32;             // pieces of q per lane, 8 dimensions each
+  static constexpr int kVc = kDh / 64;
+  static constexpr int kKw = kDh * kBits / 128;    // words of a key row per lane
+  static constexpr int kVw = kDh * kBits / 256;    // of a value row
+  static constexpr float kLift = 0.0f;
+  static constexpr float kMove = 8.0f;
+  static __host__ __device__ constexpr int ctas(int nt) { return nt == 1 ? 3 : 2; }
+  static __device__ __forceinline__ bool bf16(const Args& a) { return a.bf16; }
+  static __device__ __forceinline__ int first_own(const Args&, int, int) { return 0; }
+  static __device__ __forceinline__ int first_dim(int hh, int g) { return (kDh / 8) * g + 8 * hh; }
+  // The dimensions of q's piece p that lane t's keys have.
+  static __device__ __forceinline__ int q_dim(int p, int t) {
+    return kBits == 4 ? (kDh / 4) * t + 8 * p : kDh == 128 ? 64 * (p >> 1) + 16 * t + 8 * (p & 1) : 16 * t + 8 * p;
+  }
+
+  template <int kNt>
+  static __device__ __forceinline__ void attend(const Args& a, const Unit& un, int tile, int tile_end,
+                                                uint4 (&sq)[kNt][kKc][32], Part<kNt, kVc>& acc) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const float c2 = a.scale * 1.4426950408889634f;
+    const PagedCodes& c = a.kv;
+    const int len = un.len, heads = un.heads;
+    const uint8_t* kh = c.k + un.hk * c.head_stride + t * (kKw >= 4 ? 16 : 4 * kKw);
+    const uint8_t* vh = c.v + un.hk * c.head_stride + g * (4 * kVw);
+    const float* ksh = c.k_scale + un.hk * c.scale_head_stride;
+    const float* vsh = c.v_scale + un.hk * c.scale_head_stride;
+    const int slots = (1 << c.page_log2) - 1;
+
+    // The page of position j, -1 if it is not to be read.
+    auto page_of = [&](int j) -> int {
+      if (j >= len) return -1;
+      const int page = un.table[j >> c.page_log2];
+      if (static_cast<unsigned int>(page) >= static_cast<unsigned int>(c.pages)) {
+        atomicOr(&g_paged_err, kErrIndex);
+        return -1;
+      }
+      return page;
+    };
+
+    auto& o = acc.o;
+    auto& ref = acc.ref;
+    auto& l = acc.l;
+    uint32_t kr[kRep][2][kKw], vr[kRep][4][kVw];  // rows g, g + 8; 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+    float ks[kRep][2], vs[kRep][2];               // scales of rows g, g + 8
+    constexpr int kLook = kSmallPage ? 6 : 1;     // (pages of 16 and more: a block lies in one)
+    int pg[kRep][kLook];
+    auto look = [&](int tl) {
+#pragma unroll
+      for (int r = 0; r < kRep; ++r) {
+        const int j = tl * kTile + (warp * kRep + r) * 16;
+        pg[r][0] = page_of(kSmallPage ? j + g : j);
+        if constexpr (kSmallPage) {
+          pg[r][1] = page_of(j + g + 8);
+          pg[r][2] = page_of(j + 2 * t);
+          pg[r][3] = page_of(j + 2 * t + 1);
+          pg[r][4] = page_of(j + 2 * t + 8);
+          pg[r][5] = page_of(j + 2 * t + 9);
+        }
+      }
+    };
+    uint32_t live = 0;  // rows g, g + 8 of block r count: bits 2 r, 2 r + 1
+    auto load_k = [&](int tl) {
+      live = 0;
+#pragma unroll
+      for (int r = 0; r < kRep; ++r) {
+        const int j = tl * kTile + (warp * kRep + r) * 16;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int page = pg[r][kSmallPage ? e : 0], row = j + g + 8 * e;
+          if (page >= 0) {
+            if (row < len) live |= 1u << (2 * r + e);
+            const long long slot = row & slots;
+            load_words<kKw>(kr[r][e], kh + page * c.page_stride + slot * c.token_stride, 64);
+            const long long at = page * c.scale_page_stride + slot * c.scale_token_stride;
+            ks[r][e] = ksh[at];
+            vs[r][e] = vsh[at];
+          }
+        }
+      }
+    };
+    auto load_v = [&](int tl) {
+#pragma unroll
+      for (int r = 0; r < kRep; ++r) {
+        const int j = tl * kTile + (warp * kRep + r) * 16;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int page = pg[r][kSmallPage ? 2 + e : 0], row = j + 2 * t + (e & 1) + 8 * (e >> 1);
+          if (page >= 0) load_words<kVw>(vr[r][e], vh + page * c.page_stride + (row & slots) * c.token_stride, 16);
+        }
+      }
+    };
+
+    if (tile < tile_end) look(tile);
+    // q as fp16, and the factor that makes scores in powers of two of its products (heads 2 t, 2 t + 1)
+    float fq[kNt][2];
+    __syncwarp();
+#pragma unroll
+    for (int n = 0; n < kNt; ++n) {
+      const int h = 8 * n + g;
+      uint4 q[kKc];
+#pragma unroll
+      for (int p = 0; p < kKc; ++p) {
+        q[p] = make_uint4(0u, 0u, 0u, 0u);
+        if (h < heads)
+          q[p] = *reinterpret_cast<const uint4*>(a.q + un.b * a.ldq + static_cast<long long>(un.h0 + h) * kDh + q_dim(p, t));
+      }
+      float f = c2;
+      if (a.bf16) {
+        uint32_t most = 0;  // the largest finite |q|
+        auto finite = [](uint32_t w) { return (w & 0x7F80u) == 0x7F80u ? 0u : w & 0x7FFFu; };
+#pragma unroll
+        for (int p = 0; p < kKc; ++p) {
+          const uint32_t w[4] = {q[p].x, q[p].y, q[p].z, q[p].w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) most = max(most, max(finite(w[i] & 0xFFFFu), finite(w[i] >> 16)));
+        }
+        most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
+        most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
+        const int up = most == 0 ? 0 : min(100, 14 - (static_cast<int>(most >> 7) - 127));
+        const float by = __uint_as_float(static_cast<uint32_t>(127 + up) << 23);
+        f = c2 * __uint_as_float(static_cast<uint32_t>(127 - up) << 23);
+        auto scaled = [by](uint32_t w) {
+          const float2 v = unpack2<true>(w);
+          return pack2<false>(v.x * by, v.y * by);
+        };
+#pragma unroll
+        for (int p = 0; p < kKc; ++p) q[p] = make_uint4(scaled(q[p].x), scaled(q[p].y), scaled(q[p].z), scaled(q[p].w));
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) fq[n][e] = __shfl_sync(0xFFFFFFFFu, f, 4 * (2 * t + e));
+#pragma unroll
+      for (int p = 0; p < kKc; ++p) {
+        if (kBits == 4)  // the nibbles' pairs
+          q[p] = make_uint4(__byte_perm(q[p].x, q[p].z, 0x5410), __byte_perm(q[p].x, q[p].z, 0x7632),
+                            __byte_perm(q[p].y, q[p].w, 0x5410), __byte_perm(q[p].y, q[p].w, 0x7632));
+        sq[n][p][lane] = q[p];
+      }
+    }
+    __syncwarp();
+    if (tile < tile_end) {
+      load_k(tile);
+      load_v(tile);
+      look(tile + 1);
+    }
+    // Weights p sv of a head count times wf, at most 2^15; room = 2^15 / wf (0 and 0: none has been seen yet).
+    float wf[kNt][2], room[kNt][2];
+#pragma unroll
+    for (int n = 0; n < kNt; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) wf[n][e] = room[n][e] = 0.0f;
+
+    for (int tl = tile; tl < tile_end; ++tl) {
+      const bool more = tl + 1 < tile_end;
+      float s[kRep][kNt][4];
+#pragma unroll
+      for (int r = 0; r < kRep; ++r)
+#pragma unroll
+        for (int n = 0; n < kNt; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[r][n][e] = 0.0f;
+#pragma unroll
+      for (int r = 0; r < kRep; ++r)
+#pragma unroll
+        for (int p = 0; p < kKc; ++p) {
+          uint32_t x[2][4];  // of rows g, g + 8: four pairs of codes
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            if constexpr (kBits == 8) {
+              const uint32_t w0 = kr[r][e][2 * p] ^ 0x80808080u, w1 = kr[r][e][2 * p + 1] ^ 0x80808080u;
+              x[e][0] = codes8<0>(w0);
+              x[e][1] = codes8<1>(w0);
+              x[e][2] = codes8<0>(w1);
+              x[e][3] = codes8<1>(w1);
+            } else {
+              const uint32_t w = kr[r][e][p];
+              x[e][0] = codes4<0>(w);
+              x[e][1] = codes4<1>(w);
+              x[e][2] = codes4<0>(w >> 8);
+              x[e][3] = codes4<1>(w >> 8);
+            }
+          }
+#pragma unroll
+          for (int n = 0; n < kNt; ++n) {
+            const uint4 f = reload16(&sq[n][p][lane]);
+            mma16816<false>(s[r][n], x[0][0], x[1][0], x[0][1], x[1][1], f.x, f.y);
+            mma16816<false>(s[r][n], x[0][2], x[1][2], x[0][3], x[1][3], f.z, f.w);
+          }
+        }
+      const uint32_t counts = live;
+      float sv[kRep][2];
+#pragma unroll
+      for (int r = 0; r < kRep; ++r)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          sv[r][e] = fabsf(vs[r][e]) <= 3.402823466e38f ? vs[r][e] : __int_as_float(0x7FFFFFFF);
+#pragma unroll
+          for (int n = 0; n < kNt; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) s[r][n][2 * e + i] *= ks[r][e] * fq[n][i];
+        }
+      if (more) load_k(tl + 1);
+      constexpr uint32_t kAll = (1u << (2 * kRep)) - 1u;
+      if (!__all_sync(0xFFFFFFFFu, counts == kAll)) {
+#pragma unroll
+        for (int r = 0; r < kRep; ++r)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            if (!(counts >> (2 * r + e) & 1u)) {
+              sv[r][e] = 0.0f;
+#pragma unroll
+              for (int n = 0; n < kNt; ++n) s[r][n][2 * e] = s[r][n][2 * e + 1] = -INFINITY;
+            }
+      }
+      bool move = false;
+#pragma unroll
+      for (int r = 0; r < kRep; ++r)
+#pragma unroll
+        for (int n = 0; n < kNt; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) move = move || s[r][n][e] > ref[n][e & 1] + kMove;
+      if (__any_sync(0xFFFFFFFFu, move)) {
+#pragma unroll
+        for (int n = 0; n < kNt; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float m = ref[n][e];
+#pragma unroll
+            for (int r = 0; r < kRep; ++r) m = fmaxf(m, fmaxf(s[r][n][e], s[r][n][e + 2]));
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+            const float alpha = m == ref[n][e] ? 1.0f : exp2_fast(ref[n][e] - m);
+            ref[n][e] = m;
+            l[n][e] *= alpha;
+#pragma unroll
+            for (int hh = 0; hh < kVc; ++hh)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                o[n][hh][j][e] *= alpha;
+                o[n][hh][j][e + 2] *= alpha;
+              }
+          }
+      }
+      // p into the sums, p sv in s's place
+      move = false;
+#pragma unroll
+      for (int n = 0; n < kNt; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float from = ref[n][i] == -INFINITY ? 0.0f : ref[n][i];
+#pragma unroll
+          for (int r = 0; r < kRep; ++r)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float p = exp2_fast(s[r][n][2 * e + i] - from);
+              l[n][i] += p;
+              s[r][n][2 * e + i] = p * sv[r][e];
+              move = move || fabsf(s[r][n][2 * e + i]) > room[n][i];
+            }
+        }
+      if (__any_sync(0xFFFFFFFFu, move)) {
+#pragma unroll
+        for (int n = 0; n < kNt; ++n)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            float m = 0.0f;
+#pragma unroll
+            for (int r = 0; r < kRep; ++r) m = fmaxf(m, fmaxf(fabsf(s[r][n][i]), fabsf(s[r][n][i + 2])));
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+            if (m > room[n][i]) {
+              // the power of two that takes m to 2^10 - 2^11 (within what fp32 has)
+              const int e = min(120, max(-110, static_cast<int>(__float_as_uint(m) >> 23) - 127));
+              const float was = room[n][i];
+              wf[n][i] = __uint_as_float(static_cast<uint32_t>(127 + 10 - e) << 23);
+              room[n][i] = __uint_as_float(static_cast<uint32_t>(127 + 5 + e) << 23);
+              const float back = was / room[n][i];
+#pragma unroll
+              for (int hh = 0; hh < kVc; ++hh)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  o[n][hh][j][i] *= back;
+                  o[n][hh][j][i + 2] *= back;
+                }
+            }
+          }
+      }
+#pragma unroll
+      for (int r = 0; r < kRep; ++r) {
+        uint32_t pw[kNt][2][2];
+#pragma unroll
+        for (int n = 0; n < kNt; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {  // rows g, g + 8
+            const float w0 = s[r][n][2 * e] * wf[n][0], w1 = s[r][n][2 * e + 1] * wf[n][1];
+            const uint32_t hi = pack2<false>(w0, w1);
+            const float2 back = unpack2<false>(hi);
+            pw[n][0][e] = transpose8x8(hi);
+            pw[n][1][e] = transpose8x8(pack2<false>(w0 - back.x, w1 - back.y));
+          }
+#pragma unroll
+        for (int hh = 0; hh < kVc; ++hh) {
+          uint32_t x[4][4];  // [j][operand]: dimensions 2 j, 2 j + 1 of positions 2 t, 2 t + 1; 2 t + 8, 2 t + 9
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            if constexpr (kBits == 8) {
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                const uint32_t w0 = vr[r][2 * e][2 * hh + i], w1 = vr[r][2 * e + 1][2 * hh + i];
+                const uint32_t lo = __byte_perm(w0, w1, 0x5140) ^ 0x80808080u, hi = __byte_perm(w0, w1, 0x7362) ^ 0x80808080u;
+                x[2 * i][2 * e] = codes8<0>(lo);
+                x[2 * i][2 * e + 1] = codes8<1>(lo);
+                x[2 * i + 1][2 * e] = codes8<0>(hi);
+                x[2 * i + 1][2 * e + 1] = codes8<1>(hi);
+              }
+            } else {
+              const uint32_t w0 = vr[r][2 * e][hh], w1 = vr[r][2 * e + 1][hh];
+              const uint32_t lo = __byte_perm(w0, w1, 0x5410), hi = __byte_perm(w0, w1, 0x7632);
+              x[0][2 * e] = codes4<0>(lo);
+              x[0][2 * e + 1] = codes4<1>(lo);
+              x[1][2 * e] = codes4<0>(lo >> 8);
+              x[1][2 * e + 1] = codes4<1>(lo >> 8);
+              x[2][2 * e] = codes4<0>(hi);
+              x[2][2 * e + 1] = codes4<1>(hi);
+              x[3][2 * e] = codes4<0>(hi >> 8);
+              x[3][2 * e + 1] = codes4<1>(hi >> 8);
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int n = 0; n < kNt; ++n)
+#pragma unroll
+              for (int i = 0; i < 2; ++i)
+                mma16816<false>(o[n][hh][j], x[j][0], x[j][1], x[j][2], x[j][3], pw[n][i][0], pw[n][i][1]);
+        }
+      }
+      if (more) {
+        load_v(tl + 1);
+        look(tl + 2);
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < kNt; ++n)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float back = room[n][i] == 0.0f ? 1.0f : room[n][i] * 0x1p-15f;  // 1 / wf
+#pragma unroll
+        for (int hh = 0; hh < kVc; ++hh)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            o[n][hh][j][i] *= back;
+            o[n][hh][j][i + 2] *= back;
+          }
+      }
+  }
+};
+
+}  // namespace paged
+}  // namespace p4q

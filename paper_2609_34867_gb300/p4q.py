@@ -115,6 +115,10 @@ def lib() -> ctypes.CDLL:
         L.p4q_paged_attention_workspace_bytes.restype = S
         L.p4q_paged_attention.argtypes = [P, I, I, P, P, ctypes.c_float, P, I, P, P, S, P]
         L.p4q_paged_attention.restype = st
+        L.p4q_rope_append_quant.argtypes = [P, I, P, I, P, I, I, I, P, P, I, I, I, P, P, P, P, I, P, I, P, I, P, I, P]
+        L.p4q_rope_append_quant.restype = st
+        L.p4q_paged_attention_quant.argtypes = [P, I, I, P, I, P, ctypes.c_float, P, I, P, P, S, P]
+        L.p4q_paged_attention_quant.restype = st
         L.p4q_sample.argtypes = [P, I, ctypes.c_int64, I, I, P, P, P, P, P, P, P, P]
         L.p4q_sample.restype = st
         _lib = L
@@ -543,6 +547,123 @@ def paged_attention(q, k_cache, v_cache, table, lens, ws=None, scale=None, strea
             ws = paged_attention_workspace(q.device)
     o = _empty(q.shape, q.dtype, q.device, stream)
     p4q_paged_attention(q, k_cache, v_cache, table, lens, o, ws, scale, None, stream)
+    return o
+
+
+_PAGED_KVQ = struct.Struct("@PPPPPqqqqqq8i")  # p4q_paged_kvq
+
+
+def _paged_kvq(k_cache, v_cache, k_scale, v_scale, table):
+    """(p4q_paged_kvq as bytes, Hkv, dh, seqs) of codes [pages, page_size, Hkv, dh]
+    int8, or [.., dh / 2] uint8 with two codes of 4 bits in each (any order of slots and
+    heads in memory; unit stride along the last), scales [pages, page_size, Hkv]
+    fp32 of any strides, and a page table [seqs, pages per sequence] int32."""
+    try:
+        shape, strides, dt = k_cache.shape, k_cache.stride(), k_cache.dtype
+        pages, size, heads, dh = shape
+        ps, ts, hs, step = strides
+    except (AttributeError, ValueError):
+        dt = None
+    if (dt is not torch.int8 and dt is not torch.uint8) or step != 1 or not k_cache.is_cuda:
+        raise TypeError("k_cache: expected a CUDA int8 tensor [pages, page_size, Hkv, dh] or uint8 [.., dh / 2], unit "
+                        "stride along the last dimension")
+    if not isinstance(v_cache, torch.Tensor) or v_cache.dtype is not dt or not v_cache.is_cuda or \
+            v_cache.shape != shape or v_cache.stride() != strides:
+        raise TypeError("v_cache: expected a CUDA tensor of k_cache's type, shape and strides")
+    if not isinstance(k_scale, torch.Tensor) or k_scale.dtype is not torch.float32 or not k_scale.is_cuda or \
+            k_scale.shape != shape[:3]:
+        raise TypeError("k_scale: expected a CUDA fp32 tensor [pages, page_size, Hkv]")
+    scale_strides = k_scale.stride()
+    if not isinstance(v_scale, torch.Tensor) or v_scale.dtype is not torch.float32 or not v_scale.is_cuda or \
+            v_scale.shape != shape[:3] or v_scale.stride() != scale_strides:
+        raise TypeError("v_scale: expected a CUDA fp32 tensor of k_scale's shape and strides")
+    try:
+        seqs, cols = table.shape
+        ld, step = table.stride()
+    except (AttributeError, ValueError):
+        raise TypeError("table: expected a CUDA int32 2-D tensor with unit column stride") from None
+    if table.dtype is not torch.int32 or not table.is_cuda or (step != 1 and cols > 1):
+        raise TypeError("table: expected a CUDA int32 2-D tensor with unit column stride")
+    sps, sts, shs = scale_strides
+    bits, row = (8, dh) if dt is torch.int8 else (4, 2 * dh)
+    # (the stride of a dimension of one says nothing)
+    kv = _PAGED_KVQ.pack(k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
+                         table.data_ptr(), ps if pages > 1 else (dh + 15) // 16 * 16, ts if size > 1 else (dh + 15) // 16 * 16,
+                         hs if heads > 1 else (dh + 15) // 16 * 16, sps if pages > 1 else 1, sts if size > 1 else 1,
+                         shs if heads > 1 else 1, bits, pages, size, heads, row, seqs, ld if seqs > 1 else cols, cols)
+    return kv, heads, row, seqs
+
+
+def _row_type(t, name):
+    dt = getattr(t, "dtype", None)
+    if dt is not torch.float16 and dt is not torch.bfloat16:
+        raise TypeError(f"{name}: expected a CUDA fp16 or bf16 2-D tensor with unit column stride")
+    return dt
+
+
+def p4q_rope_append_quant(q, k, v, cos, sin, pos, k_cache, v_cache, k_scale, v_scale, table, q_out, k_out=None,
+                          v_out=None, seq=None, rot_pos=None, interleaved=False, stream=None):
+    """p4q_rope_append into a paged cache of codes: k_cache, v_cache [pages,
+    page_size, Hkv, dh] int8 (8 bits) or [.., dh / 2] uint8 (4 bits, the even dimension in the
+    low half) and k_scale, v_scale [pages, page_size, Hkv] fp32, of any order of slots and
+    heads in memory (side by side scales of a page's slots are read fastest). q, k, v
+    fp16 or bf16; k_out, v_out [T, Hkv*dh], optional, take the values that the codes stand for, and may
+    be k and v. Other arguments as p4q_rope_append."""
+    kv, heads, dh, _ = _paged_kvq(k_cache, v_cache, k_scale, v_scale, table)
+    dt = _row_type(q, "q")
+    ldq = _rows(q, dt, None, None, "q")
+    T, width = q.shape
+    if width % dh:
+        raise ValueError(f"q has {width} columns, not a multiple of the head dimension {dh}")
+    ldk, ldv = _rows(k, dt, T, heads * dh, "k"), _rows(v, dt, T, heads * dh, "v")
+    ldqo = _rows(q_out, dt, T, width, "q_out")
+    ldko = 0 if k_out is None else _rows(k_out, dt, T, heads * dh, "k_out")
+    ldvo = 0 if v_out is None else _rows(v_out, dt, T, heads * dh, "v_out")
+    _need(cos, torch.float32, 2, "cos"); _need(sin, torch.float32, 2, "sin")
+    max_pos, half = cos.shape
+    if sin.shape != cos.shape:
+        raise ValueError("cos and sin differ in shape")
+    status = lib().p4q_rope_append_quant(
+        q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, T, width // dh, cos.data_ptr(), sin.data_ptr(), max_pos,
+        2 * half, 1 if interleaved else 0, _vector(pos, torch.int32, T, "pos"),
+        _optional(rot_pos, torch.int32, T, "rot_pos"), _optional(seq, torch.int32, T, "seq"), kv, DTYPES[dt],
+        q_out.data_ptr(), ldqo, _ptr(k_out), ldko, _ptr(v_out), ldvo, _stream(stream))
+    if status:
+        raise P4QError(status, "p4q_rope_append_quant")
+
+
+def p4q_paged_attention_quant(q, k_cache, v_cache, k_scale, v_scale, table, lens, o, ws, scale=None, lse=None,
+                              stream=None):
+    """p4q_paged_attention over a paged cache of codes (caches and scales as in
+    p4q_rope_append_quant); q, o [seqs, H*dh] fp16 or bf16. Other arguments and the
+    workspace as p4q_paged_attention."""
+    kv, heads, dh, seqs = _paged_kvq(k_cache, v_cache, k_scale, v_scale, table)
+    dt = _row_type(q, "q")
+    ldq = _rows(q, dt, seqs, None, "q")
+    width = q.shape[1]
+    if width % dh:
+        raise ValueError(f"q has {width} columns, not a multiple of the head dimension {dh}")
+    ldo = _rows(o, dt, seqs, width, "o")
+    _need(ws, torch.uint8, 1, "ws")
+    if lse is not None:
+        _need(lse, torch.float32, 2, "lse")
+        if lse.shape != (seqs, width // dh):
+            raise ValueError(f"lse has shape {tuple(lse.shape)}, expected {(seqs, width // dh)}")
+    status = lib().p4q_paged_attention_quant(
+        q.data_ptr(), ldq, width // dh, kv, DTYPES[dt], _vector(lens, torch.int32, seqs, "lens"),
+        dh ** -0.5 if scale is None else scale, o.data_ptr(), ldo, _ptr(lse), ws.data_ptr(), ws.numel(),
+        _stream(stream))
+    if status:
+        raise P4QError(status, "p4q_paged_attention_quant")
+
+
+def paged_attention_quant(q, k_cache, v_cache, k_scale, v_scale, table, lens, ws=None, scale=None, stream=None):
+    """Allocating wrapper of p4q_paged_attention_quant: returns o."""
+    if ws is None:
+        with _on(stream):
+            ws = paged_attention_workspace(q.device)
+    o = _empty(q.shape, q.dtype, q.device, stream)
+    p4q_paged_attention_quant(q, k_cache, v_cache, k_scale, v_scale, table, lens, o, ws, scale, None, stream)
     return o
 
 
