@@ -633,6 +633,30 @@ p4q_status p4q_paged_attention_quant(const uint16_t* q, int ldq, int H, const p4
                                      const int32_t* lens, float scale, uint16_t* o, int ldo, float* lse, void* ws,
                                      size_t ws_bytes, p4q_stream_t stream);
 
+/* p4q_paged_attention for sequences that share prefixes (questions about one
+ * image, samples of one prompt): sequences group_start[g] .. group_start[g + 1] - 1
+ * have their first prefix_lens[g] positions in common, which are read once for
+ * all of them, and the others each of its own. o and lse are those of
+ * p4q_paged_attention over all lens[b] positions (which count the prefix).
+ * A position of the prefix lies where the page table's row of the group's first
+ * sequence has it; from prefix_lens[g] on a sequence's own row counts, so a page
+ * that the prefix ends in is not shared (each sequence has the rest of it in a
+ * page of its own; slots of that page before the prefix's end are not read, and
+ * columns wholly before it may hold anything). A sequence shorter than its
+ * group's prefix sees lens[b] positions of it. A sequence in no group (before
+ * group_start[0], from group_start[groups] on) shares nothing.
+ *   group_start [groups + 1] int32, not falling, 0 .. kv->seqs; prefix_lens
+ *         [groups] int32 (<= 0: nothing shared). Starts that fall or lie outside, and prefixes beyond the
+ *         page table's columns, give P4Q_ERR_INDEX; the rows of such groups are not defined.
+ *   ws    device workspace of p4q_prefix_attention_workspace_bytes() bytes for
+ *         these seqs, groups, H and dh (never less for more of one of them)
+ * Requires 1 <= groups <= kv->seqs, kv->seqs * H < 2^31 - 255. Other arguments, rules and precision as
+ * p4q_paged_attention. */
+size_t p4q_prefix_attention_workspace_bytes(int seqs, int groups, int H, int dh);
+p4q_status p4q_prefix_attention(const uint16_t* q, int ldq, int H, const p4q_paged_kv* kv, const int32_t* lens,
+                                const int32_t* group_start, const int32_t* prefix_lens, int groups, float scale,
+                                uint16_t* o, int ldo, float* lse, void* ws, size_t ws_bytes, p4q_stream_t stream);
+
 /* Draws one token from each row of logits with a given uniform number. With
  * x_max the row's largest logit and T its temperature:
  *   d_i = 0 where x_i = x_max, else (x_max - x_i) * (1 / T)    (fp32)

@@ -336,9 +336,10 @@ p4q_status p4q_device_status(p4q_stream_t stream) {
   if (cudaStreamSynchronize(reinterpret_cast<cudaStream_t>(stream)) != cudaSuccess) return P4Q_ERR_CUDA;
   const unsigned int g = gemm_read_and_clear_error() | gemm8_read_and_clear_error() | quant_read_and_clear_error() |
                          attn_read_and_clear_error() | fewrows_read_and_clear_error() | peak_read_and_clear_error() |
-                         diverse_read_and_clear_error();
+                         diverse_read_and_clear_error() | prefix_read_and_clear_error();
   const unsigned int i = rope_read_and_clear_error() | paged_read_and_clear_error() |
-                         rope_quant_read_and_clear_error() | paged_quant_read_and_clear_error();
+                         rope_quant_read_and_clear_error() | paged_quant_read_and_clear_error() |
+                         prefix_read_and_clear_index_error();
   if (cudaGetLastError() != cudaSuccess) return P4Q_ERR_CUDA;
   return g ? P4Q_ERR_TIMEOUT : i ? P4Q_ERR_INDEX : P4Q_OK;
 }
@@ -586,6 +587,46 @@ p4q_status p4q_paged_attention_quant(const uint16_t* q, int ldq, int H, const p4
   a.bf16 = dtype == P4Q_BF16;
   unsigned int launches = 0;
   const cudaError_t e = launch_paged_attention_quant(a, reinterpret_cast<cudaStream_t>(stream), &launches);
+  counted(cudaSuccess, launches);
+  return from_cuda(e);
+}
+
+size_t p4q_prefix_attention_workspace_bytes(int seqs, int groups, int H, int dh) {
+  if (seqs < 0 || groups < 0 || H < 1 || H > 65535 || dh < 1 || dh > 128) return 0;
+  return prefix_attention_workspace_bytes(seqs, groups, H, dh);
+}
+
+p4q_status p4q_prefix_attention(const uint16_t* q, int ldq, int H, const p4q_paged_kv* kv, const int32_t* lens,
+                                const int32_t* group_start, const int32_t* prefix_lens, int groups, float scale,
+                                uint16_t* o, int ldo, float* lse, void* ws, size_t ws_bytes, p4q_stream_t stream) {
+  PrefixArgs a;
+  p4q_status st = check_paged(kv, kv && kv->seqs > 0, &a.kv);
+  if (st != P4Q_OK) return st;
+  if (H < 1 || H % kv->Hkv != 0 || groups < 0 || !std::isfinite(scale * 1.4426950408889634f)) return P4Q_ERR_INVALID_ARG;
+  if (H > 65535 || groups > kv->seqs || static_cast<long long>(kv->seqs) * H > 0x7FFFFF00ll) return P4Q_ERR_UNSUPPORTED_SHAPE;
+  if (ldq < H * kv->dh || ldo < H * kv->dh) return P4Q_ERR_INVALID_ARG;
+  if (kv->seqs > 0 && (groups < 1 || !q || !lens || !group_start || !prefix_lens || !o)) return P4Q_ERR_INVALID_ARG;
+  if (ldq % 8 != 0 || ldo % 8 != 0 || !aligned16(q) || !aligned16(o) || !aligned4(lens) || !aligned4(group_start) ||
+      !aligned4(prefix_lens) || !aligned4(lse))
+    return P4Q_ERR_MISALIGNED;
+  if (kv->seqs == 0) return P4Q_OK;
+  if (!ws || ws_bytes < prefix_attention_workspace_bytes(kv->seqs, groups, H, kv->dh)) return P4Q_ERR_WORKSPACE_TOO_SMALL;
+  if (!aligned16(ws)) return P4Q_ERR_MISALIGNED;
+  if ((st = check_device()) != P4Q_OK) return st;
+  a.q = q;
+  a.o = o;
+  a.lse = lse;
+  a.lens = lens;
+  a.group_start = group_start;
+  a.prefix_lens = prefix_lens;
+  a.groups = groups;
+  a.ldq = ldq;
+  a.ldo = ldo;
+  a.H = H;
+  a.scale = scale;
+  a.ws = ws;
+  unsigned int launches = 0;
+  const cudaError_t e = launch_prefix_attention(a, reinterpret_cast<cudaStream_t>(stream), &launches);
   counted(cudaSuccess, launches);
   return from_cuda(e);
 }

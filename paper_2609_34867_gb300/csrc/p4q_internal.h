@@ -230,6 +230,20 @@ size_t paged_attention_workspace_bytes();
 cudaError_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t stream, unsigned int* launches);
 unsigned int paged_read_and_clear_error();
 
+// Sequences group_start[g] .. group_start[g + 1] - 1 share their first prefix_lens[g] positions.
+struct PrefixArgs : PagedAttnArgs {
+  const int32_t* group_start = nullptr;  // [groups + 1]
+  const int32_t* prefix_lens = nullptr;  // [groups]
+  int groups = 0;
+  int grid = 0;                          // CTAs of the prefix kernel
+  unsigned long long* base = nullptr;    // [groups + 1], see p4q_paged_prefix.cuh
+  float* parts = nullptr;
+};
+size_t prefix_attention_workspace_bytes(int seqs, int groups, int H, int dh);
+cudaError_t launch_prefix_attention(PrefixArgs a, cudaStream_t stream, unsigned int* launches);
+unsigned int prefix_read_and_clear_error();        // waits that ran out
+unsigned int prefix_read_and_clear_index_error();
+
 // A cache of codes: strides of the codes in bytes, of the scales in elements. Copied from p4q_paged_kvq.
 struct PagedCodes {
   uint8_t* k = nullptr;

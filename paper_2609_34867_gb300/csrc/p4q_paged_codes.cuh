@@ -83,6 +83,8 @@ struct Codes {
   static __host__ __device__ constexpr int ctas(int nt) { return nt == 1 ? 3 : 2; }
   static __device__ __forceinline__ bool bf16(const Args& a) { return a.bf16; }
   static __device__ __forceinline__ int first_own(const Args&, int, int) { return 0; }
+  static __device__ __forceinline__ int table_row(const Args&, int b, int) { return b; }
+  static __device__ __forceinline__ void add_prefix(const Args&, int, int, int, float&, float&, float4&) {}
   static __device__ __forceinline__ int first_dim(int hh, int g) { return (kDh / 8) * g + 8 * hh; }
   // The dimensions of q's piece p that lane t's keys have.
   static __device__ __forceinline__ int q_dim(int p, int t) {

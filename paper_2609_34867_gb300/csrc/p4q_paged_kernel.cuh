@@ -35,7 +35,7 @@ __device__ __forceinline__ void st_shared_cluster_v4(uint32_t a, float4 v) {
 // the reference maximum, the sum and the values against it.
 template <class C>
 __device__ __forceinline__ void write_out(const typename C::Args& a, int b, int h, int d, float m, float sum, float4 v) {
-  if constexpr (C::kOwnOnly) C::add_prefix(a, b, h, d, m, sum, v);
+  C::add_prefix(a, b, h, d, m, sum, v);
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
   uint2 w;
   if (C::bf16(a))
@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(kThreads, C::ctas(kNt)) paged_attention_kernel
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[n][hh][j][e] = 0.0f;
     }
-    const Unit un = {c.table + static_cast<long long>(b) * c.table_ld, b, hk, h0, heads, len, C::first_own(a, b, len), base};
+    const Unit un = {c.table + static_cast<long long>(C::table_row(a, b, len)) * c.table_ld, b, hk, h0, heads, len, C::first_own(a, b, len), base};
     C::template attend<kNt>(a, un, tile, tile_end, sq[warp], acc);
     if (C::kOwnOnly) pdl_wait();  // the prefix's parts
 

@@ -27,7 +27,10 @@
 // room for eight warps, which their products' and exchanges' latencies bound: 907.)
 #pragma once
 
+#include <type_traits>
+
 #include "p4q_paged.cuh"
+#include "p4q_paged_prefix.cuh"
 
 namespace p4q {
 namespace paged {
@@ -77,7 +80,7 @@ __device__ __forceinline__ void split2(float p0, float p1, uint32_t (&w)[kParts<
 // of its own, behind a prefix.
 template <bool kBf16Rows, int kDhRows, bool kSmallPage, bool kOwn = false>
 struct Rows {
-  typedef PagedAttnArgs Args;
+  typedef std::conditional_t<kOwn, PrefixArgs, PagedAttnArgs> Args;
   static constexpr bool kBf16 = kBf16Rows, kOwnOnly = kOwn;
   static constexpr int kDh = kDhRows;
   static constexpr int kRep = 128 / kDh;  // blocks of 16 positions per warp and tile: 8 KB of keys and values
@@ -87,7 +90,17 @@ struct Rows {
   static constexpr float kLift = kShift<kBf16>;
   static __host__ __device__ constexpr int ctas(int nt) { return nt == 1 ? 3 : 2; }
   static __device__ __forceinline__ bool bf16(const Args&) { return kBf16; }
-  static __device__ __forceinline__ int first_own(const Args&, int, int) { return 0; }
+  static __device__ __forceinline__ int first_own(const Args& a, int b, int len) {
+    if constexpr (kOwn) return prefix_seen(a, b, len);
+    return 0;
+  }
+  static __device__ __forceinline__ int table_row(const Args& a, int b, int len) {
+    if constexpr (kOwn) return row_of(a, b, len);
+    return b;
+  }
+  static __device__ __forceinline__ void add_prefix(const Args& a, int b, int h, int d, float& m, float& sum, float4& v) {
+    if constexpr (kOwn) add_prefix_parts(a, b, h, d, m, sum, v);
+  }
   static __device__ __forceinline__ int first_dim(int hh, int g) { return 64 * hh + 8 * g; }
 
   // Goes through tiles tile .. tile_end - 1 of the unit. sq: the warp's place for the query operand.
@@ -98,6 +111,7 @@ struct Rows {
     const float c2 = a.scale * 1.4426950408889634f;
     const PagedCache& c = a.kv;
     const int len = un.len, heads = un.heads;
+    if (kOwn && un.from >= len) return;  // (nothing behind the prefix)
     const uint16_t* kh = c.k + un.hk * c.head_stride + t * 8;
     const uint16_t* vh = c.v + un.hk * c.head_stride + g * 8;
     const int slots = (1 << c.page_log2) - 1;

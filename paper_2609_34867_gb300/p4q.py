@@ -119,6 +119,10 @@ def lib() -> ctypes.CDLL:
         L.p4q_rope_append_quant.restype = st
         L.p4q_paged_attention_quant.argtypes = [P, I, I, P, I, P, ctypes.c_float, P, I, P, P, S, P]
         L.p4q_paged_attention_quant.restype = st
+        L.p4q_prefix_attention_workspace_bytes.argtypes = [I, I, I, I]
+        L.p4q_prefix_attention_workspace_bytes.restype = S
+        L.p4q_prefix_attention.argtypes = [P, I, I, P, P, P, P, I, ctypes.c_float, P, I, P, P, S, P]
+        L.p4q_prefix_attention.restype = st
         L.p4q_sample.argtypes = [P, I, ctypes.c_int64, I, I, P, P, P, P, P, P, P, P]
         L.p4q_sample.restype = st
         _lib = L
@@ -664,6 +668,56 @@ def paged_attention_quant(q, k_cache, v_cache, k_scale, v_scale, table, lens, ws
             ws = paged_attention_workspace(q.device)
     o = _empty(q.shape, q.dtype, q.device, stream)
     p4q_paged_attention_quant(q, k_cache, v_cache, k_scale, v_scale, table, lens, o, ws, scale, None, stream)
+    return o
+
+
+def p4q_prefix_attention_workspace_bytes(seqs: int, groups: int, H: int, dh: int) -> int:
+    return int(lib().p4q_prefix_attention_workspace_bytes(seqs, groups, H, dh))
+
+
+def prefix_attention_workspace(seqs, groups, H, dh, device):
+    """A workspace for p4q_prefix_attention of up to these sizes (one per stream)."""
+    return torch.empty((p4q_prefix_attention_workspace_bytes(seqs, groups, H, dh),), dtype=torch.uint8, device=device)
+
+
+def p4q_prefix_attention(q, k_cache, v_cache, table, lens, group_start, prefix_lens, o, ws, scale=None, lse=None,
+                         stream=None):
+    """p4q_paged_attention where sequences group_start[g] .. group_start[g + 1] - 1 share
+    their first prefix_lens[g] positions, which lie in the pages of the first of them and are read
+    once for all; group_start [groups + 1], prefix_lens [groups] int32; ws as
+    prefix_attention_workspace() gives it; other arguments as p4q_paged_attention."""
+    kv, dt, heads, dh, seqs = _paged_kv(k_cache, v_cache, table)
+    ldq = _rows(q, dt, seqs, None, "q")
+    width = q.shape[1]
+    if width % dh:
+        raise ValueError(f"q has {width} columns, not a multiple of the head dimension {dh}")
+    ldo = _rows(o, dt, seqs, width, "o")
+    _need(ws, torch.uint8, 1, "ws")
+    if lse is not None:
+        _need(lse, torch.float32, 2, "lse")
+        if lse.shape != (seqs, width // dh):
+            raise ValueError(f"lse has shape {tuple(lse.shape)}, expected {(seqs, width // dh)}")
+    try:
+        (groups,) = prefix_lens.shape
+    except (AttributeError, ValueError):
+        raise TypeError("prefix_lens: expected a contiguous CUDA int32 vector") from None
+    status = lib().p4q_prefix_attention(
+        q.data_ptr(), ldq, width // dh, kv, _vector(lens, torch.int32, seqs, "lens"),
+        _vector(group_start, torch.int32, groups + 1, "group_start"), _vector(prefix_lens, torch.int32, groups, "prefix_lens"),
+        groups, dh ** -0.5 if scale is None else scale, o.data_ptr(), ldo, _ptr(lse), ws.data_ptr(), ws.numel(),
+        _stream(stream))
+    if status:
+        raise P4QError(status, "p4q_prefix_attention")
+
+
+def prefix_attention(q, k_cache, v_cache, table, lens, group_start, prefix_lens, ws=None, scale=None, stream=None):
+    """Allocating wrapper of p4q_prefix_attention: returns o."""
+    if ws is None:
+        dh = k_cache.shape[3]
+        with _on(stream):
+            ws = prefix_attention_workspace(q.shape[0], prefix_lens.shape[0], q.shape[1] // dh, dh, q.device)
+    o = _empty(q.shape, q.dtype, q.device, stream)
+    p4q_prefix_attention(q, k_cache, v_cache, table, lens, group_start, prefix_lens, o, ws, scale, None, stream)
     return o
 
 
