@@ -67,12 +67,15 @@ __device__ __forceinline__ void load_words(uint32_t (&w)[kWords], const uint8_t*
   }
 }
 
-template <int kBits, int kDhRows, bool kSmallPage>
+// kPair: at most four heads to a key/value head's unit. Columns 4 - 7 of the products, which would be
+// empty, then repeat heads 0 - 3 and take the second fp16 value of their weights, so one product
+// of O^T does for both.
+template <int kBits, int kDhRows, bool kSmallPage, bool kPair>
 struct Codes {
   typedef QuantAttnArgs Args;
   static constexpr bool kOwnOnly = false;
   static constexpr int kDh = kDhRows;
-  static constexpr int kRep = kSmallPage ? 2 : kDh * kBits == 1024 ? 2 : 4;  // blocks of 16 positions per warp and tile
+  static constexpr int kRep = kDh * kBits == 256 && !kSmallPage ? 4 : 2;  // blocks of 16 positions per warp and tile
   static constexpr int kTile = 16 * kRep * kWarps;
   static constexpr int kKc = kDh / 32;             // pieces of q per lane, 8 dimensions each
   static constexpr int kVc = kDh / 64;
@@ -80,7 +83,8 @@ struct Codes {
   static constexpr int kVw = kDh * kBits / 256;    // of a value row
   static constexpr float kLift = 0.0f;
   static constexpr float kMove = 8.0f;
-  static __host__ __device__ constexpr int ctas(int nt) { return nt == 1 ? 3 : 2; }
+  static constexpr int kSecond = kPair ? 1 : 2;    // products per operand of O^T
+  static __host__ __device__ constexpr int ctas(int nt) { return nt == 1 ? (kDh * kBits == 1024 || kSmallPage ? 3 : 4) : 2; }
   static __device__ __forceinline__ bool bf16(const Args& a) { return a.bf16; }
   static __device__ __forceinline__ int first_own(const Args&, int, int) { return 0; }
   static __device__ __forceinline__ int table_row(const Args&, int b, int) { return b; }
@@ -98,11 +102,15 @@ struct Codes {
     const float c2 = a.scale * 1.4426950408889634f;
     const PagedCodes& c = a.kv;
     const int len = un.len, heads = un.heads;
-    const uint8_t* kh = c.k + un.hk * c.head_stride + t * (kKw >= 4 ? 16 : 4 * kKw);
-    const uint8_t* vh = c.v + un.hk * c.head_stride + g * (4 * kVw);
-    const float* ksh = c.k_scale + un.hk * c.scale_head_stride;
-    const float* vsh = c.v_scale + un.hk * c.scale_head_stride;
     const int slots = (1 << c.page_log2) - 1;
+    // Where the lane's rows of a block begin: row g (and g + 8) of keys and scales, rows 2 t (2 t + 1,
+    // 2 t + 8, 2 t + 9) of values. With small pages the rows are added at the load.
+    const int kg = kSmallPage ? 0 : g, vg = kSmallPage ? 0 : 2 * t;
+    const uint8_t* const kh = c.k + un.hk * c.head_stride + kg * c.token_stride + t * (kKw >= 4 ? 16 : 4 * kKw);
+    const uint8_t* const vh = c.v + un.hk * c.head_stride + vg * c.token_stride + g * (4 * kVw);
+    const float* const ksh = c.k_scale + un.hk * c.scale_head_stride + kg * c.scale_token_stride;
+    const float* const vsh = c.v_scale + un.hk * c.scale_head_stride + kg * c.scale_token_stride;
+    const long long ts = c.token_stride, ts8 = 8 * c.token_stride, ss8 = 8 * c.scale_token_stride;
 
     // The page of position j, -1 if it is not to be read.
     auto page_of = [&](int j) -> int {
@@ -137,33 +145,56 @@ struct Codes {
       }
     };
     uint32_t live = 0;  // rows g, g + 8 of block r count: bits 2 r, 2 r + 1
+    const uint8_t* vp[kRep];
     auto load_k = [&](int tl) {
       live = 0;
 #pragma unroll
       for (int r = 0; r < kRep; ++r) {
         const int j = tl * kTile + (warp * kRep + r) * 16;
+        if constexpr (kSmallPage) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int page = pg[r][kSmallPage ? e : 0], row = j + g + 8 * e;
-          if (page >= 0) {
-            if (row < len) live |= 1u << (2 * r + e);
-            const long long slot = row & slots;
-            load_words<kKw>(kr[r][e], kh + page * c.page_stride + slot * c.token_stride, 64);
-            const long long at = page * c.scale_page_stride + slot * c.scale_token_stride;
-            ks[r][e] = ksh[at];
-            vs[r][e] = vsh[at];
+          for (int e = 0; e < 2; ++e) {
+            const int page = pg[r][e], slot = (j + g + 8 * e) & slots;
+            if (page >= 0) {
+              live |= 1u << (2 * r + e);
+              load_words<kKw>(kr[r][e], kh + page * c.page_stride + slot * ts, 64);
+              const long long at = page * c.scale_page_stride + slot * c.scale_token_stride;
+              ks[r][e] = ksh[at];
+              vs[r][e] = vsh[at];
+            }
           }
+        } else if (pg[r][0] >= 0) {
+          // rows past the length are read too (they are the page's) but do not count
+          live |= (j + g < len ? 1u << (2 * r) : 0u) | (j + g + 8 < len ? 2u << (2 * r) : 0u);
+          const long long slot = j & slots, at = pg[r][0] * c.page_stride + slot * ts;
+          const long long sat = pg[r][0] * c.scale_page_stride + slot * c.scale_token_stride;
+          const uint8_t* const p = kh + at;
+          vp[r] = vh + at;
+          load_words<kKw>(kr[r][0], p, 64);
+          load_words<kKw>(kr[r][1], p + ts8, 64);
+          const float *kp = ksh + sat, *vq = vsh + sat;
+          ks[r][0] = *kp;
+          ks[r][1] = kp[ss8];
+          vs[r][0] = *vq;
+          vs[r][1] = vq[ss8];
         }
       }
     };
     auto load_v = [&](int tl) {
 #pragma unroll
       for (int r = 0; r < kRep; ++r) {
-        const int j = tl * kTile + (warp * kRep + r) * 16;
+        if constexpr (kSmallPage) {
+          const int j = tl * kTile + (warp * kRep + r) * 16;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int page = pg[r][kSmallPage ? 2 + e : 0], row = j + 2 * t + (e & 1) + 8 * (e >> 1);
-          if (page >= 0) load_words<kVw>(vr[r][e], vh + page * c.page_stride + (row & slots) * c.token_stride, 16);
+          for (int e = 0; e < 4; ++e) {
+            const int page = pg[r][2 + e], row = j + 2 * t + (e & 1) + 8 * (e >> 1);
+            if (page >= 0) load_words<kVw>(vr[r][e], vh + page * c.page_stride + (row & slots) * ts, 16);
+          }
+        } else if (pg[r][0] >= 0) {
+          load_words<kVw>(vr[r][0], vp[r], 16);
+          load_words<kVw>(vr[r][1], vp[r] + ts, 16);
+          load_words<kVw>(vr[r][2], vp[r] + ts8, 16);
+          load_words<kVw>(vr[r][3], vp[r] + ts8 + ts, 16);
         }
       }
     };
@@ -174,7 +205,7 @@ struct Codes {
     __syncwarp();
 #pragma unroll
     for (int n = 0; n < kNt; ++n) {
-      const int h = 8 * n + g;
+      const int h = kPair ? g & 3 : 8 * n + g;
       uint4 q[kKc];
 #pragma unroll
       for (int p = 0; p < kKc; ++p) {
@@ -364,7 +395,7 @@ struct Codes {
       }
 #pragma unroll
       for (int r = 0; r < kRep; ++r) {
-        uint32_t pw[kNt][2][2];
+        uint32_t pw[kNt][kSecond][2];
 #pragma unroll
         for (int n = 0; n < kNt; ++n)
 #pragma unroll
@@ -372,8 +403,13 @@ struct Codes {
             const float w0 = s[r][n][2 * e] * wf[n][0], w1 = s[r][n][2 * e + 1] * wf[n][1];
             const uint32_t hi = pack2<false>(w0, w1);
             const float2 back = unpack2<false>(hi);
-            pw[n][0][e] = transpose8x8(hi);
-            pw[n][1][e] = transpose8x8(pack2<false>(w0 - back.x, w1 - back.y));
+            const uint32_t lo = pack2<false>(w0 - back.x, w1 - back.y);
+            if constexpr (kPair) {
+              pw[n][0][e] = transpose8x8(t < 2 ? hi : lo);
+            } else {
+              pw[n][0][e] = transpose8x8(hi);
+              pw[n][1][e] = transpose8x8(lo);
+            }
           }
 #pragma unroll
         for (int hh = 0; hh < kVc; ++hh) {
@@ -408,7 +444,7 @@ struct Codes {
 #pragma unroll
             for (int n = 0; n < kNt; ++n)
 #pragma unroll
-              for (int i = 0; i < 2; ++i)
+              for (int i = 0; i < kSecond; ++i)
                 mma16816<false>(o[n][hh][j], x[j][0], x[j][1], x[j][2], x[j][3], pw[n][i][0], pw[n][i][1]);
         }
       }
@@ -430,6 +466,14 @@ struct Codes {
             o[n][hh][j][i + 2] *= back;
           }
       }
+    if constexpr (kPair) {
+#pragma unroll
+      for (int hh = 0; hh < kVc; ++hh)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[0][hh][j][e] += __shfl_down_sync(0xFFFFFFFFu, o[0][hh][j][e], 2);
+    }
   }
 };
 

@@ -7,10 +7,13 @@ namespace {
 
 template <int kBits, int kDh>
 cudaError_t launch_for(const QuantAttnArgs& a, cudaStream_t stream, unsigned int* launches) {
-  const bool wide = a.H / a.kv.Hkv > 8, small = a.kv.page_log2 < 4;
-  if (small)
-    return wide ? launch<Codes<kBits, kDh, true>, 2>(a, stream, launches) : launch<Codes<kBits, kDh, true>, 1>(a, stream, launches);
-  return wide ? launch<Codes<kBits, kDh, false>, 2>(a, stream, launches) : launch<Codes<kBits, kDh, false>, 1>(a, stream, launches);
+  const int group = a.H / a.kv.Hkv;
+  const bool small = a.kv.page_log2 < 4;
+  if (group <= 4)
+    return small ? launch<Codes<kBits, kDh, true, true>, 1>(a, stream, launches) : launch<Codes<kBits, kDh, false, true>, 1>(a, stream, launches);
+  if (group <= 8)
+    return small ? launch<Codes<kBits, kDh, true, false>, 1>(a, stream, launches) : launch<Codes<kBits, kDh, false, false>, 1>(a, stream, launches);
+  return small ? launch<Codes<kBits, kDh, true, false>, 2>(a, stream, launches) : launch<Codes<kBits, kDh, false, false>, 2>(a, stream, launches);
 }
 
 }  // namespace
