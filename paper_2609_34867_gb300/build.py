@@ -1,7 +1,8 @@
 """Builds libp4q.so (the sm_103a kernels behind include/p4q.h) in-tree with nvcc.
 
 Each .cu under csrc/ is compiled in parallel for sm_103a only, then linked
-into paper_2609_34867_gb300/lib/libp4q.so. No fast-math: the quantizer and the
+into paper_2609_34867_gb300/lib/libp4q.so; the Python module of csrc/p4q_call.c, which
+marshals the calls of a decode step, goes beside it. No fast-math: the quantizer and the
 cosine rely on IEEE-rounded fp32 division and square root.
 """
 from __future__ import annotations
@@ -11,6 +12,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -18,6 +20,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIBDIR = os.path.join(PKG, "lib")
 LIB = os.path.join(LIBDIR, "libp4q.so")
+CALL = os.path.join(LIBDIR, "p4q_call.so")
 GENCODE = "-gencode=arch=compute_103a,code=sm_103a"
 
 
@@ -33,13 +36,13 @@ def sources():
 
 def _deps():
     return sources() + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(CSRC, "*.h")) + \
-        glob.glob(os.path.join(INCLUDE, "*.h"))
+        glob.glob(os.path.join(INCLUDE, "*.h")) + glob.glob(os.path.join(CSRC, "*.c"))
 
 
 def up_to_date() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(CALL):
         return False
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(CALL))
     return all(os.path.getmtime(p) <= t for p in _deps())
 
 
@@ -61,6 +64,11 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
         if verbose:
             print(" ".join(cmd), file=sys.stderr)
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+    call = f"{CALL}.tmp{os.getpid()}"
+    src = os.path.join(CSRC, "p4q_call.c")
+    cmd = [shutil.which("gcc") or "cc", "-O2", "-Wall", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"], "-I", INCLUDE,
+           src, "-o", call]
+    procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     failed = []
     for src, p in procs:
         out, _ = p.communicate()
@@ -74,6 +82,7 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
     # every symbol resolved at link time (a missing definition fails here, not at load)
     subprocess.run([nvcc(), GENCODE, "-shared", "-Xlinker", "--no-undefined", "-o", tmp] + objs, check=True)
     os.replace(tmp, LIB)
+    os.replace(call, CALL)
     return LIB
 
 

@@ -84,7 +84,7 @@ struct Codes {
   static constexpr float kLift = 0.0f;
   static constexpr float kMove = 8.0f;
   static constexpr int kSecond = kPair ? 1 : 2;    // products per operand of O^T
-  static __host__ __device__ constexpr int ctas(int nt) { return nt == 1 ? (kDh * kBits == 1024 || kSmallPage ? 3 : 4) : 2; }
+  static __host__ __device__ constexpr int ctas(int nt) { return nt == 1 ? (kDh * kBits == 1024 || kSmallPage ? 3 : 3) : 2; }
   static __device__ __forceinline__ bool bf16(const Args& a) { return a.bf16; }
   static __device__ __forceinline__ int first_own(const Args&, int, int) { return 0; }
   static __device__ __forceinline__ int table_row(const Args&, int b, int) { return b; }
@@ -99,7 +99,6 @@ struct Codes {
   static __device__ __forceinline__ void attend(const Args& a, const Unit& un, int tile, int tile_end,
                                                 uint4 (&sq)[kNt][kKc][32], Part<kNt, kVc>& acc) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const float c2 = a.scale * 1.4426950408889634f;
     const PagedCodes& c = a.kv;
     const int len = un.len, heads = un.heads;
     const int slots = (1 << c.page_log2) - 1;
@@ -111,6 +110,7 @@ struct Codes {
     const float* const ksh = c.k_scale + un.hk * c.scale_head_stride + kg * c.scale_token_stride;
     const float* const vsh = c.v_scale + un.hk * c.scale_head_stride + kg * c.scale_token_stride;
     const long long ts = c.token_stride, ts8 = 8 * c.token_stride, ss8 = 8 * c.scale_token_stride;
+    auto block_at = [&](int tl, int r) { return tl * kTile + (warp * kRep + r) * 16; };
 
     // The page of position j, -1 if it is not to be read.
     auto page_of = [&](int j) -> int {
@@ -124,59 +124,89 @@ struct Codes {
     };
 
     auto& o = acc.o;
-    auto& ref = acc.ref;
     auto& l = acc.l;
     uint32_t kr[kRep][2][kKw], vr[kRep][4][kVw];  // rows g, g + 8; 2 t, 2 t + 1, 2 t + 8, 2 t + 9
     float ks[kRep][2], vs[kRep][2];               // scales of rows g, g + 8
-    constexpr int kLook = kSmallPage ? 6 : 1;     // (pages of 16 and more: a block lies in one)
-    int pg[kRep][kLook];
+    // Pages of 16 and more: a block of 16 positions lies in one. Each lane has the place of one of the
+    // warp's next 32 blocks (and the page of one of the 32 after them), found once for all lanes.
+    constexpr int kStrip = 32 / kRep;             // tiles
+    int strip = tile, page_ahead = -1;
+    long long code_at = 0, scale_at = 0;
+    uint32_t found = 0;                           // the strip's blocks that are to be read
+    // Smaller pages: each row has a page.
+    int pg[kRep][6];
     auto look = [&](int tl) {
+      if constexpr (kSmallPage) {
 #pragma unroll
-      for (int r = 0; r < kRep; ++r) {
-        const int j = tl * kTile + (warp * kRep + r) * 16;
-        pg[r][0] = page_of(kSmallPage ? j + g : j);
-        if constexpr (kSmallPage) {
+        for (int r = 0; r < kRep; ++r) {
+          const int j = block_at(tl, r);
+          pg[r][0] = page_of(j + g);
           pg[r][1] = page_of(j + g + 8);
           pg[r][2] = page_of(j + 2 * t);
           pg[r][3] = page_of(j + 2 * t + 1);
           pg[r][4] = page_of(j + 2 * t + 8);
           pg[r][5] = page_of(j + 2 * t + 9);
         }
+      } else {
+        const int at = tl + lane / kRep;
+        page_ahead = at < tile_end ? page_of(block_at(at, lane % kRep)) : -1;
       }
     };
-    uint32_t live = 0;  // rows g, g + 8 of block r count: bits 2 r, 2 r + 1
-    const uint8_t* vp[kRep];
+    auto enter_strip = [&](int tl) {
+      strip = tl;
+      found = __ballot_sync(0xFFFFFFFFu, page_ahead >= 0);
+      const long long slot = block_at(0, lane % kRep) + (tl + lane / kRep) * kTile & slots;
+      code_at = page_ahead * c.page_stride + slot * ts;
+      scale_at = page_ahead * c.scale_page_stride + slot * c.scale_token_stride;
+      look(tl + kStrip);
+    };
+    // Which rows count, where not all of them do (all: bits 2 r, 2 r + 1 for rows g, g + 8 of block r).
+    constexpr uint32_t kAll = (1u << (2 * kRep)) - 1u;
+    uint32_t live = 0;
+    long long at[kRep];
     auto load_k = [&](int tl) {
-      live = 0;
+      if constexpr (kSmallPage) {
+        live = 0;
 #pragma unroll
-      for (int r = 0; r < kRep; ++r) {
-        const int j = tl * kTile + (warp * kRep + r) * 16;
-        if constexpr (kSmallPage) {
+        for (int r = 0; r < kRep; ++r) {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const int page = pg[r][e], slot = (j + g + 8 * e) & slots;
+            const int page = pg[r][e], slot = (block_at(tl, r) + g + 8 * e) & slots;
             if (page >= 0) {
               live |= 1u << (2 * r + e);
               load_words<kKw>(kr[r][e], kh + page * c.page_stride + slot * ts, 64);
-              const long long at = page * c.scale_page_stride + slot * c.scale_token_stride;
-              ks[r][e] = ksh[at];
-              vs[r][e] = vsh[at];
+              const long long place = page * c.scale_page_stride + slot * c.scale_token_stride;
+              ks[r][e] = ksh[place];
+              vs[r][e] = vsh[place];
             }
           }
-        } else if (pg[r][0] >= 0) {
-          // rows past the length are read too (they are the page's) but do not count
-          live |= (j + g < len ? 1u << (2 * r) : 0u) | (j + g + 8 < len ? 2u << (2 * r) : 0u);
-          const long long slot = j & slots, at = pg[r][0] * c.page_stride + slot * ts;
-          const long long sat = pg[r][0] * c.scale_page_stride + slot * c.scale_token_stride;
-          const uint8_t* const p = kh + at;
-          vp[r] = vh + at;
-          load_words<kKw>(kr[r][0], p, 64);
-          load_words<kKw>(kr[r][1], p + ts8, 64);
-          const float *kp = ksh + sat, *vq = vsh + sat;
-          ks[r][0] = *kp;
-          ks[r][1] = kp[ss8];
-          vs[r][0] = *vq;
-          vs[r][1] = vq[ss8];
+        }
+      } else {
+        if (tl - strip == kStrip) enter_strip(tl);
+        const int first = (tl - strip) * kRep;
+        const uint32_t mine = found >> first & ((1u << kRep) - 1u);
+        live = kAll;
+#pragma unroll
+        for (int r = 0; r < kRep; ++r) {
+          at[r] = __shfl_sync(0xFFFFFFFFu, code_at, first + r);
+          const long long sat = __shfl_sync(0xFFFFFFFFu, scale_at, first + r);
+          if (mine >> r & 1u) {  // (rows past the length are read too: they are the page's)
+            const uint8_t* const p = kh + at[r];
+            load_words<kKw>(kr[r][0], p, 64);
+            load_words<kKw>(kr[r][1], p + ts8, 64);
+            const float *kp = ksh + sat, *vp = vsh + sat;
+            ks[r][0] = *kp;
+            ks[r][1] = kp[ss8];
+            vs[r][0] = *vp;
+            vs[r][1] = vp[ss8];
+          }
+        }
+        if (mine != (1u << kRep) - 1u || block_at(tl, kRep) > len) {
+          live = 0;
+#pragma unroll
+          for (int r = 0; r < kRep; ++r)
+            if (mine >> r & 1u)
+              live |= (block_at(tl, r) + g < len ? 1u << (2 * r) : 0u) | (block_at(tl, r) + g + 8 < len ? 2u << (2 * r) : 0u);
         }
       }
     };
@@ -184,23 +214,25 @@ struct Codes {
 #pragma unroll
       for (int r = 0; r < kRep; ++r) {
         if constexpr (kSmallPage) {
-          const int j = tl * kTile + (warp * kRep + r) * 16;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int page = pg[r][2 + e], row = j + 2 * t + (e & 1) + 8 * (e >> 1);
+            const int page = pg[r][2 + e], row = block_at(tl, r) + 2 * t + (e & 1) + 8 * (e >> 1);
             if (page >= 0) load_words<kVw>(vr[r][e], vh + page * c.page_stride + (row & slots) * ts, 16);
           }
-        } else if (pg[r][0] >= 0) {
-          load_words<kVw>(vr[r][0], vp[r], 16);
-          load_words<kVw>(vr[r][1], vp[r] + ts, 16);
-          load_words<kVw>(vr[r][2], vp[r] + ts8, 16);
-          load_words<kVw>(vr[r][3], vp[r] + ts8 + ts, 16);
+        } else if (found >> ((tl - strip) * kRep + r) & 1u) {
+          const uint8_t* const p = vh + at[r];
+          load_words<kVw>(vr[r][0], p, 16);
+          load_words<kVw>(vr[r][1], p + ts, 16);
+          load_words<kVw>(vr[r][2], p + ts8, 16);
+          load_words<kVw>(vr[r][3], p + ts8 + ts, 16);
         }
       }
     };
 
     if (tile < tile_end) look(tile);
-    // q as fp16, and the factor that makes scores in powers of two of its products (heads 2 t, 2 t + 1)
+    // q as fp16 (times the sign of the scale, or 0), and the factor fq >= 0 that makes scores in powers of
+    // two of its products with a position's codes and scale (heads 2 t, 2 t + 1)
+    const float c2 = fabsf(a.scale * 1.4426950408889634f), sign = a.scale > 0.0f ? 1.0f : a.scale < 0.0f ? -1.0f : 0.0f;
     float fq[kNt][2];
     __syncwarp();
 #pragma unroll
@@ -213,7 +245,7 @@ struct Codes {
         if (h < heads)
           q[p] = *reinterpret_cast<const uint4*>(a.q + un.b * a.ldq + static_cast<long long>(un.h0 + h) * kDh + q_dim(p, t));
       }
-      float f = c2;
+      float f = c2 == 0.0f ? 1.0f : c2;
       if (a.bf16) {
         uint32_t most = 0;  // the largest finite |q|
         auto finite = [](uint32_t w) { return (w & 0x7F80u) == 0x7F80u ? 0u : w & 0x7FFFu; };
@@ -226,17 +258,24 @@ struct Codes {
         most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
         most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
         const int up = most == 0 ? 0 : min(100, 14 - (static_cast<int>(most >> 7) - 127));
-        const float by = __uint_as_float(static_cast<uint32_t>(127 + up) << 23);
-        f = c2 * __uint_as_float(static_cast<uint32_t>(127 - up) << 23);
+        const float by = sign * __uint_as_float(static_cast<uint32_t>(127 + up) << 23);
+        f *= __uint_as_float(static_cast<uint32_t>(127 - up) << 23);
         auto scaled = [by](uint32_t w) {
           const float2 v = unpack2<true>(w);
           return pack2<false>(v.x * by, v.y * by);
         };
 #pragma unroll
         for (int p = 0; p < kKc; ++p) q[p] = make_uint4(scaled(q[p].x), scaled(q[p].y), scaled(q[p].z), scaled(q[p].w));
+      } else if (sign != 1.0f) {
+        auto scaled = [sign](uint32_t w) {
+          const float2 v = unpack2<false>(w);
+          return pack2<false>(v.x * sign, v.y * sign);
+        };
+#pragma unroll
+        for (int p = 0; p < kKc; ++p) q[p] = make_uint4(scaled(q[p].x), scaled(q[p].y), scaled(q[p].z), scaled(q[p].w));
       }
 #pragma unroll
-      for (int e = 0; e < 2; ++e) fq[n][e] = __shfl_sync(0xFFFFFFFFu, f, 4 * (2 * t + e));
+      for (int e = 0; e < 2; ++e) fq[n][e] = fmaxf(0x1p-126f, __shfl_sync(0xFFFFFFFFu, f, 4 * (2 * t + e)));
 #pragma unroll
       for (int p = 0; p < kKc; ++p) {
         if (kBits == 4)  // the nibbles' pairs
@@ -247,10 +286,20 @@ struct Codes {
     }
     __syncwarp();
     if (tile < tile_end) {
+      if constexpr (!kSmallPage) enter_strip(tile);
       load_k(tile);
       load_v(tile);
-      look(tile + 1);
+      if constexpr (kSmallPage) look(tile + 1);
     }
+    // The reference is the product `top` that a head's p are 1 at; it moves at `limit`, 2^kMove above.
+    float top[kNt][2], limit[kNt][2], back_to[kNt][2];
+#pragma unroll
+    for (int n = 0; n < kNt; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        top[n][e] = limit[n][e] = -INFINITY;
+        back_to[n][e] = 0.0f;  // -top fq
+      }
     // Weights p sv of a head count times wf, at most 2^15; room = 2^15 / wf (0 and 0: none has been seen yet).
     float wf[kNt][2], room[kNt][2];
 #pragma unroll
@@ -301,15 +350,15 @@ struct Codes {
       for (int r = 0; r < kRep; ++r)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          sv[r][e] = fabsf(vs[r][e]) <= 3.402823466e38f ? vs[r][e] : __int_as_float(0x7FFFFFFF);
+          sv[r][e] = vs[r][e];
 #pragma unroll
-          for (int n = 0; n < kNt; ++n)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) s[r][n][2 * e + i] *= ks[r][e] * fq[n][i];
+          for (int n = 0; n < kNt; ++n) {
+            s[r][n][2 * e] *= ks[r][e];
+            s[r][n][2 * e + 1] *= ks[r][e];
+          }
         }
       if (more) load_k(tl + 1);
-      constexpr uint32_t kAll = (1u << (2 * kRep)) - 1u;
-      if (!__all_sync(0xFFFFFFFFu, counts == kAll)) {
+      if (kSmallPage ? !__all_sync(0xFFFFFFFFu, counts == kAll) : counts != kAll) {
 #pragma unroll
         for (int r = 0; r < kRep; ++r)
 #pragma unroll
@@ -320,25 +369,28 @@ struct Codes {
               for (int n = 0; n < kNt; ++n) s[r][n][2 * e] = s[r][n][2 * e + 1] = -INFINITY;
             }
       }
+      __syncwarp();
       bool move = false;
 #pragma unroll
       for (int r = 0; r < kRep; ++r)
 #pragma unroll
         for (int n = 0; n < kNt; ++n)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) move = move || s[r][n][e] > ref[n][e & 1] + kMove;
+          for (int e = 0; e < 4; ++e) move = move || s[r][n][e] > limit[n][e & 1];
       if (__any_sync(0xFFFFFFFFu, move)) {
 #pragma unroll
         for (int n = 0; n < kNt; ++n)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            float m = ref[n][e];
+            float m = top[n][e];
 #pragma unroll
             for (int r = 0; r < kRep; ++r) m = fmaxf(m, fmaxf(s[r][n][e], s[r][n][e + 2]));
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
-            const float alpha = m == ref[n][e] ? 1.0f : exp2_fast(ref[n][e] - m);
-            ref[n][e] = m;
+            const float alpha = m == top[n][e] ? 1.0f : exp2_fast((top[n][e] - m) * fq[n][e]);
+            top[n][e] = m;
+            limit[n][e] = m == -INFINITY ? -INFINITY : m + kMove / fq[n][e];
+            back_to[n][e] = m == -INFINITY ? 0.0f : -m * fq[n][e];
             l[n][e] *= alpha;
 #pragma unroll
             for (int hh = 0; hh < kVc; ++hh)
@@ -354,18 +406,16 @@ struct Codes {
 #pragma unroll
       for (int n = 0; n < kNt; ++n)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const float from = ref[n][i] == -INFINITY ? 0.0f : ref[n][i];
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int r = 0; r < kRep; ++r)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const float p = exp2_fast(s[r][n][2 * e + i] - from);
+              const float p = exp2_fast(fmaf(s[r][n][2 * e + i], fq[n][i], back_to[n][i]));
               l[n][i] += p;
               s[r][n][2 * e + i] = p * sv[r][e];
               move = move || fabsf(s[r][n][2 * e + i]) > room[n][i];
             }
-        }
       if (__any_sync(0xFFFFFFFFu, move)) {
 #pragma unroll
         for (int n = 0; n < kNt; ++n)
@@ -450,13 +500,14 @@ struct Codes {
       }
       if (more) {
         load_v(tl + 1);
-        look(tl + 2);
+        if constexpr (kSmallPage) look(tl + 2);
       }
     }
 #pragma unroll
     for (int n = 0; n < kNt; ++n)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
+        acc.ref[n][i] = top[n][i] * fq[n][i];
         const float back = room[n][i] == 0.0f ? 1.0f : room[n][i] * 0x1p-15f;  // 1 / wf
 #pragma unroll
         for (int hh = 0; hh < kVc; ++hh)

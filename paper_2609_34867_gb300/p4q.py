@@ -9,6 +9,8 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import importlib.machinery
+import importlib.util
 import os
 import struct
 
@@ -127,6 +129,27 @@ def lib() -> ctypes.CDLL:
         L.p4q_sample.restype = st
         _lib = L
     return _lib
+
+
+_fast = None
+
+
+def _call():
+    """csrc/p4q_call.c, bound to the library: the calls that sit in a decode loop. Its functions take
+    a wrapper's arguments by position and give the status, or -1 for arguments that the
+    wrapper's own checks are to refuse."""
+    global _fast
+    if _fast is None:
+        L = lib()
+        loader = importlib.machinery.ExtensionFileLoader("p4q_call", _build.CALL)
+        module = importlib.util.module_from_spec(importlib.util.spec_from_loader("p4q_call", loader))
+        loader.exec_module(module)
+        module.bind(tuple(ctypes.cast(f, ctypes.c_void_p).value for f in (
+            L.p4q_rope_append_quant, L.p4q_paged_attention_quant, L.p4q_prefix_attention)),
+            (torch.float16, torch.bfloat16, torch.float32, torch.int32, torch.int8, torch.uint8),
+            torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice)
+        _fast = module
+    return _fast
 
 
 # Pointers and streams go to ctypes as plain integers (the argtypes make them
@@ -613,6 +636,12 @@ def p4q_rope_append_quant(q, k, v, cos, sin, pos, k_cache, v_cache, k_scale, v_s
     heads in memory (side by side scales of a page's slots are read fastest). q, k, v
     fp16 or bf16; k_out, v_out [T, Hkv*dh], optional, take the values that the codes stand for, and may
     be k and v. Other arguments as p4q_rope_append."""
+    status = (_fast or _call()).rope_append_quant(q, k, v, cos, sin, pos, k_cache, v_cache, k_scale, v_scale, table, q_out,
+                                                  k_out, v_out, seq, rot_pos, interleaved, stream)
+    if status == P4Q_OK:
+        return
+    if status > 0:
+        raise P4QError(status, "p4q_rope_append_quant")
     kv, heads, dh, _ = _paged_kvq(k_cache, v_cache, k_scale, v_scale, table)
     dt = _row_type(q, "q")
     ldq = _rows(q, dt, None, None, "q")
@@ -641,6 +670,12 @@ def p4q_paged_attention_quant(q, k_cache, v_cache, k_scale, v_scale, table, lens
     """p4q_paged_attention over a paged cache of codes (caches and scales as in
     p4q_rope_append_quant); q, o [seqs, H*dh] fp16 or bf16. Other arguments and the
     workspace as p4q_paged_attention."""
+    status = (_fast or _call()).paged_attention_quant(q, k_cache, v_cache, k_scale, v_scale, table, lens, o, ws, scale, lse,
+                                                      stream)
+    if status == P4Q_OK:
+        return
+    if status > 0:
+        raise P4QError(status, "p4q_paged_attention_quant")
     kv, heads, dh, seqs = _paged_kvq(k_cache, v_cache, k_scale, v_scale, table)
     dt = _row_type(q, "q")
     ldq = _rows(q, dt, seqs, None, "q")
@@ -686,6 +721,12 @@ def p4q_prefix_attention(q, k_cache, v_cache, table, lens, group_start, prefix_l
     their first prefix_lens[g] positions, which lie in the pages of the first of them and are read
     once for all; group_start [groups + 1], prefix_lens [groups] int32; ws as
     prefix_attention_workspace() gives it; other arguments as p4q_paged_attention."""
+    status = (_fast or _call()).prefix_attention(q, k_cache, v_cache, table, lens, group_start, prefix_lens, o, ws, scale, lse,
+                                                 stream)
+    if status == P4Q_OK:
+        return
+    if status > 0:
+        raise P4QError(status, "p4q_prefix_attention")
     kv, dt, heads, dh, seqs = _paged_kv(k_cache, v_cache, table)
     ldq = _rows(q, dt, seqs, None, "q")
     width = q.shape[1]
