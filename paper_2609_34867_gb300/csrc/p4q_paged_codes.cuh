@@ -25,10 +25,21 @@
 namespace p4q {
 namespace paged {
 
+// Constants that the compiler is to keep in registers: an instruction has room for one of its own, and
+// it would rather use two of these (64 more per block of 16 positions at 4 bits).
+struct Magic {
+  uint32_t lo, hi, bytes;
+  __device__ __forceinline__ Magic() {
+    asm volatile("mov.b32 %0, 0x64086408;" : "=r"(lo));
+    asm volatile("mov.b32 %0, 0x64806480;" : "=r"(hi));
+    asm volatile("mov.b32 %0, 0x64646464;" : "=r"(bytes));
+  }
+};
+
 // Two codes as fp16 pairs. Bytes 2 half, 2 half + 1 of a word whose sign bits are flipped.
 template <int kHalf>
-__device__ __forceinline__ uint32_t codes8(uint32_t flipped) {
-  const uint32_t v = __byte_perm(flipped, 0x64646464u, kHalf ? 0x4342 : 0x4140);  // 1024 + 128 + c
+__device__ __forceinline__ uint32_t codes8(uint32_t flipped, const Magic& k) {
+  const uint32_t v = __byte_perm(flipped, k.bytes, kHalf ? 0x4342 : 0x4140);  // 1024 + 128 + c
   const uint32_t bias = 0x64806480u;
   const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&v), *reinterpret_cast<const __half2*>(&bias));
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -36,14 +47,17 @@ __device__ __forceinline__ uint32_t codes8(uint32_t flipped) {
 
 // Nibbles kOdd of both 16-bit halves (0: bits 0 - 3, 1: bits 4 - 7).
 template <int kOdd>
-__device__ __forceinline__ uint32_t codes4(uint32_t w) {
+__device__ __forceinline__ uint32_t codes4(uint32_t w, const Magic& k) {
   __half2 h;
+  uint32_t v;
   if (kOdd) {
-    const uint32_t v = (w & 0x00F000F0u) ^ 0x64806480u, f = 0x2C002C00u, bias = 0xD480D480u;  // 1024 + 16 (8 + c); 1/16; -72
+    const uint32_t f = 0x2C002C00u, bias = 0xD480D480u;
+    asm("lop3.b32 %0, %1, 0x00F000F0, %2, 0x6A;" : "=r"(v) : "r"(w), "r"(k.hi));  // 1024 + 16 (8 + c); 1/16; -72
     h = __hfma2(*reinterpret_cast<const __half2*>(&v), *reinterpret_cast<const __half2*>(&f),
                 *reinterpret_cast<const __half2*>(&bias));
   } else {
-    const uint32_t v = (w & 0x000F000Fu) ^ 0x64086408u, bias = 0x64086408u;  // 1024 + 8 + c
+    const uint32_t bias = 0x64086408u;
+    asm("lop3.b32 %0, %1, 0x000F000F, %2, 0x6A;" : "=r"(v) : "r"(w), "r"(k.lo));  // 1024 + 8 + c
     h = __hsub2(*reinterpret_cast<const __half2*>(&v), *reinterpret_cast<const __half2*>(&bias));
   }
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -54,17 +68,21 @@ __device__ __forceinline__ void load_words(uint32_t (&w)[kWords], const uint8_t*
   if constexpr (kWords >= 4) {
 #pragma unroll
     for (int i = 0; i < kWords; i += 4) {
-      const uint4 v = ldg_stream16(p + (i / 4) * piece_stride);
-      w[i] = v.x;
-      w[i + 1] = v.y;
-      w[i + 2] = v.z;
-      w[i + 3] = v.w;
+      asm volatile("ld.global.L1::no_allocate.L2::64B.v4.u32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3])
+                   : "l"(p + (i / 4) * piece_stride));
     }
   } else if constexpr (kWords == 2) {
-    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
+    asm volatile("ld.global.L1::no_allocate.L2::64B.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
   } else {
-    asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(w[0]) : "l"(p));
+    asm volatile("ld.global.L1::no_allocate.L2::64B.u32 %0, [%1];" : "=r"(w[0]) : "l"(p));
   }
+}
+
+__device__ __forceinline__ float load_scale(const float* p) {
+  float v;
+  asm volatile("ld.global.L2::64B.f32 %0, [%1];" : "=f"(v) : "l"(p));
+  return v;
 }
 
 // kPair: at most four heads to a key/value head's unit. Columns 4 - 7 of the products, which would be
@@ -73,7 +91,7 @@ __device__ __forceinline__ void load_words(uint32_t (&w)[kWords], const uint8_t*
 template <int kBits, int kDhRows, bool kSmallPage, bool kPair>
 struct Codes {
   typedef QuantAttnArgs Args;
-  static constexpr bool kOwnOnly = false;
+  static constexpr bool kOwnOnly = false, kHeadsOuter = true;
   static constexpr int kDh = kDhRows;
   static constexpr int kRep = kDh * kBits == 256 && !kSmallPage ? 4 : 2;  // blocks of 16 positions per warp and tile
   static constexpr int kTile = 16 * kRep * kWarps;
@@ -100,6 +118,7 @@ struct Codes {
                                                 uint4 (&sq)[kNt][kKc][32], Part<kNt, kVc>& acc) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const PagedCodes& c = a.kv;
+    const Magic magic;
     const int len = un.len, heads = un.heads;
     const int slots = (1 << c.page_log2) - 1;
     // Where the lane's rows of a block begin: row g (and g + 8) of keys and scales, rows 2 t (2 t + 1,
@@ -176,8 +195,8 @@ struct Codes {
               live |= 1u << (2 * r + e);
               load_words<kKw>(kr[r][e], kh + page * c.page_stride + slot * ts, 64);
               const long long place = page * c.scale_page_stride + slot * c.scale_token_stride;
-              ks[r][e] = ksh[place];
-              vs[r][e] = vsh[place];
+              ks[r][e] = load_scale(ksh + place);
+              vs[r][e] = load_scale(vsh + place);
             }
           }
         }
@@ -195,10 +214,10 @@ struct Codes {
             load_words<kKw>(kr[r][0], p, 64);
             load_words<kKw>(kr[r][1], p + ts8, 64);
             const float *kp = ksh + sat, *vp = vsh + sat;
-            ks[r][0] = *kp;
-            ks[r][1] = kp[ss8];
-            vs[r][0] = *vp;
-            vs[r][1] = vp[ss8];
+            ks[r][0] = load_scale(kp);
+            ks[r][1] = load_scale(kp + ss8);
+            vs[r][0] = load_scale(vp);
+            vs[r][1] = load_scale(vp + ss8);
           }
         }
         if (mine != (1u << kRep) - 1u || block_at(tl, kRep) > len) {
@@ -325,16 +344,16 @@ struct Codes {
           for (int e = 0; e < 2; ++e) {
             if constexpr (kBits == 8) {
               const uint32_t w0 = kr[r][e][2 * p] ^ 0x80808080u, w1 = kr[r][e][2 * p + 1] ^ 0x80808080u;
-              x[e][0] = codes8<0>(w0);
-              x[e][1] = codes8<1>(w0);
-              x[e][2] = codes8<0>(w1);
-              x[e][3] = codes8<1>(w1);
+              x[e][0] = codes8<0>(w0, magic);
+              x[e][1] = codes8<1>(w0, magic);
+              x[e][2] = codes8<0>(w1, magic);
+              x[e][3] = codes8<1>(w1, magic);
             } else {
               const uint32_t w = kr[r][e][p];
-              x[e][0] = codes4<0>(w);
-              x[e][1] = codes4<1>(w);
-              x[e][2] = codes4<0>(w >> 8);
-              x[e][3] = codes4<1>(w >> 8);
+              x[e][0] = codes4<0>(w, magic);
+              x[e][1] = codes4<1>(w, magic);
+              x[e][2] = codes4<0>(w >> 8, magic);
+              x[e][3] = codes4<1>(w >> 8, magic);
             }
           }
 #pragma unroll
@@ -471,22 +490,22 @@ struct Codes {
               for (int i = 0; i < 2; ++i) {
                 const uint32_t w0 = vr[r][2 * e][2 * hh + i], w1 = vr[r][2 * e + 1][2 * hh + i];
                 const uint32_t lo = __byte_perm(w0, w1, 0x5140) ^ 0x80808080u, hi = __byte_perm(w0, w1, 0x7362) ^ 0x80808080u;
-                x[2 * i][2 * e] = codes8<0>(lo);
-                x[2 * i][2 * e + 1] = codes8<1>(lo);
-                x[2 * i + 1][2 * e] = codes8<0>(hi);
-                x[2 * i + 1][2 * e + 1] = codes8<1>(hi);
+                x[2 * i][2 * e] = codes8<0>(lo, magic);
+                x[2 * i][2 * e + 1] = codes8<1>(lo, magic);
+                x[2 * i + 1][2 * e] = codes8<0>(hi, magic);
+                x[2 * i + 1][2 * e + 1] = codes8<1>(hi, magic);
               }
             } else {
               const uint32_t w0 = vr[r][2 * e][hh], w1 = vr[r][2 * e + 1][hh];
               const uint32_t lo = __byte_perm(w0, w1, 0x5410), hi = __byte_perm(w0, w1, 0x7632);
-              x[0][2 * e] = codes4<0>(lo);
-              x[0][2 * e + 1] = codes4<1>(lo);
-              x[1][2 * e] = codes4<0>(lo >> 8);
-              x[1][2 * e + 1] = codes4<1>(lo >> 8);
-              x[2][2 * e] = codes4<0>(hi);
-              x[2][2 * e + 1] = codes4<1>(hi);
-              x[3][2 * e] = codes4<0>(hi >> 8);
-              x[3][2 * e + 1] = codes4<1>(hi >> 8);
+              x[0][2 * e] = codes4<0>(lo, magic);
+              x[0][2 * e + 1] = codes4<1>(lo, magic);
+              x[1][2 * e] = codes4<0>(lo >> 8, magic);
+              x[1][2 * e + 1] = codes4<1>(lo >> 8, magic);
+              x[2][2 * e] = codes4<0>(hi, magic);
+              x[2][2 * e + 1] = codes4<1>(hi, magic);
+              x[3][2 * e] = codes4<0>(hi >> 8, magic);
+              x[3][2 * e + 1] = codes4<1>(hi >> 8, magic);
             }
           }
 #pragma unroll

@@ -53,7 +53,8 @@ __device__ __forceinline__ void write_out(const typename C::Args& a, int b, int 
 struct Plan {
   unsigned long long q, r;
   unsigned long long first;  // this CTA's
-  unsigned long long at;     // the tiles of the sequences before b
+  unsigned long long at;     // where the units of sequence b begin (kHeadsOuter: unit u of it)
+  int u;                     // (kHeadsOuter)
   int b;                     // the sequence that `first` lies in
   int pieces;                // 1: a CTA for each kMinTiles of a unit; 0: equal ranges
 };
@@ -153,15 +154,18 @@ __global__ void __launch_bounds__(kThreads, C::ctas(kNt)) paged_attention_kernel
     }
     const u64 q = pieces ? kMinTiles : quotient(total, gridDim.x), r = pieces ? 0 : total - q * gridDim.x;
     const u64 first = cta * q + min(cta, r);
+    const u64 each = C::kHeadsOuter ? 1 : units;  // units of a sequence that lie side by side
+    const int outer = C::kHeadsOuter ? static_cast<int>(quotient(first, total / units)) : 0;
+    const u64 before = outer * (total / units);
     if (tid == 0) split[blockIdx.x] = make_int4(0, 0, -1, 0);
     if (first >= total) {  // (the whole CTA)
       if (C::kOwnOnly) pdl_wait();
       return;
     }
-    if (first >= (upto - mine) * units && first < upto * units) {
-      u64 at = (upto - mine) * units;
+    if (first - before >= (upto - mine) * each && first - before < upto * each) {
+      u64 at = (upto - mine) * each + before;
       for (int i = b0; i < b1; ++i) {
-        const u64 n = static_cast<u64>(span_of(tiles_of(length(i) - base_of(i)), pieces)) * units;
+        const u64 n = static_cast<u64>(span_of(tiles_of(length(i) - base_of(i)), pieces)) * each;
         if (first < at + n) {
           plan.b = i;
           break;
@@ -173,16 +177,18 @@ __global__ void __launch_bounds__(kThreads, C::ctas(kNt)) paged_attention_kernel
       plan.first = first;
       plan.at = at;
       plan.pieces = pieces;
+      plan.u = outer;
     }
     __syncthreads();
     x = plan.first;
     last = x + plan.q + (blockIdx.x < plan.r ? 1 : 0);
     b = plan.b;
     const int span = span_of(tiles_of(length(b) - base_of(b)), plan.pieces);
-    u = static_cast<int>(quotient(x - plan.at, span));
-    tile = static_cast<int>(x - plan.at - static_cast<unsigned long long>(u) * span);
+    const int at = C::kHeadsOuter ? 0 : static_cast<int>(quotient(x - plan.at, span));
+    u = plan.u + at;
+    tile = static_cast<int>(x - plan.at - static_cast<unsigned long long>(at) * span);
   }
-  while (x < last && b < c.seqs) {
+  while (x < last && (C::kHeadsOuter ? u < units : b < c.seqs)) {
     const int len = length(b), base = base_of(b), tiles = tiles_of(len - base);
     int stop, tile_end;
     if (kCluster) {  // the CTA's share of the unit (none: a part of no weight)
@@ -195,7 +201,12 @@ __global__ void __launch_bounds__(kThreads, C::ctas(kNt)) paged_attention_kernel
     auto next_unit = [&]() {
       x += stop - tile;
       tile = 0;
-      if (++u == units) {
+      if (C::kHeadsOuter) {
+        if (++b == c.seqs) {
+          b = 0;
+          ++u;
+        }
+      } else if (++u == units) {
         u = 0;
         ++b;
       }
@@ -529,7 +540,8 @@ cudaError_t launch(const typename C::Args& a, cudaStream_t stream, unsigned int*
     if ((room + cs - 1) / cs <= units * room / (3 * wave) + kJoinTiles)
       return launch_clusters<C, kNt>(a, static_cast<int>(units), cs, stream, launches);
   }
-  const int grid = room >= wave || units >= wave ? wave : static_cast<int>(std::min<long long>(wave, units * room));
+  int grid = room >= wave || units >= wave ? wave : static_cast<int>(std::min<long long>(wave, units * room));
+  if (C::kHeadsOuter && grid >= 8 * (units / a.kv.seqs)) grid -= grid % static_cast<int>(units / a.kv.seqs);
   cudaError_t e = launch_pdl(kernel, dim3(static_cast<unsigned>(grid)), dim3(kThreads), smem, stream, a);
   if (e != cudaSuccess) return e;
   ++*launches;
