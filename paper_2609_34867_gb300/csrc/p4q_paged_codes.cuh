@@ -63,26 +63,23 @@ __device__ __forceinline__ uint32_t codes4(uint32_t w, const Magic& k) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-template <int kWords>
-__device__ __forceinline__ void load_words(uint32_t (&w)[kWords], const uint8_t* p, int piece_stride) {
-  if constexpr (kWords >= 4) {
-#pragma unroll
-    for (int i = 0; i < kWords; i += 4) {
-      asm volatile("ld.global.L1::no_allocate.L2::64B.v4.u32 {%0, %1, %2, %3}, [%4];"
-                   : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3])
-                   : "l"(p + (i / 4) * piece_stride));
-    }
-  } else if constexpr (kWords == 2) {
-    asm volatile("ld.global.L1::no_allocate.L2::64B.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
-  } else {
-    asm volatile("ld.global.L1::no_allocate.L2::64B.u32 %0, [%1];" : "=r"(w[0]) : "l"(p));
-  }
+// Asynchronous copies to shared memory, fetched 64 bytes at a time: a fetch of the whole 128-byte line
+// moved 1.65 times the bytes from HBM where a position's codes are 64 and other heads' lie between.
+__device__ __forceinline__ void copy16(uint32_t dst, const uint8_t* src) {
+  asm volatile("cp.async.cg.shared.global.L2::64B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t dst, const float* src) {
+  asm volatile("cp.async.ca.shared.global.L2::64B [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
 
-__device__ __forceinline__ float load_scale(const float* p) {
-  float v;
-  asm volatile("ld.global.L2::64B.f32 %0, [%1];" : "=f"(v) : "l"(p));
-  return v;
+template <int kWords>
+__device__ __forceinline__ void read_words(uint32_t* w, uint32_t at) {
+  if constexpr (kWords == 4)
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
+  else if constexpr (kWords == 2)
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at) : "memory");
+  else
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(at) : "memory");
 }
 
 // kPair: at most four heads to a key/value head's unit. Columns 4 - 7 of the products, which would be
@@ -93,42 +90,55 @@ struct Codes {
   typedef QuantAttnArgs Args;
   static constexpr bool kOwnOnly = false, kHeadsOuter = true;
   static constexpr int kDh = kDhRows;
-  static constexpr int kRep = kDh * kBits == 256 && !kSmallPage ? 4 : 2;  // blocks of 16 positions per warp and tile
+  static constexpr int kRep = kDh * kBits == 1024 ? 1 : kDh * kBits == 256 && !kSmallPage ? 4 : 2;  // blocks of 16 positions per warp and tile
   static constexpr int kTile = 16 * kRep * kWarps;
   static constexpr int kKc = kDh / 32;             // pieces of q per lane, 8 dimensions each
   static constexpr int kVc = kDh / 64;
   static constexpr int kKw = kDh * kBits / 128;    // words of a key row per lane
   static constexpr int kVw = kDh * kBits / 256;    // of a value row
+  static constexpr int kRow = kDh * kBits / 8;     // bytes of a row
+  static constexpr int kChunks = kRow / 16;        // copies of 16 bytes for it
+  static constexpr int kAtOnce = 32 / kChunks;     // rows that a warp copies at once
+  static constexpr int kBlock = 32 * kRow + 128;   // bytes of 16 positions: keys, values, scales
+  static constexpr int kStages = 3;
+  // Floats of a warp's ring of stages; its part of O takes their place in the end.
+  static __host__ __device__ constexpr int warp_floats(int nt) {
+    return kStages * kRep * kBlock / 4 > 8 * nt * kDh ? kStages * kRep * kBlock / 4 : 8 * nt * kDh;
+  }
+  // Where chunk ch of row r lies in a row's place: eight lanes that read rows and chunks as the
+  // products want them find them in eight banks' groups.
+  static __device__ __forceinline__ int place(int r, int ch) {
+    return r * kRow + ((kChunks == 8 ? ch ^ (r & 7) : kChunks == 4 ? ch ^ (r >> 1 & 3) : ch) << 4);
+  }
   static constexpr float kLift = 0.0f;
   static constexpr float kMove = 8.0f;
   static constexpr int kSecond = kPair ? 1 : 2;    // products per operand of O^T
-  static __host__ __device__ constexpr int ctas(int nt) { return nt == 1 ? (kDh * kBits == 1024 || kSmallPage ? 3 : 3) : 2; }
+  static __host__ __device__ constexpr int ctas(int nt) { return nt == 1 ? 3 : 2; }
   static __device__ __forceinline__ bool bf16(const Args& a) { return a.bf16; }
   static __device__ __forceinline__ int first_own(const Args&, int, int) { return 0; }
   static __device__ __forceinline__ int table_row(const Args&, int b, int) { return b; }
   static __device__ __forceinline__ void add_prefix(const Args&, int, int, int, float&, float&, float4&) {}
   static __device__ __forceinline__ int first_dim(int hh, int g) { return (kDh / 8) * g + 8 * hh; }
   // The dimensions of q's piece p that lane t's keys have.
-  static __device__ __forceinline__ int q_dim(int p, int t) {
-    return kBits == 4 ? (kDh / 4) * t + 8 * p : kDh == 128 ? 64 * (p >> 1) + 16 * t + 8 * (p & 1) : 16 * t + 8 * p;
-  }
+  static __device__ __forceinline__ int q_dim(int p, int t) { return (kDh / 4) * t + 8 * p; }
 
   template <int kNt>
   static __device__ __forceinline__ void attend(const Args& a, const Unit& un, int tile, int tile_end,
-                                                uint4 (&sq)[kNt][kKc][32], Part<kNt, kVc>& acc) {
+                                                uint4 (&sq)[kNt][kKc][32], float* ring, Part<kNt, kVc>& acc) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const PagedCodes& c = a.kv;
     const Magic magic;
     const int len = un.len, heads = un.heads;
     const int slots = (1 << c.page_log2) - 1;
-    // Where the lane's rows of a block begin: row g (and g + 8) of keys and scales, rows 2 t (2 t + 1,
-    // 2 t + 8, 2 t + 9) of values. With small pages the rows are added at the load.
-    const int kg = kSmallPage ? 0 : g, vg = kSmallPage ? 0 : 2 * t;
-    const uint8_t* const kh = c.k + un.hk * c.head_stride + kg * c.token_stride + t * (kKw >= 4 ? 16 : 4 * kKw);
-    const uint8_t* const vh = c.v + un.hk * c.head_stride + vg * c.token_stride + g * (4 * kVw);
-    const float* const ksh = c.k_scale + un.hk * c.scale_head_stride + kg * c.scale_token_stride;
-    const float* const vsh = c.v_scale + un.hk * c.scale_head_stride + kg * c.scale_token_stride;
-    const long long ts = c.token_stride, ts8 = 8 * c.token_stride, ss8 = 8 * c.scale_token_stride;
+    // The lane copies chunk `chunk` of rows `sub`, sub + kAtOnce, .. of keys and values, and of the scales of
+    // row lane % 16 the key's (lanes 0 - 15) or the value's. With small pages the rows are added at the copy.
+    const int chunk = lane % kChunks, sub = lane / kChunks;
+    const long long ts = c.token_stride, ss = c.scale_token_stride;
+    const uint8_t* const kh = c.k + un.hk * c.head_stride + (kSmallPage ? 0 : sub * ts) + 16 * chunk;
+    const uint8_t* const vh = c.v + un.hk * c.head_stride + (kSmallPage ? 0 : sub * ts) + 16 * chunk;
+    const float* const sh = (lane < 16 ? c.k_scale : c.v_scale) + un.hk * c.scale_head_stride + (kSmallPage ? 0 : (lane & 15) * ss);
+    const uint32_t slots_at = smem_u32(ring);
+    const uint32_t scale_to = 32 * kRow + 4 * (16 * (lane >> 4) + 2 * (lane & 7) + (lane >> 3 & 1));  // rows g, g + 8 side by side
     auto block_at = [&](int tl, int r) { return tl * kTile + (warp * kRep + r) * 16; };
 
     // The page of position j, -1 if it is not to be read.
@@ -144,111 +154,97 @@ struct Codes {
 
     auto& o = acc.o;
     auto& l = acc.l;
-    uint32_t kr[kRep][2][kKw], vr[kRep][4][kVw];  // rows g, g + 8; 2 t, 2 t + 1, 2 t + 8, 2 t + 9
-    float ks[kRep][2], vs[kRep][2];               // scales of rows g, g + 8
-    // Pages of 16 and more: a block of 16 positions lies in one. Each lane has the place of one of the
-    // warp's next 32 blocks (and the page of one of the 32 after them), found once for all lanes.
-    constexpr int kStrip = 32 / kRep;             // tiles
+    // Pages of 16 and more: a block of 16 positions lies in one, and each lane has the place of one of
+    // the warp's next 32 blocks (and the page of one of the 32 after them), found once for all lanes.
+    // Smaller pages: of one of the next 32 positions.
+    static_assert(!kSmallPage || kRep <= 2, "at most 32 positions of a warp in a tile");
+    constexpr int kStrip = kSmallPage ? 1 : 32 / kRep;  // tiles
     int strip = tile, page_ahead = -1;
     long long code_at = 0, scale_at = 0;
-    uint32_t found = 0;                           // the strip's blocks that are to be read
-    // Smaller pages: each row has a page.
-    int pg[kRep][6];
+    uint32_t found = 0;  // the strip's blocks (positions) that are to be read
+    auto mine_at = [&](int tl) { return kSmallPage ? block_at(tl, 0) + lane : block_at(tl + lane / kRep, lane % kRep); };
     auto look = [&](int tl) {
-      if constexpr (kSmallPage) {
-#pragma unroll
-        for (int r = 0; r < kRep; ++r) {
-          const int j = block_at(tl, r);
-          pg[r][0] = page_of(j + g);
-          pg[r][1] = page_of(j + g + 8);
-          pg[r][2] = page_of(j + 2 * t);
-          pg[r][3] = page_of(j + 2 * t + 1);
-          pg[r][4] = page_of(j + 2 * t + 8);
-          pg[r][5] = page_of(j + 2 * t + 9);
-        }
-      } else {
-        const int at = tl + lane / kRep;
-        page_ahead = at < tile_end ? page_of(block_at(at, lane % kRep)) : -1;
-      }
+      page_ahead = tl + (kSmallPage ? 0 : lane / kRep) < tile_end && (!kSmallPage || lane < 16 * kRep) ? page_of(mine_at(tl)) : -1;
     };
     auto enter_strip = [&](int tl) {
       strip = tl;
       found = __ballot_sync(0xFFFFFFFFu, page_ahead >= 0);
-      const long long slot = block_at(0, lane % kRep) + (tl + lane / kRep) * kTile & slots;
+      const long long slot = mine_at(tl) & slots;
       code_at = page_ahead * c.page_stride + slot * ts;
-      scale_at = page_ahead * c.scale_page_stride + slot * c.scale_token_stride;
+      scale_at = page_ahead * c.scale_page_stride + slot * ss;
       look(tl + kStrip);
     };
-    // Which rows count, where not all of them do (all: bits 2 r, 2 r + 1 for rows g, g + 8 of block r).
-    constexpr uint32_t kAll = (1u << (2 * kRep)) - 1u;
-    uint32_t live = 0;
-    long long at[kRep];
-    auto load_k = [&](int tl) {
-      if constexpr (kSmallPage) {
-        live = 0;
-#pragma unroll
-        for (int r = 0; r < kRep; ++r) {
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int page = pg[r][e], slot = (block_at(tl, r) + g + 8 * e) & slots;
-            if (page >= 0) {
-              live |= 1u << (2 * r + e);
-              load_words<kKw>(kr[r][e], kh + page * c.page_stride + slot * ts, 64);
-              const long long place = page * c.scale_page_stride + slot * c.scale_token_stride;
-              ks[r][e] = load_scale(ksh + place);
-              vs[r][e] = load_scale(vsh + place);
-            }
-          }
-        }
-      } else {
-        if (tl - strip == kStrip) enter_strip(tl);
-        const int first = (tl - strip) * kRep;
-        const uint32_t mine = found >> first & ((1u << kRep) - 1u);
-        live = kAll;
-#pragma unroll
-        for (int r = 0; r < kRep; ++r) {
-          at[r] = __shfl_sync(0xFFFFFFFFu, code_at, first + r);
-          const long long sat = __shfl_sync(0xFFFFFFFFu, scale_at, first + r);
-          if (mine >> r & 1u) {  // (rows past the length are read too: they are the page's)
-            const uint8_t* const p = kh + at[r];
-            load_words<kKw>(kr[r][0], p, 64);
-            load_words<kKw>(kr[r][1], p + ts8, 64);
-            const float *kp = ksh + sat, *vp = vsh + sat;
-            ks[r][0] = load_scale(kp);
-            ks[r][1] = load_scale(kp + ss8);
-            vs[r][0] = load_scale(vp);
-            vs[r][1] = load_scale(vp + ss8);
-          }
-        }
-        if (mine != (1u << kRep) - 1u || block_at(tl, kRep) > len) {
-          live = 0;
-#pragma unroll
-          for (int r = 0; r < kRep; ++r)
-            if (mine >> r & 1u)
-              live |= (block_at(tl, r) + g < len ? 1u << (2 * r) : 0u) | (block_at(tl, r) + g + 8 < len ? 2u << (2 * r) : 0u);
-        }
-      }
-    };
-    auto load_v = [&](int tl) {
+    // Copies tile tl into its stage, and says which of the blocks there are (small pages: positions).
+    auto copy = [&](int tl, int stage) -> uint32_t {
+      if (tl - strip == kStrip) enter_strip(tl);
+      const int first = (tl - strip) * kRep;
+      const uint32_t there = kSmallPage ? found : found >> first & ((1u << kRep) - 1u);
+      const uint32_t to = slots_at + stage * (kRep * kBlock);
 #pragma unroll
       for (int r = 0; r < kRep; ++r) {
         if constexpr (kSmallPage) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int page = pg[r][2 + e], row = block_at(tl, r) + 2 * t + (e & 1) + 8 * (e >> 1);
-            if (page >= 0) load_words<kVw>(vr[r][e], vh + page * c.page_stride + (row & slots) * ts, 16);
+          for (int i = 0; i < 16 / kAtOnce; ++i) {
+            const int row = i * kAtOnce + sub;
+            const long long at = __shfl_sync(0xFFFFFFFFu, code_at, 16 * r + row);
+            if (there >> (16 * r + row) & 1u) {
+              copy16(to + r * kBlock + place(row, chunk), kh + at);
+              copy16(to + r * kBlock + 16 * kRow + place(row, chunk), vh + at);
+            }
           }
-        } else if (found >> ((tl - strip) * kRep + r) & 1u) {
-          const uint8_t* const p = vh + at[r];
-          load_words<kVw>(vr[r][0], p, 16);
-          load_words<kVw>(vr[r][1], p + ts, 16);
-          load_words<kVw>(vr[r][2], p + ts8, 16);
-          load_words<kVw>(vr[r][3], p + ts8 + ts, 16);
+          const long long at = __shfl_sync(0xFFFFFFFFu, scale_at, 16 * r + (lane & 15));
+          if (there >> (16 * r + (lane & 15)) & 1u) copy4(to + r * kBlock + scale_to, sh + at);
+        } else {
+          const long long at = __shfl_sync(0xFFFFFFFFu, code_at, first + r), sat = __shfl_sync(0xFFFFFFFFu, scale_at, first + r);
+          if (there >> r & 1u) {  // (rows past the length are read too: they are the page's)
+#pragma unroll
+            for (int i = 0; i < 16 / kAtOnce; ++i) {
+              const uint32_t d = to + r * kBlock + place(i * kAtOnce + sub, chunk);
+              copy16(d, kh + at + i * kAtOnce * ts);
+              copy16(d + 16 * kRow, vh + at + i * kAtOnce * ts);
+            }
+            copy4(to + r * kBlock + scale_to, sh + sat);
+          }
         }
       }
+      return there;
     };
+    // Which rows of a tile count, where not all of them do (all: bits 2 r, 2 r + 1 for rows g, g + 8 of block r).
+    constexpr uint32_t kAll = (1u << (2 * kRep)) - 1u;
+    auto counting = [&](int tl, uint32_t there) -> uint32_t {
+      constexpr uint32_t kThere = kSmallPage ? (kRep == 2 ? 0xFFFFFFFFu : 0xFFFFu) : (1u << kRep) - 1u;
+      if (there == kThere && block_at(tl, kRep) <= len) return kAll;
+      uint32_t live = 0;
+#pragma unroll
+      for (int r = 0; r < kRep; ++r)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int row = g + 8 * e;
+          if (kSmallPage ? there >> (16 * r + row) & 1u : (there >> r & 1u) && block_at(tl, r) + row < len) live |= 1u << (2 * r + e);
+        }
+      return live;
+    };
+    uint32_t there_of[kStages];  // of the stages' tiles, the oldest first
 
     if (tile < tile_end) look(tile);
+    uint4 raw[kNt][kKc];  // q: head g of each 8 (on its way beside the page numbers)
+#pragma unroll
+    for (int n = 0; n < kNt; ++n)
+#pragma unroll
+      for (int p = 0; p < kKc; ++p) {
+        const int h = kPair ? g & 3 : 8 * n + g;
+        raw[n][p] = make_uint4(0u, 0u, 0u, 0u);
+        if (h < heads)
+          raw[n][p] = *reinterpret_cast<const uint4*>(a.q + un.b * a.ldq + static_cast<long long>(un.h0 + h) * kDh + q_dim(p, t));
+      }
+    if (tile < tile_end) {
+      enter_strip(tile);
+#pragma unroll
+      for (int i = 0; i < kStages - 1; ++i) {
+        there_of[i] = tile + i < tile_end ? copy(tile + i, i) : 0u;
+        cp_async_commit();
+      }
+    }
     // q as fp16 (times the sign of the scale, or 0), and the factor fq >= 0 that makes scores in powers of
     // two of its products with a position's codes and scale (heads 2 t, 2 t + 1)
     const float c2 = fabsf(a.scale * 1.4426950408889634f), sign = a.scale > 0.0f ? 1.0f : a.scale < 0.0f ? -1.0f : 0.0f;
@@ -256,14 +252,7 @@ struct Codes {
     __syncwarp();
 #pragma unroll
     for (int n = 0; n < kNt; ++n) {
-      const int h = kPair ? g & 3 : 8 * n + g;
-      uint4 q[kKc];
-#pragma unroll
-      for (int p = 0; p < kKc; ++p) {
-        q[p] = make_uint4(0u, 0u, 0u, 0u);
-        if (h < heads)
-          q[p] = *reinterpret_cast<const uint4*>(a.q + un.b * a.ldq + static_cast<long long>(un.h0 + h) * kDh + q_dim(p, t));
-      }
+      uint4 (&q)[kKc] = raw[n];
       float f = c2 == 0.0f ? 1.0f : c2;
       if (a.bf16) {
         uint32_t most = 0;  // the largest finite |q|
@@ -304,11 +293,16 @@ struct Codes {
       }
     }
     __syncwarp();
-    if (tile < tile_end) {
-      if constexpr (!kSmallPage) enter_strip(tile);
-      load_k(tile);
-      load_v(tile);
-      if constexpr (kSmallPage) look(tile + 1);
+    int stage = 0;
+    // the lane's rows in a block's place: keys g, g + 8, values 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+    uint32_t ka[2], va[4];
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      ka[e] = place(g + 8 * e, kKw == 8 ? 2 * t : kKw == 4 ? t : t >> 1) + (kKw == 2 ? 8 * (t & 1) : 0);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int row = 2 * t + (e & 1) + 8 * (e >> 1);
+      va[e] = 16 * kRow + place(row, kVw == 4 ? g : kVw == 2 ? g >> 1 : g >> 2) + (kVw == 2 ? 8 * (g & 1) : kVw == 1 ? 4 * (g & 3) : 0);
     }
     // The reference is the product `top` that a head's p are 1 at; it moves at `limit`, 2^kMove above.
     float top[kNt][2], limit[kNt][2], back_to[kNt][2];
@@ -327,7 +321,16 @@ struct Codes {
       for (int e = 0; e < 2; ++e) wf[n][e] = room[n][e] = 0.0f;
 
     for (int tl = tile; tl < tile_end; ++tl) {
-      const bool more = tl + 1 < tile_end;
+      cp_async_wait<kStages - 2>();
+      __syncwarp();  // this tile has landed for all lanes, and all have read the one whose stage is next
+      const uint32_t there = there_of[0];
+#pragma unroll
+      for (int i = 0; i + 1 < kStages - 1; ++i) there_of[i] = there_of[i + 1];
+      const int next = stage == 0 ? kStages - 1 : stage - 1;
+      there_of[kStages - 2] = tl + kStages - 1 < tile_end ? copy(tl + kStages - 1, next) : 0u;
+      cp_async_commit();
+      const uint32_t from = slots_at + stage * (kRep * kBlock);
+      stage = stage == kStages - 1 ? 0 : stage + 1;
       float s[kRep][kNt][4];
 #pragma unroll
       for (int r = 0; r < kRep; ++r)
@@ -336,20 +339,26 @@ struct Codes {
 #pragma unroll
           for (int e = 0; e < 4; ++e) s[r][n][e] = 0.0f;
 #pragma unroll
-      for (int r = 0; r < kRep; ++r)
+      for (int r = 0; r < kRep; ++r) {
+        uint32_t kr[2][kKw];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          read_words<kKw == 8 ? 4 : kKw>(kr[e], from + r * kBlock + ka[e]);
+          if constexpr (kKw == 8) read_words<4>(kr[e] + 4, from + r * kBlock + (ka[e] ^ 16u));  // (the other of two chunks)
+        }
 #pragma unroll
         for (int p = 0; p < kKc; ++p) {
           uint32_t x[2][4];  // of rows g, g + 8: four pairs of codes
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             if constexpr (kBits == 8) {
-              const uint32_t w0 = kr[r][e][2 * p] ^ 0x80808080u, w1 = kr[r][e][2 * p + 1] ^ 0x80808080u;
+              const uint32_t w0 = kr[e][2 * p] ^ 0x80808080u, w1 = kr[e][2 * p + 1] ^ 0x80808080u;
               x[e][0] = codes8<0>(w0, magic);
               x[e][1] = codes8<1>(w0, magic);
               x[e][2] = codes8<0>(w1, magic);
               x[e][3] = codes8<1>(w1, magic);
             } else {
-              const uint32_t w = kr[r][e][p];
+              const uint32_t w = kr[e][p];
               x[e][0] = codes4<0>(w, magic);
               x[e][1] = codes4<1>(w, magic);
               x[e][2] = codes4<0>(w >> 8, magic);
@@ -363,21 +372,25 @@ struct Codes {
             mma16816<false>(s[r][n], x[0][2], x[1][2], x[0][3], x[1][3], f.z, f.w);
           }
         }
-      const uint32_t counts = live;
+      }
+      const uint32_t counts = counting(tl, there);
       float sv[kRep][2];
 #pragma unroll
-      for (int r = 0; r < kRep; ++r)
+      for (int r = 0; r < kRep; ++r) {
+        uint32_t ks[2], vs[2];
+        read_words<2>(ks, from + r * kBlock + 32 * kRow + 8 * g);
+        read_words<2>(vs, from + r * kBlock + 32 * kRow + 64 + 8 * g);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          sv[r][e] = vs[r][e];
+          sv[r][e] = __uint_as_float(vs[e]);
 #pragma unroll
           for (int n = 0; n < kNt; ++n) {
-            s[r][n][2 * e] *= ks[r][e];
-            s[r][n][2 * e + 1] *= ks[r][e];
+            s[r][n][2 * e] *= __uint_as_float(ks[e]);
+            s[r][n][2 * e + 1] *= __uint_as_float(ks[e]);
           }
         }
-      if (more) load_k(tl + 1);
-      if (kSmallPage ? !__all_sync(0xFFFFFFFFu, counts == kAll) : counts != kAll) {
+      }
+      if (counts != kAll) {
 #pragma unroll
         for (int r = 0; r < kRep; ++r)
 #pragma unroll
@@ -480,6 +493,9 @@ struct Codes {
               pw[n][1][e] = transpose8x8(lo);
             }
           }
+        uint32_t vr[4][kVw];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) read_words<kVw>(vr[e], from + r * kBlock + va[e]);
 #pragma unroll
         for (int hh = 0; hh < kVc; ++hh) {
           uint32_t x[4][4];  // [j][operand]: dimensions 2 j, 2 j + 1 of positions 2 t, 2 t + 1; 2 t + 8, 2 t + 9
@@ -488,7 +504,7 @@ struct Codes {
             if constexpr (kBits == 8) {
 #pragma unroll
               for (int i = 0; i < 2; ++i) {
-                const uint32_t w0 = vr[r][2 * e][2 * hh + i], w1 = vr[r][2 * e + 1][2 * hh + i];
+                const uint32_t w0 = vr[2 * e][2 * hh + i], w1 = vr[2 * e + 1][2 * hh + i];
                 const uint32_t lo = __byte_perm(w0, w1, 0x5140) ^ 0x80808080u, hi = __byte_perm(w0, w1, 0x7362) ^ 0x80808080u;
                 x[2 * i][2 * e] = codes8<0>(lo, magic);
                 x[2 * i][2 * e + 1] = codes8<1>(lo, magic);
@@ -496,7 +512,7 @@ struct Codes {
                 x[2 * i + 1][2 * e + 1] = codes8<1>(hi, magic);
               }
             } else {
-              const uint32_t w0 = vr[r][2 * e][hh], w1 = vr[r][2 * e + 1][hh];
+              const uint32_t w0 = vr[2 * e][hh], w1 = vr[2 * e + 1][hh];
               const uint32_t lo = __byte_perm(w0, w1, 0x5410), hi = __byte_perm(w0, w1, 0x7632);
               x[0][2 * e] = codes4<0>(lo, magic);
               x[0][2 * e + 1] = codes4<1>(lo, magic);
@@ -517,11 +533,9 @@ struct Codes {
                 mma16816<false>(o[n][hh][j], x[j][0], x[j][1], x[j][2], x[j][3], pw[n][i][0], pw[n][i][1]);
         }
       }
-      if (more) {
-        load_v(tl + 1);
-        if constexpr (kSmallPage) look(tl + 2);
-      }
     }
+    cp_async_wait<0>();  // (what is left: empty groups)
+    __syncwarp();        // all lanes have read the ring
 #pragma unroll
     for (int n = 0; n < kNt; ++n)
 #pragma unroll

@@ -76,7 +76,8 @@ template <class C, int kNt, bool kCluster>
 __global__ void __launch_bounds__(kThreads, C::ctas(kNt)) paged_attention_kernel(const typename C::Args a) {
   constexpr int kHeads = 8 * kNt;
   constexpr int kDh = C::kDh, kVc = C::kVc, kTile = C::kTile;
-  extern __shared__ __align__(16) float so[];  // [kWarps][kHeads][kDh]
+  constexpr int kWarpFloats = C::warp_floats(kNt);
+  extern __shared__ __align__(16) float so[];  // a warp's kWarpFloats: what it loads into, then its [kHeads][kDh] of O
   __shared__ float sm[kWarps][kHeads], sl[kWarps][kHeads];
   __shared__ uint4 sq[kWarps][kNt][kDh / 32][32];  // the query operand, lane by lane (the registers are for the loads)
   __shared__ unsigned long long scan[2][kWarps];
@@ -236,7 +237,7 @@ __global__ void __launch_bounds__(kThreads, C::ctas(kNt)) paged_attention_kernel
           for (int e = 0; e < 4; ++e) o[n][hh][j][e] = 0.0f;
     }
     const Unit un = {c.table + static_cast<long long>(C::table_row(a, b, len)) * c.table_ld, b, hk, h0, heads, len, C::first_own(a, b, len), base};
-    C::template attend<kNt>(a, un, tile, tile_end, sq[warp], acc);
+    C::template attend<kNt>(a, un, tile, tile_end, sq[warp], so + warp * kWarpFloats, acc);
     if (C::kOwnOnly) pdl_wait();  // the prefix's parts
 
     // The warps' parts into shared memory.
@@ -254,7 +255,7 @@ __global__ void __launch_bounds__(kThreads, C::ctas(kNt)) paged_attention_kernel
         if (h < heads) {
 #pragma unroll
           for (int hh = 0; hh < kVc; ++hh) {
-            float* d = so + (warp * kHeads + h) * kDh + C::first_dim(hh, g);
+            float* d = so + warp * kWarpFloats + h * kDh + C::first_dim(hh, g);
 #pragma unroll
             for (int j = 0; j < 4; j += 2)
               *reinterpret_cast<float4*>(d + 2 * j) = make_float4(o[n][hh][j][e], o[n][hh][j][e + 2],
@@ -275,7 +276,7 @@ __global__ void __launch_bounds__(kThreads, C::ctas(kNt)) paged_attention_kernel
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
           const float f = sm[w][h] == -INFINITY ? 0.0f : exp2_fast(sm[w][h] - m);
-          const float4 z = *reinterpret_cast<const float4*>(so + (w * kHeads + h) * kDh + d);
+          const float4 z = *reinterpret_cast<const float4*>(so + w * kWarpFloats + h * kDh + d);
           sum += sl[w][h] * f;
           v.x += z.x * f;
           v.y += z.y * f;
@@ -287,7 +288,7 @@ __global__ void __launch_bounds__(kThreads, C::ctas(kNt)) paged_attention_kernel
     };
     if (kCluster) {  // the CTAs' parts to the first of them, and their sum there
       constexpr int kPart = kHeads * kDh + 2 * kHeads;
-      float* const all = so + kWarps * kHeads * kDh;  // [cs][kPart]
+      float* const all = so + kWarps * kWarpFloats;  // [cs][kPart]
       cluster_begun_wait();
       add_warps([&](int h, int d, float m, float sum, float4 v) {
         const uint32_t at = mapa_shared(smem_u32(all + rank * kPart), 0);
@@ -454,9 +455,9 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const typename C:
   write_out<C>(a, unit.x, h0 + h, d, m, sum, v);
 }
 
-template <int kDh, int kNt>
+template <class C, int kNt>
 constexpr size_t cluster_smem(int cs) {
-  return (static_cast<size_t>(kWarps + cs) * 8 * kNt * kDh + static_cast<size_t>(cs) * 2 * 8 * kNt) * sizeof(float);
+  return (static_cast<size_t>(kWarps) * C::warp_floats(kNt) + static_cast<size_t>(cs) * 8 * kNt * (C::kDh + 2)) * sizeof(float);
 }
 
 struct ClusterLaunch {
@@ -482,7 +483,7 @@ struct ClusterLaunch {
 template <class C, int kNt>
 cudaError_t allow_clusters() {
   static SmemLimit limit;
-  return limit.allow(paged_attention_kernel<C, kNt, true>, cluster_smem<C::kDh, kNt>(kMaxCluster));
+  return limit.allow(paged_attention_kernel<C, kNt, true>, cluster_smem<C, kNt>(kMaxCluster));
 }
 
 // Clusters of cs CTAs that the GPU holds at once; 0 where it does not say.
@@ -493,7 +494,7 @@ int clusters_at_once(int cs) {
   const cudaError_t e = known[cs].get(&n, [cs](int* number) {
     const cudaError_t le = allow_clusters<C, kNt>();
     if (le != cudaSuccess) return le;
-    ClusterLaunch l(1, cs, cluster_smem<C::kDh, kNt>(cs), nullptr);
+    ClusterLaunch l(1, cs, cluster_smem<C, kNt>(cs), nullptr);
     l.cfg.numAttrs = 1;
     return cudaOccupancyMaxActiveClusters(number, paged_attention_kernel<C, kNt, true>, &l.cfg);
   });
@@ -507,7 +508,7 @@ template <class C, int kNt>
 cudaError_t launch_clusters(const typename C::Args& a, int units, int cs, cudaStream_t stream, unsigned int* launches) {
   cudaError_t e = allow_clusters<C, kNt>();
   if (e != cudaSuccess) return e;
-  const ClusterLaunch l(units, cs, cluster_smem<C::kDh, kNt>(cs), stream);
+  const ClusterLaunch l(units, cs, cluster_smem<C, kNt>(cs), stream);
   e = cudaLaunchKernelEx(&l.cfg, paged_attention_kernel<C, kNt, true>, a);
   if (e == cudaSuccess) ++*launches;
   return e;
@@ -515,7 +516,7 @@ cudaError_t launch_clusters(const typename C::Args& a, int units, int cs, cudaSt
 
 template <class C, int kNt>
 cudaError_t launch(const typename C::Args& a, cudaStream_t stream, unsigned int* launches) {
-  constexpr size_t smem = static_cast<size_t>(kWarps) * 8 * kNt * C::kDh * sizeof(float);
+  constexpr size_t smem = static_cast<size_t>(kWarps) * C::warp_floats(kNt) * sizeof(float);
   static SmemLimit limit;
   auto* kernel = paged_attention_kernel<C, kNt, false>;
   const cudaError_t le = limit.allow(kernel, smem);

@@ -88,6 +88,7 @@ struct Rows {
   static constexpr int kKc = kDh / 32;    // 16-byte pieces of a key row per lane
   static constexpr int kVc = kDh / 64;    // of a value row
   static constexpr float kLift = kShift<kBf16>;
+  static __host__ __device__ constexpr int warp_floats(int nt) { return 8 * nt * kDh; }  // (for its part of O)
   static __host__ __device__ constexpr int ctas(int nt) { return nt == 1 ? 3 : 2; }
   static __device__ __forceinline__ bool bf16(const Args&) { return kBf16; }
   static __device__ __forceinline__ int first_own(const Args& a, int b, int len) {
@@ -106,7 +107,7 @@ struct Rows {
   // Goes through tiles tile .. tile_end - 1 of the unit. sq: the warp's place for the query operand.
   template <int kNt>
   static __device__ __forceinline__ void attend(const Args& a, const Unit& un, int tile, int tile_end,
-                                                uint4 (&sq)[kNt][kKc][32], Part<kNt, kVc>& acc) {
+                                                uint4 (&sq)[kNt][kKc][32], float*, Part<kNt, kVc>& acc) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const float c2 = a.scale * 1.4426950408889634f;
     const PagedCache& c = a.kv;
