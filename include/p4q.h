@@ -625,9 +625,10 @@ p4q_status p4q_rope_append_quant(const uint16_t* q, int ldq, const uint16_t* k, 
 /* p4q_paged_attention over a cache of codes; q and o of type dtype, P4Q_F16 or
  * P4Q_BF16. Scores are (scale log2 e s_j) (q . c_j) with whole codes c_j; the
  * weights times the values' scales enter the product with the codes in 22 bits.
- * fp32 products, softmax and sums; o rounded once. Scales may have any sign; one
- * of v that is not finite counts as NaN. Finite q of bf16 below 2^-32 of the largest of
- * their head lose bits (2^-39 of that one at most). Other arguments, rules and the workspace
+ * fp32 products, softmax and sums; o rounded once. Scales may have any sign. q enters the
+ * products in 16 bits: values below 2^-25 of the largest of their head may lose bits (2^-35 of
+ * that one at most). What is not finite in a head's q makes that head NaN, a scale of v that
+ * is not counts as NaN, one of k as in the formula. Other arguments, rules and the workspace
  * (p4q_paged_attention_workspace_bytes()) as p4q_paged_attention. */
 p4q_status p4q_paged_attention_quant(const uint16_t* q, int ldq, int H, const p4q_paged_kvq* kv, int dtype,
                                      const int32_t* lens, float scale, uint16_t* o, int ldo, float* lse, void* ws,

@@ -13,9 +13,9 @@
 // dimensions an MMA's k-th ones are is free as long as q has the same order, so the nibbles
 // {0, 4}, {1, 5}, {2, 6}, {3, 7} of a word are pairs as they lie.
 //
-// q of fp16 enters the product as it is; q of bf16 times the power of two that brings its head's
-// largest finite value below 2^15, in fp16: exact where |q| >= 2^-32 of that one, and off by
-// less than 2^-39 of it elsewhere. The weights p sv enter theirs as two fp16 values (22 bits)
+// q enters the product in fp16: with 8 bits q of fp16 as it is, else times the power of two that
+// brings its head's largest finite value below 2^15: exact where |q| is not below 2^-25 of that one, and
+// off by less than 2^-35 of it elsewhere. The weights p sv enter theirs as two fp16 values (22 bits)
 // times a power of two per head that moves like the softmax's reference, so scales
 // of any size count against the largest p sv seen and not against fp16's range.
 #pragma once
@@ -28,10 +28,12 @@ namespace paged {
 // Constants that the compiler is to keep in registers: an instruction has room for one of its own, and
 // it would rather use two of these (64 more per block of 16 positions at 4 bits).
 struct Magic {
-  uint32_t lo, hi, bytes;
+  uint32_t lo, hi, key_lo, key_hi, bytes;
   __device__ __forceinline__ Magic() {
     asm volatile("mov.b32 %0, 0x64086408;" : "=r"(lo));
     asm volatile("mov.b32 %0, 0x64806480;" : "=r"(hi));
+    asm volatile("mov.b32 %0, 0x00080008;" : "=r"(key_lo));
+    asm volatile("mov.b32 %0, 0x00800080;" : "=r"(key_hi));
     asm volatile("mov.b32 %0, 0x64646464;" : "=r"(bytes));
   }
 };
@@ -63,13 +65,34 @@ __device__ __forceinline__ uint32_t codes4(uint32_t w, const Magic& k) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// Asynchronous copies to shared memory, fetched 64 bytes at a time: a fetch of the whole 128-byte line
-// moved 1.65 times the bytes from HBM where a position's codes are 64 and other heads' lie between.
+// Asynchronous copies to shared memory. kHalfLines: fetched 64 bytes at a time, where the other half of a
+// 128-byte line is of no use soon: whole lines moved 1.65 times the bytes from HBM where a position's
+// codes are 64 and other heads' lie between (64 x 4096 x 8 heads at 4 bits 95 us instead of 71).
+template <bool kHalfLines>
 __device__ __forceinline__ void copy16(uint32_t dst, const uint8_t* src) {
-  asm volatile("cp.async.cg.shared.global.L2::64B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  if (kHalfLines)
+    asm volatile("cp.async.cg.shared.global.L2::64B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  else
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
+template <bool kHalfLines>
 __device__ __forceinline__ void copy4(uint32_t dst, const float* src) {
-  asm volatile("cp.async.ca.shared.global.L2::64B [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+  if (kHalfLines)
+    asm volatile("cp.async.ca.shared.global.L2::64B [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+
+// The same nibbles of keys as what fp16 reads in them: (8 + c) 2^-24, 16 times that of the odd ones. Exact in
+// the product; q takes the factor 16 and the accumulator begins with what the 8 adds.
+template <int kOdd>
+__device__ __forceinline__ uint32_t key_codes4(uint32_t w, const Magic& k) {
+  uint32_t v;
+  if (kOdd)
+    asm("lop3.b32 %0, %1, 0x00F000F0, %2, 0x6A;" : "=r"(v) : "r"(w), "r"(k.key_hi));
+  else
+    asm("lop3.b32 %0, %1, 0x000F000F, %2, 0x6A;" : "=r"(v) : "r"(w), "r"(k.key_lo));
+  return v;
 }
 
 template <int kWords>
@@ -85,13 +108,16 @@ __device__ __forceinline__ void read_words(uint32_t* w, uint32_t at) {
 // kPair: at most four heads to a key/value head's unit. Columns 4 - 7 of the products, which would be
 // empty, then repeat heads 0 - 3 and take the second fp16 value of their weights, so one product
 // of O^T does for both.
-template <int kBits, int kDhRows, bool kSmallPage, bool kPair>
+// kSplit: the warps of a CTA take that many neighbouring key/value heads turn by turn, whose codes of a
+// position share a line of HBM.
+template <int kBits, int kDhRows, bool kSmallPage, bool kPair, int kSplitHeads>
 struct Codes {
   typedef QuantAttnArgs Args;
   static constexpr bool kOwnOnly = false, kHeadsOuter = true;
   static constexpr int kDh = kDhRows;
   static constexpr int kRep = kDh * kBits == 1024 ? 1 : kDh * kBits == 256 && !kSmallPage ? 4 : 2;  // blocks of 16 positions per warp and tile
-  static constexpr int kTile = 16 * kRep * kWarps;
+  static constexpr int kSplit = kSplitHeads;
+  static constexpr int kTile = 16 * kRep * kWarps / kSplit;
   static constexpr int kKc = kDh / 32;             // pieces of q per lane, 8 dimensions each
   static constexpr int kVc = kDh / 64;
   static constexpr int kKw = kDh * kBits / 128;    // words of a key row per lane
@@ -100,7 +126,8 @@ struct Codes {
   static constexpr int kChunks = kRow / 16;        // copies of 16 bytes for it
   static constexpr int kAtOnce = 32 / kChunks;     // rows that a warp copies at once
   static constexpr int kBlock = 32 * kRow + 128;   // bytes of 16 positions: keys, values, scales
-  static constexpr int kStages = 3;
+  static constexpr int kStages = kRow == 128 ? 2 : 3;
+  static constexpr bool kHalf = kRow * kSplit < 128;
   // Floats of a warp's ring of stages; its part of O takes their place in the end.
   static __host__ __device__ constexpr int warp_floats(int nt) {
     return kStages * kRep * kBlock / 4 > 8 * nt * kDh ? kStages * kRep * kBlock / 4 : 8 * nt * kDh;
@@ -113,7 +140,7 @@ struct Codes {
   static constexpr float kLift = 0.0f;
   static constexpr float kMove = 8.0f;
   static constexpr int kSecond = kPair ? 1 : 2;    // products per operand of O^T
-  static __host__ __device__ constexpr int ctas(int nt) { return nt == 1 ? 3 : 2; }
+  static __host__ __device__ constexpr int ctas(int nt) { return nt == 2 ? 2 : kDh * kBits == 1024 && !kSmallPage ? 4 : 3; }
   static __device__ __forceinline__ bool bf16(const Args& a) { return a.bf16; }
   static __device__ __forceinline__ int first_own(const Args&, int, int) { return 0; }
   static __device__ __forceinline__ int table_row(const Args&, int b, int) { return b; }
@@ -139,7 +166,7 @@ struct Codes {
     const float* const sh = (lane < 16 ? c.k_scale : c.v_scale) + un.hk * c.scale_head_stride + (kSmallPage ? 0 : (lane & 15) * ss);
     const uint32_t slots_at = smem_u32(ring);
     const uint32_t scale_to = 32 * kRow + 4 * (16 * (lane >> 4) + 2 * (lane & 7) + (lane >> 3 & 1));  // rows g, g + 8 side by side
-    auto block_at = [&](int tl, int r) { return tl * kTile + (warp * kRep + r) * 16; };
+    auto block_at = [&](int tl, int r) { return tl * kTile + (warp / kSplit * kRep + r) * 16; };
 
     // The page of position j, -1 if it is not to be read.
     auto page_of = [&](int j) -> int {
@@ -188,22 +215,22 @@ struct Codes {
             const int row = i * kAtOnce + sub;
             const long long at = __shfl_sync(0xFFFFFFFFu, code_at, 16 * r + row);
             if (there >> (16 * r + row) & 1u) {
-              copy16(to + r * kBlock + place(row, chunk), kh + at);
-              copy16(to + r * kBlock + 16 * kRow + place(row, chunk), vh + at);
+              copy16<kHalf>(to + r * kBlock + place(row, chunk), kh + at);
+              copy16<kHalf>(to + r * kBlock + 16 * kRow + place(row, chunk), vh + at);
             }
           }
           const long long at = __shfl_sync(0xFFFFFFFFu, scale_at, 16 * r + (lane & 15));
-          if (there >> (16 * r + (lane & 15)) & 1u) copy4(to + r * kBlock + scale_to, sh + at);
+          if (there >> (16 * r + (lane & 15)) & 1u) copy4<kHalf>(to + r * kBlock + scale_to, sh + at);
         } else {
           const long long at = __shfl_sync(0xFFFFFFFFu, code_at, first + r), sat = __shfl_sync(0xFFFFFFFFu, scale_at, first + r);
           if (there >> r & 1u) {  // (rows past the length are read too: they are the page's)
 #pragma unroll
             for (int i = 0; i < 16 / kAtOnce; ++i) {
               const uint32_t d = to + r * kBlock + place(i * kAtOnce + sub, chunk);
-              copy16(d, kh + at + i * kAtOnce * ts);
-              copy16(d + 16 * kRow, vh + at + i * kAtOnce * ts);
+              copy16<kHalf>(d, kh + at + i * kAtOnce * ts);
+              copy16<kHalf>(d + 16 * kRow, vh + at + i * kAtOnce * ts);
             }
-            copy4(to + r * kBlock + scale_to, sh + sat);
+            copy4<kHalf>(to + r * kBlock + scale_to, sh + sat);
           }
         }
       }
@@ -248,15 +275,17 @@ struct Codes {
     // q as fp16 (times the sign of the scale, or 0), and the factor fq >= 0 that makes scores in powers of
     // two of its products with a position's codes and scale (heads 2 t, 2 t + 1)
     const float c2 = fabsf(a.scale * 1.4426950408889634f), sign = a.scale > 0.0f ? 1.0f : a.scale < 0.0f ? -1.0f : 0.0f;
-    float fq[kNt][2];
+    float fq[kNt][2], begin[kNt][2] = {};  // and what the products' sums begin with
     __syncwarp();
 #pragma unroll
     for (int n = 0; n < kNt; ++n) {
       uint4 (&q)[kKc] = raw[n];
       float f = c2 == 0.0f ? 1.0f : c2;
-      if (a.bf16) {
+      float sum = 0.0f;  // of the lane's q, as it enters the product
+      if (a.bf16 || kBits == 4) {
         uint32_t most = 0;  // the largest finite |q|
-        auto finite = [](uint32_t w) { return (w & 0x7F80u) == 0x7F80u ? 0u : w & 0x7FFFu; };
+        const uint32_t inf = a.bf16 ? 0x7F80u : 0x7C00u;
+        auto finite = [inf](uint32_t w) { return (w & inf) == inf ? 0u : w & 0x7FFFu; };
 #pragma unroll
         for (int p = 0; p < kKc; ++p) {
           const uint32_t w[4] = {q[p].x, q[p].y, q[p].z, q[p].w};
@@ -265,12 +294,16 @@ struct Codes {
         }
         most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
         most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
-        const int up = most == 0 ? 0 : min(100, 14 - (static_cast<int>(most >> 7) - 127));
+        const float largest = a.bf16 ? from16<true>(static_cast<uint16_t>(most)) : from16<false>(static_cast<uint16_t>(most));
+        const int up = most == 0 ? 0 : min(100, 14 - (static_cast<int>(__float_as_uint(largest) >> 23) - 127));
         const float by = sign * __uint_as_float(static_cast<uint32_t>(127 + up) << 23);
         f *= __uint_as_float(static_cast<uint32_t>(127 - up) << 23);
-        auto scaled = [by](uint32_t w) {
-          const float2 v = unpack2<true>(w);
-          return pack2<false>(v.x * by, v.y * by);
+        auto scaled = [&](uint32_t w) {
+          const float2 v = a.bf16 ? unpack2<true>(w) : unpack2<false>(w);
+          const uint32_t s = pack2<false>(v.x * by, v.y * by);
+          const float2 r = unpack2<false>(s);
+          sum += r.x + r.y;
+          return s;
         };
 #pragma unroll
         for (int p = 0; p < kKc; ++p) q[p] = make_uint4(scaled(q[p].x), scaled(q[p].y), scaled(q[p].z), scaled(q[p].w));
@@ -282,13 +315,25 @@ struct Codes {
 #pragma unroll
         for (int p = 0; p < kKc; ++p) q[p] = make_uint4(scaled(q[p].x), scaled(q[p].y), scaled(q[p].z), scaled(q[p].w));
       }
+      if constexpr (kBits == 4) {
+        sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
+        sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
+        f *= 0x1p24f;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) begin[n][e] = __shfl_sync(0xFFFFFFFFu, sum, 4 * (2 * t + e)) * -0x1p-21f;
+      }
 #pragma unroll
       for (int e = 0; e < 2; ++e) fq[n][e] = fmaxf(0x1p-126f, __shfl_sync(0xFFFFFFFFu, f, 4 * (2 * t + e)));
 #pragma unroll
       for (int p = 0; p < kKc; ++p) {
-        if (kBits == 4)  // the nibbles' pairs
-          q[p] = make_uint4(__byte_perm(q[p].x, q[p].z, 0x5410), __byte_perm(q[p].x, q[p].z, 0x7632),
-                            __byte_perm(q[p].y, q[p].w, 0x5410), __byte_perm(q[p].y, q[p].w, 0x7632));
+        if constexpr (kBits == 4) {  // the nibbles' pairs, the odd ones over 16 (below 2^-25 of the head's largest not exact)
+          auto over16 = [](uint32_t w) {
+            const __half2 h = __hmul2(*reinterpret_cast<const __half2*>(&w), __float2half2_rn(0.0625f));
+            return *reinterpret_cast<const uint32_t*>(&h);
+          };
+          q[p] = make_uint4(__byte_perm(q[p].x, q[p].z, 0x5410), over16(__byte_perm(q[p].x, q[p].z, 0x7632)),
+                            __byte_perm(q[p].y, q[p].w, 0x5410), over16(__byte_perm(q[p].y, q[p].w, 0x7632)));
+        }
         sq[n][p][lane] = q[p];
       }
     }
@@ -337,7 +382,7 @@ struct Codes {
 #pragma unroll
         for (int n = 0; n < kNt; ++n)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[r][n][e] = 0.0f;
+          for (int e = 0; e < 4; ++e) s[r][n][e] = kBits == 4 ? begin[n][e & 1] : 0.0f;
 #pragma unroll
       for (int r = 0; r < kRep; ++r) {
         uint32_t kr[2][kKw];
@@ -359,10 +404,10 @@ struct Codes {
               x[e][3] = codes8<1>(w1, magic);
             } else {
               const uint32_t w = kr[e][p];
-              x[e][0] = codes4<0>(w, magic);
-              x[e][1] = codes4<1>(w, magic);
-              x[e][2] = codes4<0>(w >> 8, magic);
-              x[e][3] = codes4<1>(w >> 8, magic);
+              x[e][0] = key_codes4<0>(w, magic);
+              x[e][1] = key_codes4<1>(w, magic);
+              x[e][2] = key_codes4<0>(w >> 8, magic);
+              x[e][3] = key_codes4<1>(w >> 8, magic);
             }
           }
 #pragma unroll

@@ -72,9 +72,23 @@ __device__ __forceinline__ unsigned long long quotient(unsigned long long a, uns
   return a / b;
 }
 
+// The query heads of unit u of a sequence: count from h0. A unit is 8 NT of a key/value head's at most, or
+// all of those of C::kSplit neighbouring ones, which its warps take turn by turn.
+template <class C, int kNt>
+struct UnitHeads {
+  int h0, count;
+  __device__ __forceinline__ UnitHeads(int u, int group, int parts) {
+    const int hk = u / parts * C::kSplit;
+    h0 = hk * group + u % parts * 8 * kNt;
+    count = C::kSplit > 1 ? C::kSplit * group : min(8 * kNt, hk * group + group - h0);
+  }
+};
+
 template <class C, int kNt, bool kCluster>
 __global__ void __launch_bounds__(kThreads, C::ctas(kNt)) paged_attention_kernel(const typename C::Args a) {
-  constexpr int kHeads = 8 * kNt;
+  constexpr int kHeads = 8 * kNt;                  // of a warp
+  constexpr int kUnitHeads = C::kSplit * kHeads;
+  static_assert(kUnitHeads <= 16, "parts have room for 16 heads");
   constexpr int kDh = C::kDh, kVc = C::kVc, kTile = C::kTile;
   constexpr int kWarpFloats = C::warp_floats(kNt);
   extern __shared__ __align__(16) float so[];  // a warp's kWarpFloats: what it loads into, then its [kHeads][kDh] of O
@@ -85,7 +99,7 @@ __global__ void __launch_bounds__(kThreads, C::ctas(kNt)) paged_attention_kernel
 
   const auto& c = a.kv;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-  const int group = a.H / c.Hkv, parts = (group + kHeads - 1) / kHeads, units = c.Hkv * parts;
+  const int group = a.H / c.Hkv, parts = (group + kHeads - 1) / kHeads, units = c.Hkv / C::kSplit * parts;
   const long long room = min(static_cast<long long>(c.table_cols) << c.page_log2, kMaxLen);
   int4* split = static_cast<int4*>(a.ws);
   float* partial = reinterpret_cast<float*>(split + kMaxGrid);
@@ -216,8 +230,10 @@ __global__ void __launch_bounds__(kThreads, C::ctas(kNt)) paged_attention_kernel
       next_unit();
       continue;
     }
-    const int hk = u / parts, h0 = hk * group + (u % parts) * kHeads;
-    const int heads = min(kHeads, hk * group + group - h0);
+    const UnitHeads<C, kNt> uh(u, group, parts);
+    const int h0 = uh.h0, hk = u / parts * C::kSplit + warp % C::kSplit;
+    const int heads = C::kSplit > 1 ? group : uh.count;  // of the warp, from wh0
+    const int wh0 = C::kSplit > 1 ? hk * group : h0;
     Part<kNt, kVc> acc;
     auto& o = acc.o;
     auto& ref = acc.ref;
@@ -236,7 +252,7 @@ __global__ void __launch_bounds__(kThreads, C::ctas(kNt)) paged_attention_kernel
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[n][hh][j][e] = 0.0f;
     }
-    const Unit un = {c.table + static_cast<long long>(C::table_row(a, b, len)) * c.table_ld, b, hk, h0, heads, len, C::first_own(a, b, len), base};
+    const Unit un = {c.table + static_cast<long long>(C::table_row(a, b, len)) * c.table_ld, b, hk, wh0, heads, len, C::first_own(a, b, len), base};
     C::template attend<kNt>(a, un, tile, tile_end, sq[warp], so + warp * kWarpFloats, acc);
     if (C::kOwnOnly) pdl_wait();  // the prefix's parts
 
@@ -267,14 +283,15 @@ __global__ void __launch_bounds__(kThreads, C::ctas(kNt)) paged_attention_kernel
 
     // Their maxima, sums and values added up, to done(head, dimension, maximum, sum, four values).
     auto add_warps = [&](auto&& done) {
-      for (int i = tid; i < heads * (kDh / 4); i += kThreads) {
-        const int h = i / (kDh / 4), d = (i % (kDh / 4)) * 4;
-        float m = sm[0][h], sum = 0.0f;
+      for (int i = tid; i < uh.count * (kDh / 4); i += kThreads) {
+        const int hu = i / (kDh / 4), d = (i % (kDh / 4)) * 4;
+        const int w0 = C::kSplit > 1 ? hu / group : 0, h = C::kSplit > 1 ? hu - w0 * group : hu;
+        float m = sm[w0][h], sum = 0.0f;
 #pragma unroll
-        for (int w = 1; w < kWarps; ++w) m = fmaxf(m, sm[w][h]);
+        for (int w = w0 + C::kSplit; w < kWarps; w += C::kSplit) m = fmaxf(m, sm[w][h]);
         float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
+        for (int w = w0; w < kWarps; w += C::kSplit) {
           const float f = sm[w][h] == -INFINITY ? 0.0f : exp2_fast(sm[w][h] - m);
           const float4 z = *reinterpret_cast<const float4*>(so + w * kWarpFloats + h * kDh + d);
           sum += sl[w][h] * f;
@@ -283,33 +300,33 @@ __global__ void __launch_bounds__(kThreads, C::ctas(kNt)) paged_attention_kernel
           v.z += z.z * f;
           v.w += z.w * f;
         }
-        done(h, d, m, sum, v);
+        done(hu, d, m, sum, v);
       }
     };
     if (kCluster) {  // the CTAs' parts to the first of them, and their sum there
-      constexpr int kPart = kHeads * kDh + 2 * kHeads;
+      constexpr int kPart = kUnitHeads * kDh + 2 * kUnitHeads;
       float* const all = so + kWarps * kWarpFloats;  // [cs][kPart]
       cluster_begun_wait();
       add_warps([&](int h, int d, float m, float sum, float4 v) {
         const uint32_t at = mapa_shared(smem_u32(all + rank * kPart), 0);
         st_shared_cluster_v4(at + 4 * (h * kDh + d), v);
         if (d == 0) {
-          st_shared_cluster_u32(at + 4 * (kHeads * kDh + h), __float_as_uint(m));
-          st_shared_cluster_u32(at + 4 * (kHeads * kDh + kHeads + h), __float_as_uint(sum));
+          st_shared_cluster_u32(at + 4 * (kUnitHeads * kDh + h), __float_as_uint(m));
+          st_shared_cluster_u32(at + 4 * (kUnitHeads * kDh + kUnitHeads + h), __float_as_uint(sum));
         }
       });
       cluster_sync();
       if (rank != 0) return;
-      for (int i = tid; i < heads * (kDh / 4); i += kThreads) {
+      for (int i = tid; i < uh.count * (kDh / 4); i += kThreads) {
         const int h = i / (kDh / 4), d = (i % (kDh / 4)) * 4;
         float m = -INFINITY, sum = 0.0f;
-        for (int r = 0; r < cs; ++r) m = fmaxf(m, all[r * kPart + kHeads * kDh + h]);
+        for (int r = 0; r < cs; ++r) m = fmaxf(m, all[r * kPart + kUnitHeads * kDh + h]);
         float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         for (int r = 0; r < cs; ++r) {
           const float* const part = all + r * kPart;
-          const float mr = part[kHeads * kDh + h], f = mr == -INFINITY ? 0.0f : exp2_fast(mr - m);
+          const float mr = part[kUnitHeads * kDh + h], f = mr == -INFINITY ? 0.0f : exp2_fast(mr - m);
           const float4 z = *reinterpret_cast<const float4*>(part + h * kDh + d);
-          sum += part[kHeads * kDh + kHeads + h] * f;
+          sum += part[kUnitHeads * kDh + kUnitHeads + h] * f;
           v.x += z.x * f;
           v.y += z.y * f;
           v.z += z.z * f;
@@ -376,8 +393,9 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const typename C:
   const int4 unit = split[blockIdx.x];
   const int c1 = unit.z;
   if (c1 < 0) return;
-  const int hk = unit.y / parts, h0 = hk * group + (unit.y % parts) * kHeads;
-  if (h >= hk * group + group - h0) return;
+  const UnitHeads<C, kNt> uh(unit.y, group, parts);
+  const int h0 = uh.h0;
+  if (h >= uh.count) return;
   float jm = -INFINITY, jl = 0.0f, jo[kJd];
 #pragma unroll
   for (int e = 0; e < kJd; ++e) jo[e] = 0.0f;
@@ -457,7 +475,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const typename C:
 
 template <class C, int kNt>
 constexpr size_t cluster_smem(int cs) {
-  return (static_cast<size_t>(kWarps) * C::warp_floats(kNt) + static_cast<size_t>(cs) * 8 * kNt * (C::kDh + 2)) * sizeof(float);
+  return (static_cast<size_t>(kWarps) * C::warp_floats(kNt) + static_cast<size_t>(cs) * C::kSplit * 8 * kNt * (C::kDh + 2)) * sizeof(float);
 }
 
 struct ClusterLaunch {
@@ -523,7 +541,7 @@ cudaError_t launch(const typename C::Args& a, cudaStream_t stream, unsigned int*
   if (le != cudaSuccess) return le;
   // CTAs for every tile that the table has room for, at most a wave
   const int group = a.H / a.kv.Hkv;
-  const long long units = static_cast<long long>(a.kv.Hkv) * ((group + 8 * kNt - 1) / (8 * kNt)) * a.kv.seqs;
+  const long long units = static_cast<long long>(a.kv.Hkv / C::kSplit) * ((group + 8 * kNt - 1) / (8 * kNt)) * a.kv.seqs;
   constexpr int kTile = C::kTile;
   const long long room = std::max(1ll, ((static_cast<long long>(a.kv.table_cols) << a.kv.page_log2) + kTile - 1) / kTile);
   const int wave = std::min(kMaxGrid, num_sms() * C::ctas(kNt));
@@ -546,7 +564,7 @@ cudaError_t launch(const typename C::Args& a, cudaStream_t stream, unsigned int*
   cudaError_t e = launch_pdl(kernel, dim3(static_cast<unsigned>(grid)), dim3(kThreads), smem, stream, a);
   if (e != cudaSuccess) return e;
   ++*launches;
-  const unsigned heads = static_cast<unsigned>(std::min(group, 8 * kNt));
+  const unsigned heads = static_cast<unsigned>(C::kSplit > 1 ? C::kSplit * group : std::min(group, 8 * kNt));
   e = launch_pdl(join_kernel<C, kNt>, dim3(static_cast<unsigned>(grid), heads), dim3(32 * kJoinWarps), 0, stream,
                  a);
   if (e == cudaSuccess) ++*launches;

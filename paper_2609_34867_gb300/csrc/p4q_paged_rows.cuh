@@ -82,6 +82,7 @@ template <bool kBf16Rows, int kDhRows, bool kSmallPage, bool kOwn = false>
 struct Rows {
   typedef std::conditional_t<kOwn, PrefixArgs, PagedAttnArgs> Args;
   static constexpr bool kBf16 = kBf16Rows, kOwnOnly = kOwn, kHeadsOuter = false;
+  static constexpr int kSplit = 1;
   static constexpr int kDh = kDhRows;
   static constexpr int kRep = 128 / kDh;  // blocks of 16 positions per warp and tile: 8 KB of keys and values
   static constexpr int kTile = 16 * kRep * kWarps;
