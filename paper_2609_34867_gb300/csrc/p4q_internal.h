@@ -236,10 +236,10 @@ struct PrefixArgs : PagedAttnArgs {
   const int32_t* prefix_lens = nullptr;  // [groups]
   int groups = 0;
   int grid = 0;                          // CTAs of the prefix kernel
-  unsigned long long* base = nullptr;    // [groups + 1], see p4q_paged_prefix.cuh
+  float* own = nullptr;                  // the parts, see p4q_paged_prefix.cuh
   float* parts = nullptr;
 };
-size_t prefix_attention_workspace_bytes(int seqs, int groups, int H, int dh);
+size_t prefix_attention_workspace_bytes(int seqs, int H, int dh);
 cudaError_t launch_prefix_attention(PrefixArgs a, cudaStream_t stream, unsigned int* launches);
 unsigned int prefix_read_and_clear_error();        // waits that ran out
 unsigned int prefix_read_and_clear_index_error();

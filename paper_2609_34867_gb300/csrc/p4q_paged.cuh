@@ -59,6 +59,14 @@ struct Unit {
   int b, hk, h0, heads, len, from, base;
 };
 
+// Of a sequence whose positions are all the kernel's own.
+struct NoPrefix {
+  static constexpr int from = 0;
+  int row;
+  template <class Args>
+  __device__ __forceinline__ NoPrefix(const Args&, int b, int) : row(b) {}
+};
+
 // A warp's part of a unit: O^T ([.][hh][j]: dimensions C::first_dim(hh, g) + 2 j (+ 1),
 // heads 2 t, 2 t + 1), the references and the sums.
 template <int kNt, int kVc>

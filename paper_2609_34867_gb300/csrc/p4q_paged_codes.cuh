@@ -142,9 +142,7 @@ struct Codes {
   static constexpr int kSecond = kPair ? 1 : 2;    // products per operand of O^T
   static __host__ __device__ constexpr int ctas(int nt) { return nt == 2 ? 2 : kDh * kBits == 1024 && !kSmallPage ? 4 : 3; }
   static __device__ __forceinline__ bool bf16(const Args& a) { return a.bf16; }
-  static __device__ __forceinline__ int first_own(const Args&, int, int) { return 0; }
-  static __device__ __forceinline__ int table_row(const Args&, int b, int) { return b; }
-  static __device__ __forceinline__ void add_prefix(const Args&, int, int, int, float&, float&, float4&) {}
+  typedef NoPrefix Behind;
   static __device__ __forceinline__ int first_dim(int hh, int g) { return (kDh / 8) * g + 8 * hh; }
   // The dimensions of q's piece p that lane t's keys have.
   static __device__ __forceinline__ int q_dim(int p, int t) { return (kDh / 4) * t + 8 * p; }

@@ -7,6 +7,7 @@
 #include <algorithm>
 
 #include "p4q_paged.cuh"
+#include "p4q_paged_prefix.cuh"
 
 namespace p4q {
 namespace {
@@ -35,7 +36,12 @@ __device__ __forceinline__ void st_shared_cluster_v4(uint32_t a, float4 v) {
 // the reference maximum, the sum and the values against it.
 template <class C>
 __device__ __forceinline__ void write_out(const typename C::Args& a, int b, int h, int d, float m, float sum, float4 v) {
-  C::add_prefix(a, b, h, d, m, sum, v);
+  if constexpr (C::kOwnOnly) {  // a part of what another kernel adds up
+    float* const part = a.own + (static_cast<long long>(b) * a.H + h) * (C::kDh + kPartExtra);
+    *reinterpret_cast<float4*>(part + d) = v;
+    if (d == 0) *reinterpret_cast<float4*>(part + C::kDh) = make_float4(m, sum, 0.0f, 0.0f);
+    return;
+  }
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
   uint2 w;
   if (C::bf16(a))
@@ -64,12 +70,6 @@ struct Plan {
 // 2048 x 40 heads 118 us), or its tiles rounded up to whole pieces.
 __device__ __forceinline__ int span_of(int tiles, int pieces) {
   return pieces ? (tiles + kMinTiles - 1) / kMinTiles * kMinTiles : tiles + kUnitCost;
-}
-
-// 64-bit quotients of numbers that mostly fit in 32.
-__device__ __forceinline__ unsigned long long quotient(unsigned long long a, unsigned long long b) {
-  if (((a | b) >> 32) == 0) return static_cast<unsigned int>(a) / static_cast<unsigned int>(b);
-  return a / b;
 }
 
 // The query heads of unit u of a sequence: count from h0. A unit is 8 NT of a key/value head's at most, or
@@ -112,8 +112,6 @@ __global__ void __launch_bounds__(kThreads, C::ctas(kNt)) paged_attention_kernel
     const int n = a.lens[b];
     return n < 0 ? 0 : n > room ? static_cast<int>(room) : n;
   };
-  // (a block of 16 positions has to begin at one of the sequence's)
-  auto base_of = [&](int b) -> int { return C::first_own(a, b, length(b)) & ~15; };
   auto tiles_of = [&](int n) { return n <= kTile ? 1 : (n + kTile - 1) / kTile; };
 
   unsigned long long x = 0, last = 1;
@@ -132,7 +130,7 @@ __global__ void __launch_bounds__(kThreads, C::ctas(kNt)) paged_attention_kernel
     const int per = (c.seqs + kThreads - 1) / kThreads, b0 = min(c.seqs, tid * per), b1 = min(c.seqs, b0 + per);
     u64 mine = 0, padded = 0;
     for (int i = b0; i < b1; ++i) {
-      const int n = tiles_of(length(i) - base_of(i));
+      const int n = tiles_of(length(i));
       if (a.lens[i] > room && blockIdx.x == 0) atomicOr(&g_paged_err, kErrIndex);
       mine += span_of(n, 0);
       padded += span_of(n, 1);
@@ -173,14 +171,11 @@ __global__ void __launch_bounds__(kThreads, C::ctas(kNt)) paged_attention_kernel
     const int outer = C::kHeadsOuter ? static_cast<int>(quotient(first, total / units)) : 0;
     const u64 before = outer * (total / units);
     if (tid == 0) split[blockIdx.x] = make_int4(0, 0, -1, 0);
-    if (first >= total) {  // (the whole CTA)
-      if (C::kOwnOnly) pdl_wait();
-      return;
-    }
+    if (first >= total) return;  // (the whole CTA)
     if (first - before >= (upto - mine) * each && first - before < upto * each) {
       u64 at = (upto - mine) * each + before;
       for (int i = b0; i < b1; ++i) {
-        const u64 n = static_cast<u64>(span_of(tiles_of(length(i) - base_of(i)), pieces)) * each;
+        const u64 n = static_cast<u64>(span_of(tiles_of(length(i)), pieces)) * each;
         if (first < at + n) {
           plan.b = i;
           break;
@@ -198,13 +193,15 @@ __global__ void __launch_bounds__(kThreads, C::ctas(kNt)) paged_attention_kernel
     x = plan.first;
     last = x + plan.q + (blockIdx.x < plan.r ? 1 : 0);
     b = plan.b;
-    const int span = span_of(tiles_of(length(b) - base_of(b)), plan.pieces);
+    const int span = span_of(tiles_of(length(b)), plan.pieces);
     const int at = C::kHeadsOuter ? 0 : static_cast<int>(quotient(x - plan.at, span));
     u = plan.u + at;
     tile = static_cast<int>(x - plan.at - static_cast<unsigned long long>(at) * span);
   }
   while (x < last && (C::kHeadsOuter ? u < units : b < c.seqs)) {
-    const int len = length(b), base = base_of(b), tiles = tiles_of(len - base);
+    const int len = length(b);
+    const typename C::Behind behind(a, b, len);
+    const int base = behind.from & ~15, tiles = tiles_of(len - base);  // (a block of 16 positions begins at one of the sequence's)
     int stop, tile_end;
     if (kCluster) {  // the CTA's share of the unit (none: a part of no weight)
       tile = rank * tiles / cs;
@@ -252,9 +249,8 @@ __global__ void __launch_bounds__(kThreads, C::ctas(kNt)) paged_attention_kernel
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[n][hh][j][e] = 0.0f;
     }
-    const Unit un = {c.table + static_cast<long long>(C::table_row(a, b, len)) * c.table_ld, b, hk, wh0, heads, len, C::first_own(a, b, len), base};
+    const Unit un = {c.table + static_cast<long long>(behind.row) * c.table_ld, b, hk, wh0, heads, len, behind.from, base};
     C::template attend<kNt>(a, un, tile, tile_end, sq[warp], so + warp * kWarpFloats, acc);
-    if (C::kOwnOnly) pdl_wait();  // the prefix's parts
 
     // The warps' parts into shared memory.
 #pragma unroll
@@ -316,6 +312,8 @@ __global__ void __launch_bounds__(kThreads, C::ctas(kNt)) paged_attention_kernel
         }
       });
       cluster_sync();
+      // (one CTA of the grid ends behind the prefix kernel, so that who waits for this kernel waits for that one too)
+      if (C::kOwnOnly && blockIdx.x == gridDim.x - 1) pdl_wait();
       if (rank != 0) return;
       for (int i = tid; i < uh.count * (kDh / 4); i += kThreads) {
         const int h = i / (kDh / 4), d = (i % (kDh / 4)) * 4;
@@ -357,7 +355,6 @@ __global__ void __launch_bounds__(kThreads, C::ctas(kNt)) paged_attention_kernel
 
     next_unit();
   }
-  if (C::kOwnOnly) pdl_wait();
 }
 
 // Joins the units that several CTAs share: CTA (x, y) head y of the unit that
@@ -535,10 +532,6 @@ cudaError_t launch_clusters(const typename C::Args& a, int units, int cs, cudaSt
 template <class C, int kNt>
 cudaError_t launch(const typename C::Args& a, cudaStream_t stream, unsigned int* launches) {
   constexpr size_t smem = static_cast<size_t>(kWarps) * C::warp_floats(kNt) * sizeof(float);
-  static SmemLimit limit;
-  auto* kernel = paged_attention_kernel<C, kNt, false>;
-  const cudaError_t le = limit.allow(kernel, smem);
-  if (le != cudaSuccess) return le;
   // CTAs for every tile that the table has room for, at most a wave
   const int group = a.H / a.kv.Hkv;
   const long long units = static_cast<long long>(a.kv.Hkv / C::kSplit) * ((group + 8 * kNt - 1) / (8 * kNt)) * a.kv.seqs;
@@ -552,16 +545,22 @@ cudaError_t launch(const typename C::Args& a, cudaStream_t stream, unsigned int*
   // wider ones (8 heads 4.7, 8.7). us, with it and without: one sequence of 704 x 40 heads 6.2, 9.4, of 2048 x 8 6.5, 9.0, of 4096 x 8 11.0, 10.7, half as long as the table 4.1,
   // 7.9; 16 of up to 768 x 8 10.3, 13.7, 12 of up to 768 x 32 (12 tiles) 21.2, 19.6. A CTA for each of up to twice as many units of few tiles: 25 of 128 x 32
   // 14.2, 15.9, of 256 22.0, 23.5 (of five waves: 100 of 200 x 32 73, 66).
-  if (units <= wave || (units <= 2 * wave && room <= 2 * kMinTiles)) {
+  if (C::kOwnOnly || units <= wave || (units <= 2 * wave && room <= 2 * kMinTiles)) {
     const bool spread = units * room <= num_sms();  // a tile each (256 x 32 heads 3.9, of two 4.8; 4 of 512 x 8 5.5, 4.9)
     int cs = static_cast<int>(std::min<long long>(kMaxCluster, spread ? room : (room + kMinTiles - 1) / kMinTiles));
     while (cs > 1 && units * 8 > clusters_at_once<C, kNt>(cs) * 7) --cs;
-    if ((room + cs - 1) / cs <= units * room / (3 * wave) + kJoinTiles)
+    // (Behind a prefix the table says nothing of the lengths.)
+    if (C::kOwnOnly || (room + cs - 1) / cs <= units * room / (3 * wave) + kJoinTiles)
       return launch_clusters<C, kNt>(a, static_cast<int>(units), cs, stream, launches);
   }
+  if constexpr (!C::kOwnOnly) {
+  static SmemLimit limit;
+  auto* kernel = paged_attention_kernel<C, kNt, false>;
+  cudaError_t e = limit.allow(kernel, smem);
+  if (e != cudaSuccess) return e;
   int grid = room >= wave || units >= wave ? wave : static_cast<int>(std::min<long long>(wave, units * room));
   if (C::kHeadsOuter && grid >= 8 * (units / a.kv.seqs)) grid -= grid % static_cast<int>(units / a.kv.seqs);
-  cudaError_t e = launch_pdl(kernel, dim3(static_cast<unsigned>(grid)), dim3(kThreads), smem, stream, a);
+  e = launch_pdl(kernel, dim3(static_cast<unsigned>(grid)), dim3(kThreads), smem, stream, a);
   if (e != cudaSuccess) return e;
   ++*launches;
   const unsigned heads = static_cast<unsigned>(C::kSplit > 1 ? C::kSplit * group : std::min(group, 8 * kNt));
@@ -569,6 +568,8 @@ cudaError_t launch(const typename C::Args& a, cudaStream_t stream, unsigned int*
                  a);
   if (e == cudaSuccess) ++*launches;
   return e;
+  }
+  return cudaErrorInvalidValue;  // (not reached)
 }
 
 unsigned int read_and_clear_paged_error() {

@@ -92,17 +92,7 @@ struct Rows {
   static __host__ __device__ constexpr int warp_floats(int nt) { return 8 * nt * kDh; }  // (for its part of O)
   static __host__ __device__ constexpr int ctas(int nt) { return nt == 1 ? 3 : 2; }
   static __device__ __forceinline__ bool bf16(const Args&) { return kBf16; }
-  static __device__ __forceinline__ int first_own(const Args& a, int b, int len) {
-    if constexpr (kOwn) return prefix_seen(a, b, len);
-    return 0;
-  }
-  static __device__ __forceinline__ int table_row(const Args& a, int b, int len) {
-    if constexpr (kOwn) return row_of(a, b, len);
-    return b;
-  }
-  static __device__ __forceinline__ void add_prefix(const Args& a, int b, int h, int d, float& m, float& sum, float4& v) {
-    if constexpr (kOwn) add_prefix_parts(a, b, h, d, m, sum, v);
-  }
+  typedef std::conditional_t<kOwn, PrefixOf, NoPrefix> Behind;
   static __device__ __forceinline__ int first_dim(int hh, int g) { return 64 * hh + 8 * g; }
 
   // Goes through tiles tile .. tile_end - 1 of the unit. sq: the warp's place for the query operand.

@@ -8,15 +8,15 @@
 // prefix's parts at its end and writes the outputs. It needs nothing of the first before
 // that, so it starts beside it, on what the first leaves free of the SMs.
 //
-// prefix_kernel: units and ranges as p4q_paged_prefix.cuh says. Nine warps:
+// prefix_kernel: units and ranges as p4q_paged_prefix.cuh says. Thirteen warps:
 //   warps 0-3  queries, keys and values into shared memory with 16-byte asynchronous copies (pages
 //              may be of any size and order, and positions past the prefix or of a page outside the
 //              cache have to be zeros: 0 weight times an infinite value is NaN), in the 128-byte
 //              swizzle that the products read; two stages each of keys and values;
-//   warps 4-7  one thread per row (its TMEM lane): scores' maximum, p = 2^(s - reference),
+//   warps 4-11 two threads per row (its TMEM lane): scores' maximum, p = 2^(s - reference),
 //              their sum, p as two fp16 or three bf16 values over the scores in TMEM; the
 //              reference moves, and O with it, only when a score exceeds it by 2^4 (bf16 2^8);
-//   warp 8     issues the products: S = Q K^T of the next chunk, then O += P V of this one, with
+//   warp 12    issues the products: S = Q K^T of the next chunk, then O += P V of this one, with
 //              P from TMEM and V in place as an MN-major operand.
 // p goes into the product in parts for the reasons that p4q_paged_rows.cuh gives, by the same
 // rules. Every wait is bounded; a time-out sets the device error word.
@@ -32,19 +32,24 @@ namespace {
 
 __device__ unsigned int g_prefix_wait_err;
 
-constexpr int kProducers = 4, kSoftmax = 4;          // warps
-constexpr int kPrefixThreads = 32 * (kProducers + kSoftmax + 1);
+constexpr int kProducers = 4, kSoftmax = 8;          // warps
+constexpr int kMmaWarp = kProducers + kSoftmax;
+constexpr int kPrefixThreads = 32 * (kMmaWarp + 1);
+// (more than there are: 96 registers per thread, which leave room for a CTA of the own positions' kernel beside)
+constexpr int kPrefixBound = 640;
 constexpr int kMaxPrefixGrid = 160;
 constexpr int kTileBytes = 16384;                    // 128 rows of 128 bytes
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kColS = 128, kSCols = 192;        // O: columns 0 .. 127; two S buffers, with room for P's third part
-constexpr int kMetas = 4;                            // of chunks' valid positions, see the producers
+constexpr int kKStages = 3, kVStages = 2;            // (keys are wanted a chunk earlier than values)
+constexpr int kMetas = 8;                            // of chunks' valid positions, see the producers
 
 struct Bars {
-  uint64_t q_full, q_empty, k_full[2], k_empty[2], v_full[2], v_empty[2], meta_full[kMetas];
+  uint64_t q_full, q_empty, k_full[kKStages], k_empty[kKStages], v_full[kVStages], v_empty[kVStages], meta_full[kMetas];
   uint64_t s_full[2], p_ready[2], pv_done[2], o_free, mma_done;
   unsigned long long first, base, share, total;  // the CTA's range and the start of its first group
   int group;
+  Group its;                                     // (that group)
   uint32_t valid[kMetas][kProducers];
   uint32_t tmem_slot;
   int abort_flag;
@@ -52,7 +57,7 @@ struct Bars {
 
 template <int kDh>
 constexpr int smem_bytes() {
-  return (kDh / 64) * kTileBytes * 5 + static_cast<int>(sizeof(Bars)) + 1024;
+  return (kDh / 64) * kTileBytes * (1 + kKStages + kVStages) + static_cast<int>(sizeof(Bars)) + 1024;
 }
 
 __device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void* src, bool full) {
@@ -85,6 +90,12 @@ __device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t (&r)[
       : "memory");
 }
 
+__device__ __forceinline__ void tmem_st_x8(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]),
+               "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // kind::f16 with fp16 or bf16 A and B (K-major; bit 16 set: B MN-major) and an fp32 accumulator, M x N.
@@ -92,6 +103,12 @@ template <bool kBf16>
 constexpr uint32_t idesc16(int M, int N) {
   return (1u << 4) | (kBf16 ? (1u << 7) | (1u << 10) : 0u) | (static_cast<uint32_t>(N >> 3) << 17) |
          (static_cast<uint32_t>(M >> 4) << 24);
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
 }
 
 // A and B from shared memory.
@@ -128,10 +145,11 @@ struct Walk {
   int g;
   Group gr;
   int hk, tile, c0, c1;
+  int copies;  // of the tile's rows, see the softmax
   __device__ Walk(const PrefixArgs& a, const Bars& br) : x(br.first), base(br.base), g(br.group) {
     end = min(br.total, x + br.share);
     if (x < end) {
-      gr = load_group(a, g);
+      gr = br.its;
       find(a);
     }
   }
@@ -141,11 +159,13 @@ struct Walk {
       base += group_chunks(a, gr);
       gr = load_group(a, ++g);
     }
-    const unsigned int at = static_cast<unsigned int>((x - base) / static_cast<unsigned int>(gr.chunks));
+    const unsigned int at = static_cast<unsigned int>(quotient(x - base, gr.chunks));
     c0 = static_cast<int>(x - base - static_cast<unsigned long long>(at) * gr.chunks);
     c1 = static_cast<int>(min(static_cast<unsigned long long>(gr.chunks), c0 + (end - x)));
     hk = static_cast<int>(at) / gr.tiles;
     tile = static_cast<int>(at) - hk * gr.tiles;
+    const int rows = gr.n * (a.H / a.kv.Hkv) - tile * kPrefixRows;
+    copies = copies_of(rows);
   }
   __device__ void next(const PrefixArgs& a) {
     x += c1 - c0;
@@ -154,12 +174,12 @@ struct Walk {
 };
 
 template <bool kBf16, int kDh>
-__global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const PrefixArgs a) {
+__global__ void __launch_bounds__(kPrefixBound) prefix_kernel(const PrefixArgs a) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   constexpr int kHalves = kDh / 64;                 // 128-byte halves of a row
   constexpr int kOperand = kHalves * kTileBytes;
-  constexpr int kOffK = kOperand, kOffV = 3 * kOperand, kOffBars = 5 * kOperand;
+  constexpr int kOffK = kOperand, kOffV = kOffK + kKStages * kOperand, kOffBars = kOffV + kVStages * kOperand;
   constexpr int kPw = kParts<kBf16>;
   Bars& br = *reinterpret_cast<Bars*>(smem + kOffBars);
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
@@ -170,11 +190,15 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const PrefixA
   if (t == 0) {
     mbar_init(&br.q_full, 32 * kProducers);
     mbar_init(&br.q_empty, 1);
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < kKStages; ++i) {
       mbar_init(&br.k_full[i], 32 * kProducers);
       mbar_init(&br.k_empty[i], 1);
+    }
+    for (int i = 0; i < kVStages; ++i) {
       mbar_init(&br.v_full[i], 32 * kProducers);
       mbar_init(&br.v_empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
       mbar_init(&br.s_full[i], 1);
       mbar_init(&br.p_ready[i], kSoftmax);
       mbar_init(&br.pv_done[i], 1);
@@ -185,7 +209,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const PrefixA
     br.abort_flag = 0;
     fence_barrier_init();
   }
-  if (warp == 8) {
+  if (warp == kMmaWarp) {
     tmem_alloc(&br.tmem_slot, kTmemCols);
     tmem_relinquish();
   }
@@ -193,44 +217,54 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const PrefixA
   pdl_launch_dependents();
   if (warp == 0) {
     // the chunks before each group, their sum, and the group that the CTA's range begins in
-    unsigned long long total = 0;
-    for (int pass = 0; pass < 2; ++pass) {
-      const unsigned long long share = prefix_share(total, a.grid), first = blockIdx.x * share;
-      unsigned long long upto = 0;
-      for (int g0 = 0; g0 < a.groups; g0 += 32) {
+    unsigned long long total = 0, last_begin = 0, last_end = 0;
+    int most = 0;  // chunks of a unit
+    Group gr = {};
+    for (int g0 = 0; g0 < a.groups; g0 += 32) {
+      const int g = g0 + lane;
+      unsigned long long n = 0;
+      if (g < a.groups) {
+        gr = load_group(a, g);
+        n = group_chunks(a, gr);
+        if (n > 0) most = max(most, gr.chunks);
+        if (blockIdx.x == 0 && (a.group_start[g] < 0 || a.group_start[g + 1] < a.group_start[g] ||
+                                a.group_start[g + 1] > c.seqs || a.prefix_lens[g] > paged_room(c)))
+          atomicOr(&g_paged_err, kErrIndex);
+      }
+      __syncwarp();
+      const unsigned long long upto = total + scan_add(n);
+      last_begin = upto - n;
+      last_end = upto;
+      total = __shfl_sync(0xFFFFFFFFu, upto, 31);
+    }
+    most = __reduce_max_sync(0xFFFFFFFFu, most);
+    const unsigned long long share = prefix_share(total, most, a.grid);
+    const unsigned long long first = blockIdx.x * share;
+    auto look = [&](int g, unsigned long long begin, unsigned long long end) {
+      if (first >= begin && first < end) {
+        br.group = g;
+        br.base = begin;
+        br.its = gr;
+      }
+    };
+    if (a.groups <= 32) {
+      look(lane, last_begin, last_end);
+    } else {
+      unsigned long long sum = 0;
+      for (int g0 = 0; g0 < a.groups && sum <= first; g0 += 32) {
         const int g = g0 + lane;
-        unsigned long long n = 0;
-        if (g < a.groups) {
-          n = group_chunks(a, load_group(a, g));
-          if (pass == 0 && blockIdx.x == 0 &&
-              (a.group_start[g] < 0 || a.group_start[g + 1] < a.group_start[g] || a.group_start[g + 1] > c.seqs ||
-               a.prefix_lens[g] > paged_room(c)))
-            atomicOr(&g_paged_err, kErrIndex);
-        }
-        unsigned long long s = n;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-          const unsigned long long v = __shfl_up_sync(0xFFFFFFFFu, s, d);
-          if (lane >= d) s += v;
-        }
-        const unsigned long long before = upto + s - n;
-        if (pass == 1) {
-          if (blockIdx.x == 0 && g < a.groups) a.base[g] = before;
-          if (g < a.groups && first >= before && first < before + n) {
-            br.group = g;
-            br.base = before;
-          }
-        }
-        upto += __shfl_sync(0xFFFFFFFFu, s, 31);
+        gr = g < a.groups ? load_group(a, g) : Group{};
+        const unsigned long long n = g < a.groups ? group_chunks(a, gr) : 0;
+        __syncwarp();
+        const unsigned long long upto = sum + scan_add(n);
+        look(g, upto - n, upto);
+        sum = __shfl_sync(0xFFFFFFFFu, upto, 31);
       }
-      if (pass == 0) {
-        total = upto;
-      } else if (lane == 0) {
-        if (blockIdx.x == 0) a.base[a.groups] = total;
-        br.first = first;
-        br.share = share;
-        br.total = total;
-      }
+    }
+    if (lane == 0) {
+      br.first = first;
+      br.share = share;
+      br.total = total;
     }
   }
   tc_fence_before();
@@ -265,39 +299,39 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const PrefixA
       int page = page_of(w.c0);
       if (uq > 0) ok = mbar_wait_all(&br.q_empty, (uq - 1) & 1, abort_flag, &g_prefix_wait_err);
       if (!ok) break;
-      const int idx = w.tile * kPrefixRows + warp * 32 + lane;
+      const int idx = w.tile * kPrefixRows + (warp * 32 + lane & kPrefixRows / w.copies - 1);
       const uint16_t* qrow = nullptr;
       if (idx < w.gr.n * G)
         qrow = a.q + (w.gr.first + idx / G) * a.ldq + static_cast<long long>(w.hk * G + idx % G) * kDh;
       copy_rows(smem, qrow, a.q);
       cp_async_arrive(&br.q_full);
       for (int ch = w.c0; ch < w.c1; ++ch, ++j) {
-        const int st = j & 1;
+        const int vs = j % kVStages, ks = j % kKStages;
         const int p = ch * kPrefixChunk + warp * 32 + lane;
         const bool valid = p < w.gr.prefix && static_cast<unsigned int>(page) < static_cast<unsigned int>(c.pages);
         const long long off = valid ? page * c.page_stride + (p & ((1 << c.page_log2) - 1)) * c.token_stride + w.hk * c.head_stride : 0;
         page = page_of(ch + 1);
-        if (j >= 2) ok = mbar_wait_all(&br.k_empty[st], ((j >> 1) - 1) & 1, abort_flag, &g_prefix_wait_err);
+        if (j >= kKStages) ok = mbar_wait_all(&br.k_empty[ks], (j / kKStages - 1) & 1, abort_flag, &g_prefix_wait_err);
         if (!ok) break;
-        // The scores' warps read it after S of this chunk, whose product ran before that of chunk
-        // j + kMetas - 2 released the stage that is waited for here; by then they had
-        // this chunk's P ready, which the P V before that product waits for.
+        // Its place held those of chunk j - kMetas, which have been read: the product waited for here, S of chunk
+        // j - kKStages, was issued behind P V of chunk j - kKStages - 2, and that one waited for the weights.
+        static_assert(kMetas >= kKStages + 2, "valid positions");
         const uint32_t bits = __ballot_sync(0xFFFFFFFFu, valid);
         if (lane == 0) {
           br.valid[j & (kMetas - 1)][warp] = bits;
           mbar_arrive(&br.meta_full[j & (kMetas - 1)]);
         }
-        copy_rows(smem + kOffK + st * kOperand, valid ? c.k + off : nullptr, c.k);
-        cp_async_arrive(&br.k_full[st]);
-        if (j >= 2) ok = mbar_wait_all(&br.v_empty[st], ((j >> 1) - 1) & 1, abort_flag, &g_prefix_wait_err);
+        copy_rows(smem + kOffK + ks * kOperand, valid ? c.k + off : nullptr, c.k);
+        cp_async_arrive(&br.k_full[ks]);
+        if (j >= kVStages) ok = mbar_wait_all(&br.v_empty[vs], (j / kVStages - 1) & 1, abort_flag, &g_prefix_wait_err);
         if (!ok) break;
-        copy_rows(smem + kOffV + st * kOperand, valid ? c.v + off : nullptr, c.v);
-        cp_async_arrive(&br.v_full[st]);
+        copy_rows(smem + kOffV + vs * kOperand, valid ? c.v + off : nullptr, c.v);
+        cp_async_arrive(&br.v_full[vs]);
       }
     }
     cp_async_commit();
     cp_async_wait<0>();  // nothing of this CTA's copies may be in flight when it exits
-  } else if (warp == 8) {
+  } else if (warp == kMmaWarp) {
     // ---------------------------------------------------------------- products
     const bool leader = elect_one();
     bool ok = true;
@@ -311,14 +345,14 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const PrefixA
     Walk s(a, br);
     int js = 0, us = 0, cs = s.more() ? s.c0 : 0;
     auto issue_s = [&]() {
-      const int st = js & 1;
+      const int st = js & 1, ks = js % kKStages;
       if (cs == s.c0) ok = ok && mbar_wait_all(&br.q_full, us & 1, abort_flag, &g_prefix_wait_err);
-      ok = ok && mbar_wait_all(&br.k_full[st], (js >> 1) & 1, abort_flag, &g_prefix_wait_err);
+      ok = ok && mbar_wait_all(&br.k_full[ks], (js / kKStages) & 1, abort_flag, &g_prefix_wait_err);
       if (!ok) return;
       fence_proxy_async_smem();  // the copies are seen by the products
       tc_fence_after();
       const uint32_t d = tmem + kColS + kSCols * static_cast<uint32_t>(st);
-      const uint64_t b0 = k_desc + static_cast<uint32_t>(st * (kOperand >> 4));
+      const uint64_t b0 = k_desc + static_cast<uint32_t>(ks * (kOperand >> 4));
       const bool last = cs + 1 == s.c1;
       if (leader) {
 #pragma unroll
@@ -327,7 +361,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const PrefixA
           for (int k = 0; k < 4; ++k)
             mma_ss(d, q_desc + kb * (kTileBytes >> 4) + 2 * k, b0 + kb * (kTileBytes >> 4) + 2 * k, idS, (kb | k) != 0 ? 1u : 0u);
         mma_commit(&br.s_full[st]);
-        mma_commit(&br.k_empty[st]);
+        mma_commit(&br.k_empty[ks]);
         if (last) mma_commit(&br.q_empty);
       }
       ++js;
@@ -344,23 +378,23 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const PrefixA
     for (Walk w(a, br); w.more() && ok; w.next(a), ++uq) {
       for (int ch = w.c0; ch < w.c1 && ok; ++ch, ++j) {
         if (s.more()) issue_s();
-        const int st = j & 1;
+        const int st = j & 1, vs = j % kVStages;
         ok = ok && mbar_wait_all(&br.p_ready[st], (j >> 1) & 1, abort_flag, &g_prefix_wait_err);
         if (ch == w.c0 && uq > 0) ok = ok && mbar_wait_all(&br.o_free, (uq - 1) & 1, abort_flag, &g_prefix_wait_err);
-        ok = ok && mbar_wait_all(&br.v_full[st], (j >> 1) & 1, abort_flag, &g_prefix_wait_err);
+        ok = ok && mbar_wait_all(&br.v_full[vs], (j / kVStages) & 1, abort_flag, &g_prefix_wait_err);
         if (!ok) break;
         fence_proxy_async_smem();
         tc_fence_after();
         const uint32_t pa = tmem + kColS + kSCols * static_cast<uint32_t>(st);
-        const uint64_t b0 = v_desc + static_cast<uint32_t>(st * (kOperand >> 4));
+        const uint64_t b0 = v_desc + static_cast<uint32_t>(vs * (kOperand >> 4));
         if (leader) {
 #pragma unroll
           for (int kt = 0; kt < kPrefixChunk / 16; ++kt)  // 16 positions per product: 8 columns of P, 16 rows of V
 #pragma unroll
             for (int i = 0; i < kPw; ++i)
-              mma_ts(tmem, pa + (i < 2 ? 32u * (kt >> 1) + 16u * i + 8u * (kt & 1) : 128u + 8u * kt), b0 + (2048 >> 4) * kt, idO,
+              mma_ts(tmem, pa + (i < 2 ? 16u * kt + 8u * i : 128u + 8u * kt), b0 + (2048 >> 4) * kt, idO,
                      (ch > w.c0 || kt > 0 || i > 0) ? 1u : 0u);
-          mma_commit(&br.v_empty[st]);
+          mma_commit(&br.v_empty[vs]);
           mma_commit(&br.pv_done[st]);
         }
       }
@@ -372,59 +406,86 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const PrefixA
     }
   } else {
     // ---------------------------------------------------------------- softmax
-    const int quad = warp & 3, r = quad * 32 + lane;
+    // Two warps per 32 rows: both find the rows' maxima (which spares them an exchange), each makes the
+    // weights of every other piece of 16 positions and has half of O's columns.
+    // A tile of 32 rows and less stands in the products four times, of 64 and less twice; each copy
+    // has weights for its share of a chunk's positions only, so that all warps work on them, and leaves
+    // a part of its own. (For the others a copy has the least weights there are, not 0, which
+    // would make NaN of an infinite value: 2^-34 of that at the reference in fp16, 2^-125 in bf16.)
+    constexpr uint32_t kNone = kBf16 ? 0x00800080u : 0x00010001u;
+    constexpr int kPieces = kPrefixChunk / 16;
+    const int quad = warp & 3, half = (warp - kProducers) >> 2, r = quad * 32 + lane;
     const uint32_t tl = tmem + (static_cast<uint32_t>(quad * 32) << 16);
     const float c2 = a.scale * 1.4426950408889634f;
+    const float2 c22 = make_float2(c2, c2);
     const int pitch = kDh + kPartExtra;
     bool ok = true;
     int j = 0;
-    for (Walk w(a, br); w.more() && ok; w.next(a)) {
-      const int rows = w.gr.n * G, idx = w.tile * kPrefixRows + r;
-      const bool used = w.tile * kPrefixRows + quad * 32 < rows;  // (some row of the warp)
+    // (After a failed wait a warp walks on without waits and work, so that the other one of its rows is
+    // never left at their barrier.)
+    for (Walk w(a, br); w.more(); w.next(a)) {
+      const int per = kPrefixRows / w.copies, copy = r / per;  // rows of a copy
+      const int rows = w.gr.n * G, idx = w.tile * kPrefixRows + (r & per - 1);
+      const bool used = w.tile * kPrefixRows + (quad * 32 & per - 1) < rows;  // (some row of the warp)
       const int b = w.gr.first + min(idx, rows - 1) / G;
-      const bool counts = idx < rows && a.lens[b] >= w.gr.prefix;
+      const int i0 = copy * (kPieces / w.copies), i1 = i0 + kPieces / w.copies;  // its pieces
       float ref = -INFINITY, l = 0.0f;
+      uint32_t lost = 0;
       for (int ch = w.c0; ch < w.c1; ++ch, ++j) {
         const int st = j & 1, me = j & (kMetas - 1);
         const uint32_t ts = tl + kColS + kSCols * static_cast<uint32_t>(st);
-        ok = mbar_wait_all(&br.meta_full[me], (j / kMetas) & 1, abort_flag, &g_prefix_wait_err);
+        ok = ok && mbar_wait_all(&br.meta_full[me], (j / kMetas) & 1, abort_flag, &g_prefix_wait_err);
         ok = ok && mbar_wait_all(&br.s_full[st], (j >> 1) & 1, abort_flag, &g_prefix_wait_err);
-        if (!ok) break;
         tc_fence_after();
-        if (used) {
+        if (used && !ok) named_bar_sync(1 + quad, 64);
+        if (used && ok) {
+          if (w.copies > 1) {  // other copies' pieces
+            uint32_t none[16], none2[8];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) none[e] = kNone;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) none2[e] = kNone;
+#pragma unroll 1
+            for (int i = half; i < kPieces; i += 2)
+              if (i < i0 || i >= i1) {
+                tmem_st_x16(ts + 16u * i, none);
+                if constexpr (kBf16) tmem_st_x8(ts + 128u + 8u * i, none2);
+              }
+          }
           uint32_t valid[4];
-          bool all = true;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            valid[i] = br.valid[me][i];
-            all = all && valid[i] == 0xFFFFFFFFu;
-          }
-          if (!all && counts) {  // a page outside the cache, among the prefix's positions
+          for (int i = 0; i < 4; ++i) valid[i] = br.valid[me][i];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int left = w.gr.prefix - (ch * kPrefixChunk + 32 * i);
-              const uint32_t want = left >= 32 ? 0xFFFFFFFFu : left <= 0 ? 0u : (1u << left) - 1u;
-              if (want & ~valid[i]) atomicOr(&g_paged_err, kErrIndex);
-            }
+          for (int i = 0; i < 4; ++i) {  // a page outside the cache, among the prefix's positions
+            const int left = w.gr.prefix - (ch * kPrefixChunk + 32 * i);
+            lost |= ~valid[i] & (left >= 32 ? 0xFFFFFFFFu : left <= 0 ? 0u : (1u << left) - 1u);
           }
-          __syncwarp();
+          auto valid16 = [&](int i) { return (i & 4 ? (i & 2 ? valid[3] : valid[2]) : (i & 2 ? valid[1] : valid[0])) >> (16 * (i & 1)) & 0xFFFFu; };
           float top = -INFINITY;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
+#pragma unroll 1
+          for (int i = i0; i < i1; i += 2) {  // (an even number)
             uint32_t s[32];
-            tmem_ld_32x32b_x32(ts + 32u * i, s);
+            tmem_ld_32x32b_x32(ts + 16u * i, s);
+            const uint32_t v = valid16(i) | valid16(i + 1) << 16;
             tmem_ld_wait();
-            float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-            if (valid[i] == 0xFFFFFFFFu) {
-#pragma unroll
-              for (int e = 0; e < 32; ++e) m4[e & 3] = fmaxf(m4[e & 3], __uint_as_float(s[e]) * c2);
-            } else {
+            if (v != 0xFFFFFFFFu) {
 #pragma unroll
               for (int e = 0; e < 32; ++e)
-                if (valid[i] >> e & 1u) m4[e & 3] = fmaxf(m4[e & 3], __uint_as_float(s[e]) * c2);
+                if (!(v >> e & 1u)) s[e] = 0x7FFFFFFFu;  // (NaN: no maximum)
             }
-            top = fmaxf(top, fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])));
+            float m4[4] = {top, top, top, top};
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+              const float2 x = __fmul2_rn(make_float2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), c22);
+              const float2 y = __fmul2_rn(make_float2(__uint_as_float(s[e + 2]), __uint_as_float(s[e + 3])), c22);
+              m4[e >> 2 & 3] = max3(m4[e >> 2 & 3], x.x, x.y);
+              m4[(e >> 2) + 2 & 3] = max3(m4[(e >> 2) + 2 & 3], y.x, y.y);
+            }
+            top = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
           }
+          // both warps have read all of their rows' scores: either overwrites only its own pieces with weights,
+          // but the other one's maxima are of all
+          named_bar_sync(1 + quad, 64);
           float alpha = 1.0f;
           if (top > ref + kMove<kBf16>) {  // (-inf: the first score)
             alpha = exp2_fast(ref - top);
@@ -433,46 +494,54 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const PrefixA
           }
           __syncwarp();
           const float from = ref == -INFINITY ? 0.0f : ref - kShift<kBf16>;
-          float l4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+          const float2 from2 = make_float2(-from, -from);
+          float2 l2[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
 #pragma unroll 1
-          for (int i = 0; i < 4; ++i) {
-            uint32_t s[32];
-            tmem_ld_32x32b_x32(ts + 32u * i, s);
+          for (int i = i0 + half; i < i1; i += 2) {
+            uint32_t s[16], p01[16], p2[8];
+            tmem_ld_32x32b_x16(ts + 16u * i, s);
+            const uint32_t v = valid16(i);
             tmem_ld_wait();
-            uint32_t p01[32], p2[16];
+            auto weights = [&](auto whole) {
 #pragma unroll
-            for (int e = 0; e < 32; e += 2) {
-              float x0 = __uint_as_float(s[e]) * c2, x1 = __uint_as_float(s[e + 1]) * c2;
-              if (valid[i] != 0xFFFFFFFFu) {
-                if (!(valid[i] >> e & 1u)) x0 = -INFINITY;
-                if (!(valid[i] >> e & 2u)) x1 = -INFINITY;
+              for (int e = 0; e < 16; e += 2) {
+                float2 x = __ffma2_rn(make_float2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), c22, from2);
+                if constexpr (!decltype(whole)::value) {
+                  if (!(v >> e & 1u)) x.x = -INFINITY;
+                  if (!(v >> e & 2u)) x.y = -INFINITY;
+                }
+                const float2 p = make_float2(exp2_fast(x.x), exp2_fast(x.y));
+                l2[e >> 1 & 1] = __fadd2_rn(l2[e >> 1 & 1], p);
+                uint32_t part[kPw];
+                split2<kBf16>(p.x, p.y, part);
+                p01[e / 2] = part[0];
+                p01[8 + e / 2] = part[1];
+                if constexpr (kBf16) p2[e / 2] = part[2];
               }
-              const float p0 = exp2_fast(x0 - from), p1 = exp2_fast(x1 - from);
-              l4[e & 2] += p0;
-              l4[(e & 2) + 1] += p1;
-              uint32_t part[kPw];
-              split2<kBf16>(p0, p1, part);
-              p01[e / 2] = part[0];
-              p01[16 + e / 2] = part[1];
-              if constexpr (kBf16) p2[e / 2] = part[2];
-            }
-            tmem_st_x32(ts + 32u * i, p01);
-            if constexpr (kBf16) tmem_st_x16(ts + 128u + 16u * i, p2);
+            };
+            if (v == 0xFFFFu)
+              weights(std::true_type{});
+            else
+              weights(std::false_type{});
+            __syncwarp();
+            tmem_st_x16(ts + 16u * i, p01);
+            if constexpr (kBf16) tmem_st_x8(ts + 128u + 8u * i, p2);
           }
-          l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
+          l += (l2[0].x + l2[0].y) + (l2[1].x + l2[1].y);
           // O of the unit's earlier chunks follows a moved reference, after their P V (the barrier of
           // chunk j - 1 cannot be a phase further: that is chunk j + 1's, which needs this warp's P)
           if (ch > w.c0 && __any_sync(0xFFFFFFFFu, alpha != 1.0f)) {
             ok = mbar_wait_all(&br.pv_done[(j - 1) & 1], ((j - 1) >> 1) & 1, abort_flag, &g_prefix_wait_err);
             tc_fence_after();
 #pragma unroll 1
-            for (int i = 0; i < kDh / 32 && ok; ++i) {
+            for (int i = 0; i < kDh / 64 && ok; ++i) {
               uint32_t o[32];
-              tmem_ld_32x32b_x32(tl + 32u * i, o);
+              const uint32_t at = tl + static_cast<uint32_t>(kDh / 2 * half + 32 * i);
+              tmem_ld_32x32b_x32(at, o);
               tmem_ld_wait();
 #pragma unroll
               for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
-              tmem_st_x32(tl + 32u * i, o);
+              tmem_st_x32(at, o);
             }
           }
           tmem_st_wait();
@@ -480,30 +549,34 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const PrefixA
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&br.p_ready[st]);
-        if (!ok) break;
       }
-      if (!ok) break;
+      if (lost != 0 && idx < rows && a.lens[b] >= w.gr.prefix) atomicOr(&g_paged_err, kErrIndex);
+      __syncwarp();
       // the part of the unit
       const int jl = j - 1;
-      ok = mbar_wait_all(&br.pv_done[jl & 1], (jl >> 1) & 1, abort_flag, &g_prefix_wait_err);
-      if (!ok) break;
+      ok = ok && mbar_wait_all(&br.pv_done[jl & 1], (jl >> 1) & 1, abort_flag, &g_prefix_wait_err);
       tc_fence_after();
-      if (used) {
+      if (used && ok) {
         const int h = w.hk * G + min(idx, rows - 1) % G;
-        float* part = w.c0 == 0 ? a.parts + (static_cast<long long>(b) * a.H + h) * pitch
-                                : a.parts + (static_cast<long long>(c.seqs) * a.H + static_cast<long long>(blockIdx.x) * kPrefixRows + r) * pitch;
+        const long long all = static_cast<long long>(c.seqs) * a.H;
+        float* part = a.parts + pitch * (w.c0 == 0 ? copy * all + static_cast<long long>(b) * a.H + h
+                                                   : kCopies * all + static_cast<long long>(blockIdx.x) * kPrefixRows + r);
 #pragma unroll 1
-        for (int i = 0; i < kDh / 32; ++i) {
+        for (int i = 0; i < kDh / 64; ++i) {
           uint32_t o[32];
+          const int at = kDh / 2 * half + 32 * i;
           __syncwarp();
-          tmem_ld_32x32b_x32(tl + 32u * i, o);
+          tmem_ld_32x32b_x32(tl + static_cast<uint32_t>(at), o);
           tmem_ld_wait();
           if (idx < rows) {
 #pragma unroll
-            for (int e = 0; e < 32; e += 4) *reinterpret_cast<uint4*>(part + 32 * i + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+            for (int e = 0; e < 32; e += 4) *reinterpret_cast<uint4*>(part + at + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
           }
         }
-        if (idx < rows) *reinterpret_cast<float2*>(part + kDh) = make_float2(ref, l);
+        if (idx < rows) {  // (the sum is of both warps' pieces)
+          if (half == 0) part[kDh] = ref;
+          part[kDh + 1 + half] = l;
+        }
         tc_fence_before();
       }
       __syncwarp();
@@ -512,7 +585,129 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const PrefixA
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 8) tmem_dealloc(tmem, kTmemCols);
+  if (warp == kMmaWarp) tmem_dealloc(tmem, kTmemCols);
+}
+
+// Adds up the parts of every head of every sequence: kWarpsPer warps per head (dh 64: two heads at once), each every
+// kWarpsPer-th part, eight of them on their way together.
+constexpr int kJoinThreads = 128;
+
+template <bool kBf16, int kDh, int kWarpsPer>
+__global__ void __launch_bounds__(kJoinThreads) prefix_join_kernel(const PrefixArgs a) {
+  constexpr int kLanes = kDh / 4, kSides = 32 / kLanes, kRows = kJoinThreads / 32 / kWarpsPer * kSides, kBatch = 8;
+  constexpr int kPitch = kDh + kPartExtra;
+  __shared__ float4 so[kJoinThreads / 32][32];
+  __shared__ float2 sml[kJoinThreads / 32][kSides];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, side = lane / kLanes, d = lane % kLanes * 4;
+  const long long rows = static_cast<long long>(a.kv.seqs) * a.H;
+  const long long at = static_cast<long long>(blockIdx.x) * kRows + warp / kWarpsPer * kSides;
+  const long long row = min(at + side, rows - 1);  // (all warps stay, for their barrier)
+  const int G = a.H / a.kv.Hkv, b0 = static_cast<int>(min(at, rows - 1) / a.H), b = static_cast<int>(row / a.H);
+  const int h = static_cast<int>(row - static_cast<long long>(b) * a.H);
+  PrefixOf of(a, b0, a.lens[b0]);
+  if (kSides > 1) {  // (the second of two heads may be the next sequence's first)
+    const int b1 = static_cast<int>(min(at + kSides - 1, rows - 1) / a.H);
+    if (b1 != b0) {
+      const PrefixOf other(a, b1, a.lens[b1]);
+      if (side == 1) of = other;
+    }
+  }
+  int parts = 0, c0 = 0, copies = 1, per = kPrefixRows, lane_row = 0;
+  if (of.g >= 0) {
+    const Group& r = of.r;
+    const unsigned long long share = prefix_share(of.total, of.most, a.grid);
+    const int i = (b - r.first) * G + h % G;
+    const unsigned long long x = of.begin + static_cast<unsigned long long>(h / G * r.tiles + i / kPrefixRows) * r.chunks;
+    c0 = min(static_cast<int>(quotient(x, share)), a.grid - 1);
+    const int c1 = min(static_cast<int>(quotient(x + r.chunks - 1, share)), a.grid - 1);
+    copies = copies_of(r.n * G - i / kPrefixRows * kPrefixRows);
+    per = kPrefixRows / copies;
+    lane_row = i % kPrefixRows;
+    parts = (c1 - c0 + 1) * copies;
+  }
+  const float* const first = a.parts + row * kPitch;
+  const float* const more = a.parts + (kCopies * rows + lane_row) * kPitch;
+  pdl_wait();
+  pdl_launch_dependents();
+  float top = -INFINITY, sum = 0.0f;
+  float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  // part 0 is that of the sequence's own positions
+  for (int k = warp % kWarpsPer; k <= parts; k += kBatch * kWarpsPer) {
+    float pm[kBatch], pl[kBatch];
+    float4 pv[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int n = k + i * kWarpsPer;
+      pm[i] = -INFINITY;
+      pl[i] = 0.0f;
+      pv[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (n <= parts) {
+        const int c = (n - 1) / copies, copy = (n - 1) % copies;
+        const float* p = n == 0   ? a.own + row * kPitch
+                         : c == 0 ? first + copy * rows * kPitch
+                                  : more + (static_cast<long long>(c0 + c) * kPrefixRows + copy * per) * kPitch;
+        const float4 ml = *reinterpret_cast<const float4*>(p + kDh);
+        pm[i] = ml.x;
+        pl[i] = ml.y + ml.z;
+        pv[i] = *reinterpret_cast<const float4*>(p + d);
+      }
+    }
+    const float old = top;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) top = fmaxf(top, pm[i]);
+    const float f = old == -INFINITY ? 0.0f : exp2_fast(old - top);
+    sum *= f;
+    v.x *= f;
+    v.y *= f;
+    v.z *= f;
+    v.w *= f;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const float e = pm[i] == -INFINITY ? 0.0f : exp2_fast(pm[i] - top);  // (of NaN sums 0 makes NaN)
+      sum += pl[i] * e;
+      if (e != 0.0f) {  // (a copy without positions has infinite values where others have)
+        v.x += pv[i].x * e;
+        v.y += pv[i].y * e;
+        v.z += pv[i].z * e;
+        v.w += pv[i].w * e;
+      }
+    }
+  }
+  if (kWarpsPer > 1) {
+    so[warp][lane] = v;
+    if (d == 0) sml[warp][side] = make_float2(top, sum);
+    __syncthreads();
+    if (warp % kWarpsPer != 0) return;
+    const float mine = top;
+#pragma unroll
+    for (int w = 1; w < kWarpsPer; ++w) top = fmaxf(top, sml[warp + w][side].x);
+    const float f = mine == -INFINITY ? 0.0f : exp2_fast(mine - top);
+    sum *= f;
+    if (f == 0.0f) v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    v.x *= f;
+    v.y *= f;
+    v.z *= f;
+    v.w *= f;
+#pragma unroll
+    for (int w = 1; w < kWarpsPer; ++w) {
+      const float2 ml = sml[warp + w][side];
+      const float e = ml.x == -INFINITY ? 0.0f : exp2_fast(ml.x - top);
+      const float4 z = so[warp + w][lane];
+      sum += ml.y * e;
+      if (e != 0.0f) {
+        v.x += z.x * e;
+        v.y += z.y * e;
+        v.z += z.z * e;
+        v.w += z.w * e;
+      }
+    }
+  }
+  if (at + side >= rows) return;
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  uint2 w = make_uint2(pack2<kBf16>(v.x * inv, v.y * inv), pack2<kBf16>(v.z * inv, v.w * inv));
+  if (sum == 0.0f) w = make_uint2(0u, 0u);
+  *reinterpret_cast<uint2*>(a.o + b * a.ldo + static_cast<long long>(h) * kDh + d) = w;
+  if (d == 0 && a.lse) a.lse[row] = sum == 0.0f ? -INFINITY : (top - kShift<kBf16>) * 0.6931471805599453f + logf(sum);
 }
 
 template <bool kBf16, int kDh>
@@ -526,23 +721,32 @@ cudaError_t launch_prefix(const PrefixArgs& a, cudaStream_t stream, unsigned int
   ++*launches;
   const bool wide = a.H / a.kv.Hkv > 8, small = a.kv.page_log2 < 4;
   if (small)
-    return wide ? launch<Rows<kBf16, kDh, true, true>, 2>(a, stream, launches) : launch<Rows<kBf16, kDh, true, true>, 1>(a, stream, launches);
-  return wide ? launch<Rows<kBf16, kDh, false, true>, 2>(a, stream, launches) : launch<Rows<kBf16, kDh, false, true>, 1>(a, stream, launches);
+    e = wide ? launch<Rows<kBf16, kDh, true, true>, 2>(a, stream, launches) : launch<Rows<kBf16, kDh, true, true>, 1>(a, stream, launches);
+  else
+    e = wide ? launch<Rows<kBf16, kDh, false, true>, 2>(a, stream, launches) : launch<Rows<kBf16, kDh, false, true>, 1>(a, stream, launches);
+  if (e != cudaSuccess) return e;
+  // four warps per head while they fit at once
+  const long long rows = static_cast<long long>(a.kv.seqs) * a.H;
+  constexpr int kSides = kDh == 64 ? 2 : 1;
+  if (rows <= 16ll * num_sms() * kSides)
+    e = launch_pdl(prefix_join_kernel<kBf16, kDh, 4>, dim3(static_cast<unsigned>((rows + kSides - 1) / kSides)), dim3(kJoinThreads), 0, stream, a);
+  else
+    e = launch_pdl(prefix_join_kernel<kBf16, kDh, 1>, dim3(static_cast<unsigned>((rows + 4 * kSides - 1) / (4 * kSides))), dim3(kJoinThreads), 0, stream, a);
+  if (e == cudaSuccess) ++*launches;
+  return e;
 }
-
-size_t base_bytes(int groups) { return ((static_cast<size_t>(groups) + 1) * sizeof(unsigned long long) + 15) / 16 * 16; }
 
 }  // namespace
 
-size_t prefix_attention_workspace_bytes(int seqs, int groups, int H, int dh) {
-  const size_t rows = static_cast<size_t>(seqs) * H + static_cast<size_t>(kMaxPrefixGrid) * kPrefixRows;
-  return kWsBytes + base_bytes(groups) + rows * (dh + kPartExtra) * sizeof(float);
+size_t prefix_attention_workspace_bytes(int seqs, int H, int dh) {
+  const size_t rows = (kCopies + 1) * static_cast<size_t>(seqs) * H + static_cast<size_t>(kMaxPrefixGrid) * kPrefixRows;
+  return rows * (dh + kPartExtra) * sizeof(float);
 }
 
 cudaError_t launch_prefix_attention(PrefixArgs a, cudaStream_t stream, unsigned int* launches) {
-  uint8_t* ws = static_cast<uint8_t*>(a.ws) + kWsBytes;
-  a.base = reinterpret_cast<unsigned long long*>(ws);
-  a.parts = reinterpret_cast<float*>(ws + base_bytes(a.groups));
+  const size_t rows = static_cast<size_t>(a.kv.seqs) * a.H;
+  a.own = static_cast<float*>(a.ws);
+  a.parts = a.own + rows * (a.kv.dh + kPartExtra);
   a.grid = std::min(num_sms(), kMaxPrefixGrid);
   if (a.kv.bf16) return a.kv.dh == 64 ? launch_prefix<true, 64>(a, stream, launches) : launch_prefix<true, 128>(a, stream, launches);
   return a.kv.dh == 64 ? launch_prefix<false, 64>(a, stream, launches) : launch_prefix<false, 128>(a, stream, launches);

@@ -22,7 +22,7 @@ namespace {
 __device__ unsigned int g_rope_quant_err;
 
 constexpr int kThreads = 256;
-constexpr int kItems = 4;  // per thread, at most
+constexpr int kItems = 8;  // per thread, at most
 
 // Pairs (x, y) of four dimensions each turned by angles c, s, each operation rounded.
 __device__ __forceinline__ float2 turned(float x, float y, float c, float s) {
@@ -30,7 +30,7 @@ __device__ __forceinline__ float2 turned(float x, float y, float c, float s) {
 }
 
 template <bool kBf16, bool kInter, int kBits>
-__global__ void __launch_bounds__(kThreads) rope_append_quant_kernel(const RopeQuantArgs a, const int tx_log2) {
+__global__ void __launch_bounds__(kThreads, 5) rope_append_quant_kernel(const RopeQuantArgs a, const int tx_log2) {
   const PagedCodes& c = a.kv;
   const int tx = 1 << tx_log2;  // threads per token
   const long long t = static_cast<long long>(blockIdx.x) * (kThreads >> tx_log2) + (threadIdx.x >> tx_log2);
