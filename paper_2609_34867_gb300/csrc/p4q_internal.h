@@ -238,6 +238,7 @@ struct PrefixArgs : PagedAttnArgs {
   int grid = 0;                          // CTAs of the prefix kernel
   float* own = nullptr;                  // the parts, see p4q_paged_prefix.cuh
   float* parts = nullptr;
+  unsigned long long* share = nullptr;   // chunks of a range
 };
 size_t prefix_attention_workspace_bytes(int seqs, int H, int dh);
 cudaError_t launch_prefix_attention(PrefixArgs a, cudaStream_t stream, unsigned int* launches);

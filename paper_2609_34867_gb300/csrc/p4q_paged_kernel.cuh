@@ -523,7 +523,11 @@ template <class C, int kNt>
 cudaError_t launch_clusters(const typename C::Args& a, int units, int cs, cudaStream_t stream, unsigned int* launches) {
   cudaError_t e = allow_clusters<C, kNt>();
   if (e != cudaSuccess) return e;
-  const ClusterLaunch l(units, cs, cluster_smem<C, kNt>(cs), stream);
+  ClusterLaunch l(units, cs, cluster_smem<C, kNt>(cs), stream);
+  if (C::kOwnOnly && cs == 1) {  // (a CTA by itself finds a place sooner: 16 sequences of up to 96 x 40 heads 22.8 -> 21.8)
+    l.attr[0] = l.attr[1];
+    l.cfg.numAttrs = 1;
+  }
   e = cudaLaunchKernelEx(&l.cfg, paged_attention_kernel<C, kNt, true>, a);
   if (e == cudaSuccess) ++*launches;
   return e;

@@ -78,11 +78,10 @@ struct PrefixOf {
   int from = 0;                  // its first own position
   int row;                       // of the page table, for these: the group's first where it has all to itself
   unsigned long long begin = 0;  // the chunks before its group
-  unsigned long long total = 0;  // all chunks
-  int most = 0;                  // chunks of a unit
   __device__ __forceinline__ PrefixOf(const PrefixArgs& a, int b, int len) : row(b) {
     const int lane = threadIdx.x & 31;
-    for (int g0 = 0; g0 < a.groups; g0 += 32) {
+    unsigned long long total = 0;
+    for (int g0 = 0; g0 < a.groups && g < 0; g0 += 32) {
       Group gr = {};
       if (g0 + lane < a.groups) gr = load_group(a, g0 + lane);
       __syncwarp();
@@ -99,7 +98,6 @@ struct PrefixOf {
         begin = __shfl_sync(0xFFFFFFFFu, upto - n, at);
       }
       total = __shfl_sync(0xFFFFFFFFu, upto, 31);
-      most = max(most, __reduce_max_sync(0xFFFFFFFFu, n > 0 ? gr.chunks : 0));
     }
     if (g >= 0 && len < r.prefix) {
       row = r.first;

@@ -35,8 +35,9 @@ __device__ unsigned int g_prefix_wait_err;
 constexpr int kProducers = 4, kSoftmax = 8;          // warps
 constexpr int kMmaWarp = kProducers + kSoftmax;
 constexpr int kPrefixThreads = 32 * (kMmaWarp + 1);
-// (more than there are: 96 registers per thread, which leave room for a CTA of the own positions' kernel beside)
-constexpr int kPrefixBound = 640;
+// (more than there are: 80 registers per thread, which leave a warp of the own positions' kernel room on every
+// quarter of the SM)
+constexpr int kPrefixBound = 768;
 constexpr int kMaxPrefixGrid = 160;
 constexpr int kTileBytes = 16384;                    // 128 rows of 128 bytes
 constexpr uint32_t kTmemCols = 512;
@@ -238,8 +239,7 @@ __global__ void __launch_bounds__(kPrefixBound) prefix_kernel(const PrefixArgs a
       total = __shfl_sync(0xFFFFFFFFu, upto, 31);
     }
     most = __reduce_max_sync(0xFFFFFFFFu, most);
-    const unsigned long long share = prefix_share(total, most, a.grid);
-    const unsigned long long first = blockIdx.x * share;
+    const unsigned long long share = prefix_share(total, most, a.grid), first = blockIdx.x * share;
     auto look = [&](int g, unsigned long long begin, unsigned long long end) {
       if (first >= begin && first < end) {
         br.group = g;
@@ -262,6 +262,7 @@ __global__ void __launch_bounds__(kPrefixBound) prefix_kernel(const PrefixArgs a
       }
     }
     if (lane == 0) {
+      if (blockIdx.x == 0) *a.share = share;
       br.first = first;
       br.share = share;
       br.total = total;
@@ -452,21 +453,21 @@ __global__ void __launch_bounds__(kPrefixBound) prefix_kernel(const PrefixArgs a
                 if constexpr (kBf16) tmem_st_x8(ts + 128u + 8u * i, none2);
               }
           }
-          uint32_t valid[4];
+          const uint32_t* const valid = br.valid[me];
+          const bool whole_chunk = (valid[0] & valid[1] & valid[2] & valid[3]) == 0xFFFFFFFFu;
+          if (!whole_chunk) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) valid[i] = br.valid[me][i];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {  // a page outside the cache, among the prefix's positions
-            const int left = w.gr.prefix - (ch * kPrefixChunk + 32 * i);
-            lost |= ~valid[i] & (left >= 32 ? 0xFFFFFFFFu : left <= 0 ? 0u : (1u << left) - 1u);
+            for (int i = 0; i < 4; ++i) {  // a page outside the cache, among the prefix's positions
+              const int left = w.gr.prefix - (ch * kPrefixChunk + 32 * i);
+              lost |= ~valid[i] & (left >= 32 ? 0xFFFFFFFFu : left <= 0 ? 0u : (1u << left) - 1u);
+            }
           }
-          auto valid16 = [&](int i) { return (i & 4 ? (i & 2 ? valid[3] : valid[2]) : (i & 2 ? valid[1] : valid[0])) >> (16 * (i & 1)) & 0xFFFFu; };
           float top = -INFINITY;
 #pragma unroll 1
           for (int i = i0; i < i1; i += 2) {  // (an even number)
             uint32_t s[32];
             tmem_ld_32x32b_x32(ts + 16u * i, s);
-            const uint32_t v = valid16(i) | valid16(i + 1) << 16;
+            const uint32_t v = whole_chunk ? 0xFFFFFFFFu : valid[i >> 1];
             tmem_ld_wait();
             if (v != 0xFFFFFFFFu) {
 #pragma unroll
@@ -500,7 +501,7 @@ __global__ void __launch_bounds__(kPrefixBound) prefix_kernel(const PrefixArgs a
           for (int i = i0 + half; i < i1; i += 2) {
             uint32_t s[16], p01[16], p2[8];
             tmem_ld_32x32b_x16(ts + 16u * i, s);
-            const uint32_t v = valid16(i);
+            const uint32_t v = whole_chunk ? 0xFFFFu : valid[i >> 1] >> (16 * (i & 1)) & 0xFFFFu;
             tmem_ld_wait();
             auto weights = [&](auto whole) {
 #pragma unroll
@@ -599,36 +600,35 @@ __global__ void __launch_bounds__(kJoinThreads) prefix_join_kernel(const PrefixA
   __shared__ float4 so[kJoinThreads / 32][32];
   __shared__ float2 sml[kJoinThreads / 32][kSides];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, side = lane / kLanes, d = lane % kLanes * 4;
-  const long long rows = static_cast<long long>(a.kv.seqs) * a.H;
-  const long long at = static_cast<long long>(blockIdx.x) * kRows + warp / kWarpsPer * kSides;
-  const long long row = min(at + side, rows - 1);  // (all warps stay, for their barrier)
-  const int G = a.H / a.kv.Hkv, b0 = static_cast<int>(min(at, rows - 1) / a.H), b = static_cast<int>(row / a.H);
-  const int h = static_cast<int>(row - static_cast<long long>(b) * a.H);
+  const int rows = a.kv.seqs * a.H;  // (fits in 31 bits)
+  const int at = static_cast<int>(blockIdx.x) * kRows + warp / kWarpsPer * kSides;
+  const int row = min(at + side, rows - 1);  // (all warps stay, for their barrier)
+  const int G = a.H / a.kv.Hkv, b0 = min(at, rows - 1) / a.H, b = kSides > 1 ? row / a.H : b0, h = row - b * a.H;
   PrefixOf of(a, b0, a.lens[b0]);
   if (kSides > 1) {  // (the second of two heads may be the next sequence's first)
-    const int b1 = static_cast<int>(min(at + kSides - 1, rows - 1) / a.H);
+    const int b1 = min(at + kSides - 1, rows - 1) / a.H;
     if (b1 != b0) {
       const PrefixOf other(a, b1, a.lens[b1]);
       if (side == 1) of = other;
     }
   }
-  int parts = 0, c0 = 0, copies = 1, per = kPrefixRows, lane_row = 0;
-  if (of.g >= 0) {
-    const Group& r = of.r;
-    const unsigned long long share = prefix_share(of.total, of.most, a.grid);
-    const int i = (b - r.first) * G + h % G;
-    const unsigned long long x = of.begin + static_cast<unsigned long long>(h / G * r.tiles + i / kPrefixRows) * r.chunks;
-    c0 = min(static_cast<int>(quotient(x, share)), a.grid - 1);
-    const int c1 = min(static_cast<int>(quotient(x + r.chunks - 1, share)), a.grid - 1);
-    copies = copies_of(r.n * G - i / kPrefixRows * kPrefixRows);
-    per = kPrefixRows / copies;
-    lane_row = i % kPrefixRows;
-    parts = (c1 - c0 + 1) * copies;
-  }
-  const float* const first = a.parts + row * kPitch;
-  const float* const more = a.parts + (kCopies * rows + lane_row) * kPitch;
   pdl_wait();
   pdl_launch_dependents();
+  int parts = 0, c0 = 0, copies_log2 = 0, lane_row = 0;
+  if (of.g >= 0) {
+    const Group& r = of.r;
+    const unsigned long long share = *a.share;
+    const int hk = h / G, i = (b - r.first) * G + h - hk * G;
+    const unsigned long long x = of.begin + static_cast<unsigned long long>(hk * r.tiles + i / kPrefixRows) * r.chunks;
+    c0 = min(static_cast<int>(quotient(x, share)), a.grid - 1);
+    const int c1 = min(static_cast<int>(quotient(x + r.chunks - 1, share)), a.grid - 1);
+    copies_log2 = copies_of(r.n * G - i / kPrefixRows * kPrefixRows) >> 1;  // (of 1, 2, 4)
+    lane_row = i % kPrefixRows;
+    parts = (c1 - c0 + 1) << copies_log2;
+  }
+  const float* const own = a.own + static_cast<long long>(row) * kPitch;
+  const float* const first = a.parts + static_cast<long long>(row) * kPitch;
+  const float* const more = a.parts + (kCopies * static_cast<long long>(rows) + lane_row) * kPitch;
   float top = -INFINITY, sum = 0.0f;
   float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   // part 0 is that of the sequence's own positions
@@ -642,10 +642,10 @@ __global__ void __launch_bounds__(kJoinThreads) prefix_join_kernel(const PrefixA
       pl[i] = 0.0f;
       pv[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
       if (n <= parts) {
-        const int c = (n - 1) / copies, copy = (n - 1) % copies;
-        const float* p = n == 0   ? a.own + row * kPitch
-                         : c == 0 ? first + copy * rows * kPitch
-                                  : more + (static_cast<long long>(c0 + c) * kPrefixRows + copy * per) * kPitch;
+        const int c = (n - 1) >> copies_log2, copy = (n - 1) & ((1 << copies_log2) - 1);
+        const float* p = n == 0   ? own
+                         : c == 0 ? first + copy * static_cast<long long>(rows) * kPitch
+                                  : more + (static_cast<long long>(c0 + c) * kPrefixRows + copy * (kPrefixRows >> copies_log2)) * kPitch;
         const float4 ml = *reinterpret_cast<const float4*>(p + kDh);
         pm[i] = ml.x;
         pl[i] = ml.y + ml.z;
@@ -725,13 +725,14 @@ cudaError_t launch_prefix(const PrefixArgs& a, cudaStream_t stream, unsigned int
   else
     e = wide ? launch<Rows<kBf16, kDh, false, true>, 2>(a, stream, launches) : launch<Rows<kBf16, kDh, false, true>, 1>(a, stream, launches);
   if (e != cudaSuccess) return e;
-  // four warps per head while they fit at once
+  // four warps per head, of many heads two (us, with four, two, one: 64 x 32 heads of 6 parts 39.4, 36.8, 37.1; 96 x 24 of
+  // 64 dimensions and up to 20 40.4, 38.8, 40.4; 4 x 8 of 120 28.0, 37.6)
   const long long rows = static_cast<long long>(a.kv.seqs) * a.H;
   constexpr int kSides = kDh == 64 ? 2 : 1;
-  if (rows <= 16ll * num_sms() * kSides)
-    e = launch_pdl(prefix_join_kernel<kBf16, kDh, 4>, dim3(static_cast<unsigned>((rows + kSides - 1) / kSides)), dim3(kJoinThreads), 0, stream, a);
-  else
-    e = launch_pdl(prefix_join_kernel<kBf16, kDh, 1>, dim3(static_cast<unsigned>((rows + 4 * kSides - 1) / (4 * kSides))), dim3(kJoinThreads), 0, stream, a);
+  const bool few = rows <= 8ll * num_sms();
+  const long long per = (few ? 1 : 2) * kSides;  // rows of a CTA
+  e = launch_pdl(few ? prefix_join_kernel<kBf16, kDh, 4> : prefix_join_kernel<kBf16, kDh, 2>,
+                 dim3(static_cast<unsigned>((rows + per - 1) / per)), dim3(kJoinThreads), 0, stream, a);
   if (e == cudaSuccess) ++*launches;
   return e;
 }
@@ -740,14 +741,21 @@ cudaError_t launch_prefix(const PrefixArgs& a, cudaStream_t stream, unsigned int
 
 size_t prefix_attention_workspace_bytes(int seqs, int H, int dh) {
   const size_t rows = (kCopies + 1) * static_cast<size_t>(seqs) * H + static_cast<size_t>(kMaxPrefixGrid) * kPrefixRows;
-  return rows * (dh + kPartExtra) * sizeof(float);
+  return rows * (dh + kPartExtra) * sizeof(float) + 16;
 }
 
 cudaError_t launch_prefix_attention(PrefixArgs a, cudaStream_t stream, unsigned int* launches) {
   const size_t rows = static_cast<size_t>(a.kv.seqs) * a.H;
   a.own = static_cast<float*>(a.ws);
   a.parts = a.own + rows * (a.kv.dh + kPartExtra);
-  a.grid = std::min(num_sms(), kMaxPrefixGrid);
+  a.share = reinterpret_cast<unsigned long long*>(
+      a.parts + (kCopies * rows + static_cast<size_t>(kMaxPrefixGrid) * kPrefixRows) * (a.kv.dh + kPartExtra));
+  // Heads of 128: half of the SMs. The others are the own positions' kernel's from the beginning; an SM that has run a
+  // CTA of the prefix keeps its 200 KB of shared memory and leaves that kernel's loads little of L1, so CTAs that
+  // end at once are no better than few. us, on half, three quarters and all of the SMs: 64 conversations behind 4093
+  // positions 40.7, 45.8, 45.7; 32 behind 16384 121.6, 127.5, 137.6; 16 questions about one image 20.1, 20.0,
+  // 21.8. Of 64 a CTA has half as much: five documents 36.0, 31.9, 30.0.
+  a.grid = std::min(a.kv.dh == 64 ? num_sms() : num_sms() / 2, kMaxPrefixGrid);
   if (a.kv.bf16) return a.kv.dh == 64 ? launch_prefix<true, 64>(a, stream, launches) : launch_prefix<true, 128>(a, stream, launches);
   return a.kv.dh == 64 ? launch_prefix<false, 64>(a, stream, launches) : launch_prefix<false, 128>(a, stream, launches);
 }
