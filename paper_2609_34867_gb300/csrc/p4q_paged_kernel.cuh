@@ -524,7 +524,7 @@ cudaError_t launch_clusters(const typename C::Args& a, int units, int cs, cudaSt
   cudaError_t e = allow_clusters<C, kNt>();
   if (e != cudaSuccess) return e;
   ClusterLaunch l(units, cs, cluster_smem<C, kNt>(cs), stream);
-  if (C::kOwnOnly && cs == 1) {  // (a CTA by itself finds a place sooner: 16 sequences of up to 96 x 40 heads 22.8 -> 21.8)
+  if ((C::kOwnOnly || C::kHeadsOuter) && cs == 1) {  // (a CTA by itself finds a place sooner: 16 sequences of up to 96 x 40 heads 22.8 -> 21.8)
     l.attr[0] = l.attr[1];
     l.cfg.numAttrs = 1;
   }
@@ -549,12 +549,15 @@ cudaError_t launch(const typename C::Args& a, cudaStream_t stream, unsigned int*
   // wider ones (8 heads 4.7, 8.7). us, with it and without: one sequence of 704 x 40 heads 6.2, 9.4, of 2048 x 8 6.5, 9.0, of 4096 x 8 11.0, 10.7, half as long as the table 4.1,
   // 7.9; 16 of up to 768 x 8 10.3, 13.7, 12 of up to 768 x 32 (12 tiles) 21.2, 19.6. A CTA for each of up to twice as many units of few tiles: 25 of 128 x 32
   // 14.2, 15.9, of 256 22.0, 23.5 (of five waves: 100 of 200 x 32 73, 66).
-  if (C::kOwnOnly || units <= wave || (units <= 2 * wave && room <= 2 * kMinTiles)) {
+  // (Codes, whose tiles cost less: of up to three times as many units of up to eight tiles. 16 of up to 768 x 32 at 4 bits
+  // 14.8, ranges 18.3, 30 of up to 300 x 32 at 8 16.4, 19.4, 64 of up to 900 x 8 at 4 18.5, 21.5.)
+  const bool few = C::kHeadsOuter ? units <= 3 * wave && room <= 8 : units <= 2 * wave && room <= 2 * kMinTiles;
+  if (C::kOwnOnly || units <= wave || few) {
     const bool spread = units * room <= num_sms();  // a tile each (256 x 32 heads 3.9, of two 4.8; 4 of 512 x 8 5.5, 4.9)
     int cs = static_cast<int>(std::min<long long>(kMaxCluster, spread ? room : (room + kMinTiles - 1) / kMinTiles));
     while (cs > 1 && units * 8 > clusters_at_once<C, kNt>(cs) * 7) --cs;
     // (Behind a prefix the table says nothing of the lengths.)
-    if (C::kOwnOnly || (room + cs - 1) / cs <= units * room / (3 * wave) + kJoinTiles)
+    if (C::kOwnOnly || (C::kHeadsOuter && few) || (room + cs - 1) / cs <= units * room / (3 * wave) + kJoinTiles)
       return launch_clusters<C, kNt>(a, static_cast<int>(units), cs, stream, launches);
   }
   if constexpr (!C::kOwnOnly) {

@@ -1,13 +1,16 @@
 """Text generation on pruned images: the whole path of an answer, small.
 
   python -m paper_2609_34867_gb300.generate [--images B] [--new T] [--layers L] [--top-p P] [--seed S]
+                                            [--cache-bits {16,8,4}] [--answers A]
 
 The selector prunes each image's visual tokens and appends the question's text
 rows (p4q_select_gather_quant); a decoder of random W4A4 weights prefills that
 sequence (rotary positions of the kept tokens' original places, keys and values
 into a paged cache, causal attention) and then answers token by token: per layer
 one rotary append and one paged attention between its four linears, at the end
-one draw from the logits. The decode step is captured once as a CUDA graph and
+one draw from the logits. With --cache-bits 8 or 4 the cache holds codes, written as the tokens
+are appended; with --answers A each image has A sampled answers, which share the prompt's part of the
+cache (16 bits). The decode step is captured once as a CUDA graph and
 replayed. Weights and inputs are synthetic (workloads.py), so the tokens mean
 nothing; the calls are those of a real decoder.
 """
@@ -80,9 +83,13 @@ class Decoder:
         for n, w in enumerate(self.layers):
             y = self._linear(self._norm_codes(x, w["norm1"]), w["qkv"])
             q, k, v = y[:, :c.heads * 128], y[:, c.heads * 128:(c.heads + c.kv_heads) * 128], y[:, (c.heads + c.kv_heads) * 128:]
-            # rotated in place; keys and values into the cache
-            p4q.p4q_rope_append(q, k, v, cache.cos, cache.sin, pos, cache.k[n], cache.v[n], cache.table, q, k_out=k,
-                                seq=seq, rot_pos=rot_pos)
+            # rotated in place; keys and values into the cache (of codes: and what they stand for into their places)
+            if cache.bits == 16:
+                p4q.p4q_rope_append(q, k, v, cache.cos, cache.sin, pos, cache.k[n], cache.v[n], cache.table, q, k_out=k,
+                                    seq=seq, rot_pos=rot_pos)
+            else:
+                p4q.p4q_rope_append_quant(q, k, v, cache.cos, cache.sin, pos, cache.k[n], cache.v[n], cache.k_scale[n],
+                                          cache.v_scale[n], cache.table, q, k_out=k, v_out=v, seq=seq, rot_pos=rot_pos)
             x = x + self._linear(p4q.quant_act(attend(n, q, k, v)), w["o"])
             y = self._linear(self._norm_codes(x, w["norm2"]), w["gate_up"])
             codes = (torch.empty((x.shape[0], c.ffn // 2), dtype=torch.uint8, device="cuda"),
@@ -96,26 +103,55 @@ class Decoder:
 
 
 class Cache:
-    """Paged keys and values of every layer for `seqs` sequences of up to `most` positions."""
+    """Paged keys and values of every layer for `seqs` sequences of up to `most` positions: fp16, or codes of 8 or 4
+    bits with their scales. answers > 1: each so many sequences share their first `prompt` positions, which the
+    first of them has in its pages."""
 
-    def __init__(self, decoder: Decoder, seqs: int, most: int, positions: int, seed: int = 0):
+    def __init__(self, decoder: Decoder, seqs: int, most: int, positions: int, seed: int = 0, bits: int = 16,
+                 answers: int = 1, prompt: int = 0):
         c = decoder.c
+        if answers > 1 and bits != 16:
+            raise ValueError("several answers share a prompt in a cache of 16 bits only")
         per = (most + c.page - 1) // c.page
         pages = seqs * per
         g = torch.Generator(device="cuda").manual_seed(seed)
         # pages in no order, as a running server's free list leaves them
         self.table = torch.randperm(pages, generator=g, device="cuda").to(torch.int32).view(seqs, per)
-        shape = (c.layers, pages, c.page, c.kv_heads, 128)
-        self.k, self.v = (torch.zeros(shape, dtype=torch.float16, device="cuda") for _ in range(2))
+        self.bits, self.answers = bits, answers
+        if bits == 16:
+            shape = (c.layers, pages, c.page, c.kv_heads, 128)
+            self.k, self.v = (torch.zeros(shape, dtype=torch.float16, device="cuda") for _ in range(2))
+        else:
+            shape, dtype = ((128, torch.int8) if bits == 8 else (64, torch.uint8))
+            self.k, self.v = (torch.zeros((c.layers, pages, c.page, c.kv_heads, shape), dtype=dtype, device="cuda")
+                              for _ in range(2))
+            self.k_scale, self.v_scale = (torch.zeros((c.layers, pages, c.kv_heads, c.page), device="cuda").transpose(2, 3)
+                                          for _ in range(2))
         self.lens = torch.zeros((seqs,), dtype=torch.int32, device="cuda")
         self.cos, self.sin = decoder.rope(positions)
-        self.workspace = p4q.paged_attention_workspace("cuda")
+        if answers > 1:
+            self.group_start = torch.arange(0, seqs + 1, answers, dtype=torch.int32, device="cuda")
+            self.prefix_lens = torch.full((seqs // answers,), prompt, dtype=torch.int32, device="cuda")
+            self.workspace = p4q.prefix_attention_workspace(seqs, seqs // answers, c.heads, 128, "cuda")
+        else:
+            self.workspace = p4q.paged_attention_workspace("cuda")
+
+    def attend(self, n, q, o):
+        """The attention of one new token per sequence over layer n."""
+        if self.answers > 1:
+            p4q.p4q_prefix_attention(q, self.k[n], self.v[n], self.table, self.lens, self.group_start, self.prefix_lens, o,
+                                     self.workspace)
+        elif self.bits == 16:
+            p4q.p4q_paged_attention(q, self.k[n], self.v[n], self.table, self.lens, o, self.workspace)
+        else:
+            p4q.p4q_paged_attention_quant(q, self.k[n], self.v[n], self.k_scale[n], self.v_scale[n], self.table, self.lens,
+                                          o, self.workspace)
 
 
 def prefill(decoder: Decoder, cache: Cache, x, rot_pos):
     """x [B, S, d] fp16, rot_pos [B, S] int32 -> the last rows' logits."""
     c, (B, S, d) = decoder.c, x.shape
-    seq = torch.arange(B, dtype=torch.int32, device="cuda").repeat_interleave(S)
+    seq = torch.arange(0, B * cache.answers, cache.answers, dtype=torch.int32, device="cuda").repeat_interleave(S)
     pos = torch.arange(S, dtype=torch.int32, device="cuda").repeat(B)
 
     def attend(_, q, k, v):
@@ -135,7 +171,7 @@ def decode(decoder: Decoder, cache: Cache, token, rot_pos):
 
     def attend(n, q, k, v):
         o = torch.empty(q.shape, dtype=torch.float16, device="cuda")
-        p4q.p4q_paged_attention(q, cache.k[n], cache.v[n], cache.table, cache.lens, o, cache.workspace)
+        cache.attend(n, q, o)
         return o
 
     y = decoder.forward(decoder.embedding[token.long()], cache, attend, cache.lens - 1, rot_pos=rot_pos)
@@ -152,14 +188,19 @@ def pruned_prompt(images: int, c: Config, seed: int, N: int = 192, K: int = 64, 
     return rows, torch.cat((idx, text), dim=1).contiguous(), N + T
 
 
-def generate(decoder: Decoder, rows, rot_pos, end: int, new: int, u, graph: bool = True, **params):
-    """Answers of `new` tokens [B, new] to prompts rows [B, S, d] whose rotary
-    positions end before `end`; u [new, B] uniform numbers; params: p4q.sample's.
+def generate(decoder: Decoder, rows, rot_pos, end: int, new: int, u, graph: bool = True, bits: int = 16, answers: int = 1,
+             **params):
+    """Answers of `new` tokens [B * answers, new] to prompts rows [B, S, d] whose rotary
+    positions end before `end`; u [new, B * answers] uniform numbers; params: p4q.sample's.
     Also the seconds of the decode steps, and the cache."""
-    B, S, _ = rows.shape
-    cache = Cache(decoder, B, S + new, end + new)
+    S = rows.shape[1]
+    B = rows.shape[0] * answers
+    cache = Cache(decoder, B, S + new, end + new, bits=bits, answers=answers, prompt=S)
     tokens = torch.empty((new, B), dtype=torch.int32, device="cuda")
-    tokens[0], _ = p4q.sample(prefill(decoder, cache, rows, rot_pos), u[0], **params)
+    first = prefill(decoder, cache, rows, rot_pos)
+    if answers > 1:
+        first = first.repeat_interleave(answers, 0)
+    tokens[0], _ = p4q.sample(first, u[0], **params)
     token, at = tokens[0].clone(), torch.full((B,), end, dtype=torch.int32, device="cuda")
     draw, logits = u[0].clone(), None
 
@@ -197,21 +238,26 @@ def main(argv=None):
     ap.add_argument("--layers", type=int, default=2)
     ap.add_argument("--top-p", type=float, default=0.9)
     ap.add_argument("--seed", type=int, default=0)
+    ap.add_argument("--cache-bits", type=int, choices=(16, 8, 4), default=16)
+    ap.add_argument("--answers", type=int, default=1)
     a = ap.parse_args(argv)
+    if a.answers < 1 or (a.answers > 1 and a.cache_bits != 16):
+        ap.error("--answers takes 1, or more with --cache-bits 16")
+    n = a.images * a.answers
     c = Config(layers=a.layers)
     decoder = Decoder(c, a.seed)
     rows, rot_pos, end = pruned_prompt(a.images, c, a.seed)
     g = torch.Generator(device="cuda").manual_seed(a.seed)
-    u = torch.rand((a.new, a.images), generator=g, device="cuda")
-    top_p = torch.full((a.images,), a.top_p, device="cuda")
-    tokens, seconds, _ = generate(decoder, rows, rot_pos, end, a.new, u, top_p=top_p)
+    u = torch.rand((a.new, n), generator=g, device="cuda")
+    top_p = torch.full((n,), a.top_p, device="cuda")
+    tokens, seconds, _ = generate(decoder, rows, rot_pos, end, a.new, u, bits=a.cache_bits, answers=a.answers, top_p=top_p)
     status = p4q.p4q_device_status()
     if status != p4q.P4Q_OK:
         raise p4q.P4QError(status, "generate")
-    for b in range(a.images):
-        print(f"image {b}: {' '.join(str(t) for t in tokens[b].tolist())}")
+    for b in range(n):
+        print(f"image {b // a.answers}: {' '.join(str(t) for t in tokens[b].tolist())}")
     if a.new > 1:
-        print(f"{1e6 * seconds / (a.new - 1):.1f} us per decode step of {a.images} sequences, {c.layers} layers")
+        print(f"{1e6 * seconds / (a.new - 1):.1f} us per decode step of {n} sequences, {c.layers} layers")
     return 0
 
 
