@@ -615,7 +615,8 @@ typedef struct {
  *   k_out, v_out [T, ldko / ldvo]  dtype, or NULL: fl32(code * scale) rounded to dtype,
  *         the values that attention over the cache will see (for a prompt's own
  *         attention); each may be its input with its input's pitch
- * dtype P4Q_F16 or P4Q_BF16. Other arguments and rules as p4q_rope_append. */
+ * dtype P4Q_F16 or P4Q_BF16. Two tokens for one slot of a call may leave codes of one
+ * with scales of the other: a slot is named once. Other arguments and rules as p4q_rope_append. */
 p4q_status p4q_rope_append_quant(const uint16_t* q, int ldq, const uint16_t* k, int ldk, const uint16_t* v, int ldv,
                                  int T, int H, const float* cos, const float* sin, int max_pos, int rot,
                                  int interleaved, const int32_t* pos, const int32_t* rot_pos, const int32_t* seq,
@@ -627,7 +628,8 @@ p4q_status p4q_rope_append_quant(const uint16_t* q, int ldq, const uint16_t* k, 
  * weights times the values' scales enter the product with the codes in 22 bits.
  * fp32 products, softmax and sums; o rounded once. Scales may have any sign. q enters the
  * products in 16 bits: values below 2^-25 of the largest of their head may lose bits (2^-35 of
- * that one at most). What is not finite in a head's q makes that head NaN, a scale of v that
+ * that one at most). What is not finite in a head's q, or 2^118
+ * and above, may make that head NaN, a scale of v that
  * is not counts as NaN, one of k as in the formula. Other arguments, rules and the workspace
  * (p4q_paged_attention_workspace_bytes()) as p4q_paged_attention. */
 p4q_status p4q_paged_attention_quant(const uint16_t* q, int ldq, int H, const p4q_paged_kvq* kv, int dtype,

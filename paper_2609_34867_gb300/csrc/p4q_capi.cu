@@ -593,7 +593,7 @@ p4q_status p4q_paged_attention_quant(const uint16_t* q, int ldq, int H, const p4
 
 size_t p4q_prefix_attention_workspace_bytes(int seqs, int groups, int H, int dh) {
   if (seqs < 0 || groups < 0 || H < 1 || H > 65535 || dh < 1 || dh > 128) return 0;
-  return prefix_attention_workspace_bytes(seqs, H, dh);
+  return prefix_attention_workspace_bytes(seqs, groups, H, dh);
 }
 
 p4q_status p4q_prefix_attention(const uint16_t* q, int ldq, int H, const p4q_paged_kv* kv, const int32_t* lens,
@@ -610,7 +610,7 @@ p4q_status p4q_prefix_attention(const uint16_t* q, int ldq, int H, const p4q_pag
       !aligned4(prefix_lens) || !aligned4(lse))
     return P4Q_ERR_MISALIGNED;
   if (kv->seqs == 0) return P4Q_OK;
-  if (!ws || ws_bytes < prefix_attention_workspace_bytes(kv->seqs, H, kv->dh)) return P4Q_ERR_WORKSPACE_TOO_SMALL;
+  if (!ws || ws_bytes < prefix_attention_workspace_bytes(kv->seqs, groups, H, kv->dh)) return P4Q_ERR_WORKSPACE_TOO_SMALL;
   if (!aligned16(ws)) return P4Q_ERR_MISALIGNED;
   if ((st = check_device()) != P4Q_OK) return st;
   a.q = q;

@@ -226,6 +226,8 @@ struct PagedAttnArgs {
   void* ws = nullptr;
 };
 size_t paged_attention_workspace_bytes();
+// Clusters that fit at once of a launch like cfg, whose kernel may ask for `smem` bytes; 0 where the GPU does not say.
+int paged_clusters_at_once(DeviceNumber& known, SmemLimit& limit, const void* kernel, size_t smem, const cudaLaunchConfig_t& cfg);
 // Adds the kernels it launches (one, or two where units are shared) to *launches.
 cudaError_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t stream, unsigned int* launches);
 unsigned int paged_read_and_clear_error();
@@ -239,8 +241,9 @@ struct PrefixArgs : PagedAttnArgs {
   float* own = nullptr;                  // the parts, see p4q_paged_prefix.cuh
   float* parts = nullptr;
   unsigned long long* share = nullptr;   // chunks of a range
+  unsigned long long* base = nullptr;    // [groups] chunks before each, of more than 32
 };
-size_t prefix_attention_workspace_bytes(int seqs, int H, int dh);
+size_t prefix_attention_workspace_bytes(int seqs, int groups, int H, int dh);
 cudaError_t launch_prefix_attention(PrefixArgs a, cudaStream_t stream, unsigned int* launches);
 unsigned int prefix_read_and_clear_error();        // waits that ran out
 unsigned int prefix_read_and_clear_index_error();

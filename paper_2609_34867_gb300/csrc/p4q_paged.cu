@@ -37,6 +37,18 @@ cudaError_t launch_for(const PagedAttnArgs& a, cudaStream_t stream, unsigned int
 
 size_t paged_attention_workspace_bytes() { return kWsBytes; }
 
+int paged_clusters_at_once(DeviceNumber& known, SmemLimit& limit, const void* kernel, size_t smem, const cudaLaunchConfig_t& cfg) {
+  int n = 0;
+  const cudaError_t e = known.get(&n, [&](int* number) {
+    const cudaError_t le = limit.allow(kernel, smem);
+    if (le != cudaSuccess) return le;
+    return cudaOccupancyMaxActiveClusters(number, kernel, &cfg);
+  });
+  if (e == cudaSuccess) return n;
+  cudaGetLastError();
+  return 0;
+}
+
 cudaError_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t stream, unsigned int* launches) {
   if (a.kv.bf16) return a.kv.dh == 64 ? launch_for<true, 64>(a, stream, launches) : launch_for<true, 128>(a, stream, launches);
   return a.kv.dh == 64 ? launch_for<false, 64>(a, stream, launches) : launch_for<false, 128>(a, stream, launches);

@@ -51,6 +51,11 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return y;
 }
 
+// For a kernel that reads what the stream's earlier kernels wrote without waiting for the one before it, which writes
+// none of that: the one before has waited for all of them before it let this one begin, so they
+// are complete; what this SM's L1 may still have of their data from before is given up here.
+__device__ __forceinline__ void see_earlier_kernels() { __threadfence(); }
+
 // What a unit is to the part of the kernel that goes through its tiles: heads h0 ..
 // h0 + heads - 1 of sequence b over key/value head hk, positions from .. len - 1
 // (from is 0 but where a prefix is another kernel's), tiles counted from base.

@@ -105,7 +105,10 @@ __global__ void __launch_bounds__(kThreads, C::ctas(kNt)) paged_attention_kernel
   float* partial = reinterpret_cast<float*>(split + kMaxGrid);
 
   if (kCluster) cluster_begun_arrive();
-  if (!C::kOwnOnly) pdl_wait();
+  if (C::kOwnOnly)
+    see_earlier_kernels();
+  else
+    pdl_wait();
   pdl_launch_dependents();
 
   auto length = [&](int b) -> int {
@@ -496,32 +499,25 @@ struct ClusterLaunch {
 
 // The shared memory that a cluster's CTAs ask for, whatever their number.
 template <class C, int kNt>
-cudaError_t allow_clusters() {
+SmemLimit& cluster_limit() {
   static SmemLimit limit;
-  return limit.allow(paged_attention_kernel<C, kNt, true>, cluster_smem<C, kNt>(kMaxCluster));
+  return limit;
 }
 
 // Clusters of cs CTAs that the GPU holds at once; 0 where it does not say.
 template <class C, int kNt>
 int clusters_at_once(int cs) {
   static DeviceNumber known[kMaxCluster + 1];
-  int n = 0;
-  const cudaError_t e = known[cs].get(&n, [cs](int* number) {
-    const cudaError_t le = allow_clusters<C, kNt>();
-    if (le != cudaSuccess) return le;
-    ClusterLaunch l(1, cs, cluster_smem<C, kNt>(cs), nullptr);
-    l.cfg.numAttrs = 1;
-    return cudaOccupancyMaxActiveClusters(number, paged_attention_kernel<C, kNt, true>, &l.cfg);
-  });
-  if (e == cudaSuccess) return n;
-  cudaGetLastError();
-  return 0;
+  ClusterLaunch l(1, cs, cluster_smem<C, kNt>(cs), nullptr);
+  l.cfg.numAttrs = 1;
+  return paged_clusters_at_once(known[cs], cluster_limit<C, kNt>(), reinterpret_cast<const void*>(paged_attention_kernel<C, kNt, true>),
+                                cluster_smem<C, kNt>(kMaxCluster), l.cfg);
 }
 
 // A cluster of cs CTAs for each unit.
 template <class C, int kNt>
 cudaError_t launch_clusters(const typename C::Args& a, int units, int cs, cudaStream_t stream, unsigned int* launches) {
-  cudaError_t e = allow_clusters<C, kNt>();
+  cudaError_t e = cluster_limit<C, kNt>().allow(paged_attention_kernel<C, kNt, true>, cluster_smem<C, kNt>(kMaxCluster));
   if (e != cudaSuccess) return e;
   ClusterLaunch l(units, cs, cluster_smem<C, kNt>(cs), stream);
   if ((C::kOwnOnly || C::kHeadsOuter) && cs == 1) {  // (a CTA by itself finds a place sooner: 16 sequences of up to 96 x 40 heads 22.8 -> 21.8)

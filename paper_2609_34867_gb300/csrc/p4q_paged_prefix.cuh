@@ -77,27 +77,35 @@ struct PrefixOf {
   Group r = {};
   int from = 0;                  // its first own position
   int row;                       // of the page table, for these: the group's first where it has all to itself
-  unsigned long long begin = 0;  // the chunks before its group
+  unsigned long long begin = 0;  // the chunks before its group (of up to 32 groups; else base[g], once the prefix kernel has ended)
   __device__ __forceinline__ PrefixOf(const PrefixArgs& a, int b, int len) : row(b) {
-    const int lane = threadIdx.x & 31;
-    unsigned long long total = 0;
-    for (int g0 = 0; g0 < a.groups && g < 0; g0 += 32) {
+    if (a.groups <= 32) {  // a lane each
+      const int lane = threadIdx.x & 31;
       Group gr = {};
-      if (g0 + lane < a.groups) gr = load_group(a, g0 + lane);
+      if (lane < a.groups) gr = load_group(a, lane);
       __syncwarp();
-      const unsigned long long n = group_chunks(a, gr), upto = total + scan_add(n);
+      const unsigned long long n = group_chunks(a, gr), upto = scan_add(n);
       const uint32_t in = __ballot_sync(0xFFFFFFFFu, gr.first <= b && b < gr.first + gr.n);
-      if (in != 0 && g < 0) {
-        const int at = __ffs(in) - 1;
-        g = g0 + at;
-        r.first = __shfl_sync(0xFFFFFFFFu, gr.first, at);
-        r.n = __shfl_sync(0xFFFFFFFFu, gr.n, at);
-        r.prefix = __shfl_sync(0xFFFFFFFFu, gr.prefix, at);
-        r.tiles = __shfl_sync(0xFFFFFFFFu, gr.tiles, at);
-        r.chunks = __shfl_sync(0xFFFFFFFFu, gr.chunks, at);
-        begin = __shfl_sync(0xFFFFFFFFu, upto - n, at);
+      if (in != 0) {
+        g = __ffs(in) - 1;
+        r.first = __shfl_sync(0xFFFFFFFFu, gr.first, g);
+        r.n = __shfl_sync(0xFFFFFFFFu, gr.n, g);
+        r.prefix = __shfl_sync(0xFFFFFFFFu, gr.prefix, g);
+        r.tiles = __shfl_sync(0xFFFFFFFFu, gr.tiles, g);
+        r.chunks = __shfl_sync(0xFFFFFFFFu, gr.chunks, g);
+        begin = __shfl_sync(0xFFFFFFFFu, upto - n, g);
       }
-      total = __shfl_sync(0xFFFFFFFFu, upto, 31);
+    } else {  // the last one that begins at or before it
+      int lo = 0, hi = a.groups;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (a.group_start[mid] <= b)
+          lo = mid;
+        else
+          hi = mid;
+      }
+      r = load_group(a, lo);
+      if (r.first <= b && b < r.first + r.n) g = lo;
     }
     if (g >= 0 && len < r.prefix) {
       row = r.first;

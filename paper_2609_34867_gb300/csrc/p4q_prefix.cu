@@ -234,6 +234,7 @@ __global__ void __launch_bounds__(kPrefixBound) prefix_kernel(const PrefixArgs a
       }
       __syncwarp();
       const unsigned long long upto = total + scan_add(n);
+      if (blockIdx.x == 0 && a.groups > 32 && g < a.groups) a.base[g] = upto - n;
       last_begin = upto - n;
       last_end = upto;
       total = __shfl_sync(0xFFFFFFFFu, upto, 31);
@@ -604,6 +605,7 @@ __global__ void __launch_bounds__(kJoinThreads) prefix_join_kernel(const PrefixA
   const int at = static_cast<int>(blockIdx.x) * kRows + warp / kWarpsPer * kSides;
   const int row = min(at + side, rows - 1);  // (all warps stay, for their barrier)
   const int G = a.H / a.kv.Hkv, b0 = min(at, rows - 1) / a.H, b = kSides > 1 ? row / a.H : b0, h = row - b * a.H;
+  see_earlier_kernels();
   PrefixOf of(a, b0, a.lens[b0]);
   if (kSides > 1) {  // (the second of two heads may be the next sequence's first)
     const int b1 = min(at + kSides - 1, rows - 1) / a.H;
@@ -619,7 +621,7 @@ __global__ void __launch_bounds__(kJoinThreads) prefix_join_kernel(const PrefixA
     const Group& r = of.r;
     const unsigned long long share = *a.share;
     const int hk = h / G, i = (b - r.first) * G + h - hk * G;
-    const unsigned long long x = of.begin + static_cast<unsigned long long>(hk * r.tiles + i / kPrefixRows) * r.chunks;
+    const unsigned long long x = (a.groups > 32 ? a.base[of.g] : of.begin) + static_cast<unsigned long long>(hk * r.tiles + i / kPrefixRows) * r.chunks;
     c0 = min(static_cast<int>(quotient(x, share)), a.grid - 1);
     const int c1 = min(static_cast<int>(quotient(x + r.chunks - 1, share)), a.grid - 1);
     copies_log2 = copies_of(r.n * G - i / kPrefixRows * kPrefixRows) >> 1;  // (of 1, 2, 4)
@@ -739,9 +741,9 @@ cudaError_t launch_prefix(const PrefixArgs& a, cudaStream_t stream, unsigned int
 
 }  // namespace
 
-size_t prefix_attention_workspace_bytes(int seqs, int H, int dh) {
+size_t prefix_attention_workspace_bytes(int seqs, int groups, int H, int dh) {
   const size_t rows = (kCopies + 1) * static_cast<size_t>(seqs) * H + static_cast<size_t>(kMaxPrefixGrid) * kPrefixRows;
-  return rows * (dh + kPartExtra) * sizeof(float) + 16;
+  return rows * (dh + kPartExtra) * sizeof(float) + (2 + static_cast<size_t>(groups)) * sizeof(unsigned long long);
 }
 
 cudaError_t launch_prefix_attention(PrefixArgs a, cudaStream_t stream, unsigned int* launches) {
@@ -750,6 +752,7 @@ cudaError_t launch_prefix_attention(PrefixArgs a, cudaStream_t stream, unsigned 
   a.parts = a.own + rows * (a.kv.dh + kPartExtra);
   a.share = reinterpret_cast<unsigned long long*>(
       a.parts + (kCopies * rows + static_cast<size_t>(kMaxPrefixGrid) * kPrefixRows) * (a.kv.dh + kPartExtra));
+  a.base = a.share + 1;
   // Heads of 128: half of the SMs. The others are the own positions' kernel's from the beginning; an SM that has run a
   // CTA of the prefix keeps its 200 KB of shared memory and leaves that kernel's loads little of L1, so CTAs that
   // end at once are no better than few. us, on half, three quarters and all of the SMs: 64 conversations behind 4093

@@ -55,5 +55,5 @@ def test_workspace_grows_with_every_size(lib):
     size = lib.p4q_prefix_attention_workspace_bytes
     last = size(4, 1, 8, 64)
     assert last > 0
-    assert size(5, 1, 8, 64) > last and size(4, 9, 8, 64) >= last and size(4, 1, 9, 64) > last and size(4, 1, 8, 128) > last
+    assert size(5, 1, 8, 64) > last and size(4, 9, 8, 64) > last and size(4, 1, 9, 64) > last and size(4, 1, 8, 128) > last
     assert size(-1, 1, 8, 64) == 0 and size(4, 1, 0, 64) == 0 and size(4, 1, 8, 256) == 0

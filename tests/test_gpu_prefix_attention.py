@@ -280,3 +280,64 @@ def test_steps_back_to_back_on_one_workspace(p4q, dev):
     torch.cuda.synchronize()
     for o, w in zip(outs, want):
         assert torch.equal(o, w)
+
+
+def test_more_groups_than_a_warp_has_lanes(p4q, dev):
+    c = make(dev, [(30 + 3 * i, [i % 4, 9][:1 + i % 2]) for i in range(100)], 8, 2, 64, 8, "bf16", seed=5, before=[20], behind=[5])
+    check(c, *run(p4q, dev, c))
+    c = make(dev, [(17, [2])] * 33 + [(900, [1, 30])], 4, 4, 128, 16, "fp16", seed=6)
+    check(c, *run(p4q, dev, c))
+
+
+@pytest.mark.parametrize("graph", [False, True])
+def test_what_is_appended_just_before_is_seen(p4q, dev, graph):
+    """Append and attention back to back, nothing in between: each step's rows lie in slots that the
+    attention before has read as masked ones, on the same SMs perhaps."""
+    steps, H, Hkv, dh, page = 24, 8, 4, 128, 32
+    c = make(dev, [(200, [3, 40, 7, 0, 12])] * 3, H, Hkv, dh, page, "fp16", seed=8, cols=9)
+    n = c["lens"].shape[0]
+    free = torch.arange(c["k"].shape[0], c["k"].shape[0] + 2 * n, device=dev, dtype=torch.int32)
+    k, v = (torch.cat((x, torch.zeros((2 * n, *x.shape[1:]), dtype=x.dtype, device=dev))).nan_to_num_(nan=3.0) for x in (c["k"], c["v"]))
+    table = c["table"].clone()
+    at = 0
+    for b in range(n):  # pages for the steps to come
+        for col in range(table.shape[1]):
+            if (b % 5 == 0 or col >= 200 // page) and int(table[b, col]) >= k.shape[0] and at < free.numel() and col * page < int(c["lens"][b]) + steps:
+                table[b, col] = free[at]
+                at += 1
+    g = torch.Generator(device=dev).manual_seed(1)
+    rows = torch.randn((steps, n, (H + 2 * Hkv) * dh), generator=g, device=dev).half()
+    one, zero = torch.ones((400, dh // 2), device=dev), torch.zeros((400, dh // 2), device=dev)
+    lens = [c["lens"] + i + 1 for i in range(steps)]
+    pos = [x - 1 for x in lens]
+    outs = [torch.empty((n, H * dh), dtype=torch.float16, device=dev) for _ in range(steps)]
+    ws = workspace(p4q, dev, c)
+
+    def step(i, o):
+        y = rows[i]
+        q = y[:, :H * dh]
+        p4q.p4q_rope_append(q, y[:, H * dh:(H + Hkv) * dh], y[:, (H + Hkv) * dh:], one, zero, pos[i], k, v, table, q)
+        p4q.p4q_prefix_attention(q, k, v, table, lens[i], c["start"], c["prefix"], o, ws)
+
+    def all_steps():
+        for i in range(steps):
+            step(i, outs[i])
+
+    k0, v0 = k.clone(), v.clone()
+    torch.cuda.synchronize()
+    if graph:
+        cg = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(cg):
+            all_steps()
+        cg.replay()
+    else:
+        all_steps()
+    torch.cuda.synchronize()
+    assert p4q.p4q_device_status() == 0
+    k.copy_(k0)
+    v.copy_(v0)
+    for i in range(steps):  # the same, each step waited for
+        want = torch.empty_like(outs[i])
+        step(i, want)
+        torch.cuda.synchronize()
+        assert torch.equal(outs[i], want), f"step {i}"
