@@ -11,6 +11,9 @@
   python -m paper_2609_34867_gb300.kernel_cases attn B M H [--reps R]
   python -m paper_2609_34867_gb300.kernel_cases append T H HKV [--reps R]
   python -m paper_2609_34867_gb300.kernel_cases attend B L H HKV [--reps R]
+  python -m paper_2609_34867_gb300.kernel_cases appendq T H HKV BITS [--reps R]
+  python -m paper_2609_34867_gb300.kernel_cases attendq B L H HKV BITS [--reps R]
+  python -m paper_2609_34867_gb300.kernel_cases prefix B P OWN H HKV [--reps R]
   python -m paper_2609_34867_gb300.kernel_cases sample B V {plain,top_k,top_p,min_p} [--reps R]
   python -m paper_2609_34867_gb300.kernel_cases mse B M D [--reps R]
   python -m paper_2609_34867_gb300.kernel_cases topk B N K [--reps R]
@@ -50,6 +53,12 @@ selects the first replayed launch.
           pages of 16, bf16 (bytes: 4 T (H + 2 HKV) 128 in and out);
   attend  p4q_paged_attention, B sequences of L positions, H heads over HKV
           of 128, shuffled pages of 16, bf16 (bytes: 4 B L HKV 128 in);
+  appendq p4q_rope_append_quant as append, fp16, codes of BITS bits (bytes: 2 T
+          (2 H + 2 HKV) 128 and the codes with their scales);
+  attendq p4q_paged_attention_quant as attend, fp16, codes of BITS bits (bytes:
+          2 B L HKV (16 BITS + 4) in);
+  prefix  p4q_prefix_attention: B sequences behind one prefix of P positions, OWN
+          positions each, heads of 128, bf16 (bytes: 4 (P + B OWN) HKV 128 in);
   sample  p4q_sample on B x V fp32 logits with one cut (bytes: 4 B V in);
   mse     p4q_block_mse on B samples of M rows x D fp16 (bytes: 4 B M D in);
   topk    p4q_topk_replacement on B x N fp32 score pairs (bytes: 8 B N in);
@@ -197,9 +206,20 @@ def _sweep(kind: str, reps: int, dev):
             del V, Q, A, ws, idx
 
 
+def _codes(g, pages, heads, bits, dev):
+    """Keys (or values) of a cache of codes, pages of 16, heads of 128, and their scales."""
+    if bits == 8:
+        c = torch.randint(-127, 128, (pages, 16, heads, 128), generator=g, device=dev, dtype=torch.int8)
+    else:
+        c = torch.randint(-7, 8, (pages, 16, heads, 128), generator=g, device=dev, dtype=torch.int8)
+        c = ((c[..., 0::2] & 15) | (c[..., 1::2] << 4)).view(torch.uint8)
+    s = (1.5 + 2.0 * torch.rand((pages, heads, 16), generator=g, device=dev)) / (127.0 if bits == 8 else 7.0)
+    return c, s.transpose(1, 2)
+
+
 def main(argv=None):
     ap = argparse.ArgumentParser()
-    ap.add_argument("case", choices=["gemm", "gemm8", "quant", "requant", "requant1", "select", "saliency", "swiglu", "rmsnorm", "attn", "append", "attend",
+    ap.add_argument("case", choices=["gemm", "gemm8", "quant", "requant", "requant1", "select", "saliency", "swiglu", "rmsnorm", "attn", "append", "attend", "appendq", "attendq", "prefix",
                                      "sample",
                                      "mse", "topk", "peak", "sweep", "hostlink"])
     ap.add_argument("args", nargs="+")
@@ -317,6 +337,50 @@ def main(argv=None):
         ms = _timed(lambda: p4q.p4q_paged_attention(q, kc, vc, table, lens, out, ws), a.reps, dev)
         nbytes = 4 * B * L * HK * 128
         print(f"attend {B}x{L} H={H}/{HK}: {ms * 1e3:.1f} us/call, {nbytes / ms / 1e6:.1f} GB/s")
+    elif a.case == "appendq":
+        T, H, HK, bits = (int(x) for x in a.args)
+        g = torch.Generator(device=dev).manual_seed(0)
+        y = torch.randn((T, (H + 2 * HK) * 128), generator=g, device=dev).half()
+        q, k, v = y[:, :H * 128], y[:, H * 128:(H + HK) * 128], y[:, (H + HK) * 128:]
+        kc, ks = _codes(g, (T + 15) // 16, HK, bits, dev)
+        vc, vs = _codes(g, (T + 15) // 16, HK, bits, dev)
+        table = torch.randperm((T + 15) // 16, generator=g, device=dev).to(torch.int32)[None]
+        pos = torch.arange(T, dtype=torch.int32, device=dev)
+        seq = torch.zeros((T,), dtype=torch.int32, device=dev)
+        cos, sin = (torch.rand((T, 64), generator=g, device=dev) for _ in range(2))
+        out = torch.empty((T, H * 128), dtype=torch.float16, device=dev)
+        ms = _timed(lambda: p4q.p4q_rope_append_quant(q, k, v, cos, sin, pos, kc, vc, ks, vs, table, out, seq=seq), a.reps,
+                    dev)
+        nbytes = T * (2 * (2 * H + 2 * HK) * 128 + 2 * HK * (16 * bits + 4))
+        print(f"appendq {T} H={H}/{HK} {bits} bits: {ms * 1e3:.1f} us/call, {nbytes / ms / 1e6:.1f} GB/s")
+    elif a.case == "attendq":
+        B, L, H, HK, bits = (int(x) for x in a.args)
+        g = torch.Generator(device=dev).manual_seed(0)
+        per = (L + 15) // 16
+        kc, ks = _codes(g, B * per, HK, bits, dev)
+        vc, vs = _codes(g, B * per, HK, bits, dev)
+        table = torch.randperm(B * per, generator=g, device=dev).to(torch.int32).view(B, per)
+        lens = torch.full((B,), L, dtype=torch.int32, device=dev)
+        q = torch.randn((B, H * 128), generator=g, device=dev).half()
+        out, ws = torch.empty_like(q), p4q.paged_attention_workspace(dev)
+        ms = _timed(lambda: p4q.p4q_paged_attention_quant(q, kc, vc, ks, vs, table, lens, out, ws), a.reps, dev)
+        nbytes = 2 * B * L * HK * (16 * bits + 4)
+        print(f"attendq {B}x{L} H={H}/{HK} {bits} bits: {ms * 1e3:.1f} us/call, {nbytes / ms / 1e6:.1f} GB/s")
+    elif a.case == "prefix":
+        B, P, own, H, HK = (int(x) for x in a.args)
+        g = torch.Generator(device=dev).manual_seed(0)
+        per = (P + own + 15) // 16
+        kc, vc = (torch.randn((B * per, 16, HK, 128), generator=g, device=dev).bfloat16() for _ in range(2))
+        table = torch.randperm(B * per, generator=g, device=dev).to(torch.int32).view(B, per)
+        table[1:, :P // 16] = table[0, :P // 16]
+        lens = torch.full((B,), P + own, dtype=torch.int32, device=dev)
+        start = torch.tensor([0, B], dtype=torch.int32, device=dev)
+        prefix = torch.tensor([P], dtype=torch.int32, device=dev)
+        q = torch.randn((B, H * 128), generator=g, device=dev).bfloat16()
+        out, ws = torch.empty_like(q), p4q.prefix_attention_workspace(B, 1, H, 128, dev)
+        ms = _timed(lambda: p4q.p4q_prefix_attention(q, kc, vc, table, lens, start, prefix, out, ws), a.reps, dev)
+        nbytes = 4 * (P + B * own) * HK * 128
+        print(f"prefix {B} behind {P}, {own} each, H={H}/{HK}: {ms * 1e3:.1f} us/call, {nbytes / ms / 1e6:.1f} GB/s")
     elif a.case == "sample":
         B, V, cut = int(a.args[0]), int(a.args[1]), a.args[2]
         g = torch.Generator(device=dev).manual_seed(0)
