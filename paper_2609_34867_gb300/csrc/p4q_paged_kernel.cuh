@@ -556,23 +556,24 @@ cudaError_t launch(const typename C::Args& a, cudaStream_t stream, unsigned int*
     if (C::kOwnOnly || (C::kHeadsOuter && few) || (room + cs - 1) / cs <= units * room / (3 * wave) + kJoinTiles)
       return launch_clusters<C, kNt>(a, static_cast<int>(units), cs, stream, launches);
   }
-  if constexpr (!C::kOwnOnly) {
-  static SmemLimit limit;
-  auto* kernel = paged_attention_kernel<C, kNt, false>;
-  cudaError_t e = limit.allow(kernel, smem);
-  if (e != cudaSuccess) return e;
-  int grid = room >= wave || units >= wave ? wave : static_cast<int>(std::min<long long>(wave, units * room));
-  if (C::kHeadsOuter && grid >= 8 * (units / a.kv.seqs)) grid -= grid % static_cast<int>(units / a.kv.seqs);
-  e = launch_pdl(kernel, dim3(static_cast<unsigned>(grid)), dim3(kThreads), smem, stream, a);
-  if (e != cudaSuccess) return e;
-  ++*launches;
-  const unsigned heads = static_cast<unsigned>(C::kSplit > 1 ? C::kSplit * group : std::min(group, 8 * kNt));
-  e = launch_pdl(join_kernel<C, kNt>, dim3(static_cast<unsigned>(grid), heads), dim3(32 * kJoinWarps), 0, stream,
-                 a);
-  if (e == cudaSuccess) ++*launches;
-  return e;
+  if constexpr (C::kOwnOnly) {
+    return cudaErrorInvalidValue;  // (not reached)
+  } else {
+    static SmemLimit limit;
+    auto* kernel = paged_attention_kernel<C, kNt, false>;
+    cudaError_t e = limit.allow(kernel, smem);
+    if (e != cudaSuccess) return e;
+    int grid = room >= wave || units >= wave ? wave : static_cast<int>(std::min<long long>(wave, units * room));
+    if (C::kHeadsOuter && grid >= 8 * (units / a.kv.seqs)) grid -= grid % static_cast<int>(units / a.kv.seqs);
+    e = launch_pdl(kernel, dim3(static_cast<unsigned>(grid)), dim3(kThreads), smem, stream, a);
+    if (e != cudaSuccess) return e;
+    ++*launches;
+    const unsigned heads = static_cast<unsigned>(C::kSplit > 1 ? C::kSplit * group : std::min(group, 8 * kNt));
+    e = launch_pdl(join_kernel<C, kNt>, dim3(static_cast<unsigned>(grid), heads), dim3(32 * kJoinWarps), 0, stream,
+                   a);
+    if (e == cudaSuccess) ++*launches;
+    return e;
   }
-  return cudaErrorInvalidValue;  // (not reached)
 }
 
 unsigned int read_and_clear_paged_error() {

@@ -6,7 +6,10 @@
 // one row, group after group, head after head, tile after tile, are dealt to the CTAs in
 // consecutive ranges of equal length. A range that begins in the middle of a unit leaves its part of
 // that unit's rows with the CTA's number; the range in which a unit begins, with the rows' own
-// (parts: [copies][seqs * H] rows, then [grid][128], each dh values, the reference maximum and the sum, in two numbers).
+// (parts: [copies][seqs * H] rows, then [grid][128], each dh values, the reference maximum and the sum).
+// A unit's rows are few where little is asked of a prefix: then they stand in the tile two or four times and
+// each copy takes its share of every chunk's positions (16 rows behind 661 positions x 40 heads: a chunk
+// takes about 1.2 us instead of 3).
 #pragma once
 
 #include "p4q_paged.cuh"

@@ -1,4 +1,5 @@
-// Attention of one new token per sequence over a paged cache of 8- or 4-bit codes.
+// Attention of one new token per sequence over a paged cache of 8- or 4-bit codes: the instances of the
+// paged attention kernel with p4q_paged_codes.cuh's way through a unit's tiles, and which call takes which.
 #include "p4q_paged_kernel.cuh"
 #include "p4q_paged_codes.cuh"
 

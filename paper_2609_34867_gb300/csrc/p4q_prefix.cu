@@ -1,12 +1,23 @@
 // Attention of one new token per sequence for groups of sequences that share a prefix: the
 // prefix's keys and values are read once per group instead of once per sequence.
 //
-// Two kernels. prefix_kernel takes the prefixes: with n sequences of G query heads per
+//   o = sum_i 2^(ref_i - ref) o_i / sum_i 2^(ref_i - ref) l_i
+// over parts i of a sequence's positions, each with a reference ref_i, the sum l_i of the weights
+// 2^(x_j - ref_i), x_j = scale log2(e) q . k_j, and the values o_i weighted so, all in fp32.
+//
+// Three kernels. prefix_kernel takes the prefixes: with n sequences of G query heads per
 // key/value head there are n G rows of queries to the same keys, enough for the tensor cores'
 // 128-row products (tcgen05 kind::f16, fp32 accumulators in TMEM). The paged attention kernel
-// (p4q_paged_kernel.cuh) takes the positions that each sequence has of its own, adds the
-// prefix's parts at its end and writes the outputs. It needs nothing of the first before
-// that, so it starts beside it, on what the first leaves free of the SMs.
+// (p4q_paged_kernel.cuh) takes the positions that each sequence has of its own and leaves their
+// parts. It needs nothing of the first, so it starts beside it, on what the first leaves free of the
+// SMs. prefix_join_kernel adds the parts up and writes the outputs (inside the paged attention its
+// waits held up the warps of all other units: 16 sequences behind 661 positions, 40 heads, 28.6 us,
+// 21 this way).
+//
+// Bound: HBM where prefixes are long and their rows fill a tile or less (32 sequences behind 16384
+// positions, 32 heads of 128, bf16: 119 us, 0.79 of what their bytes take); with several tiles per key head
+// the softmax's chain, 3 us per chunk of 128 x 128 (64 sequences behind 4093, 32 heads over 8: 37 us of which
+// bytes are 12.7); for short prefixes the chain of plan, queries and keys, chunk, end and join (21 us, bytes 4.5).
 //
 // prefix_kernel: units and ranges as p4q_paged_prefix.cuh says. Thirteen warps:
 //   warps 0-3  queries, keys and values into shared memory with 16-byte asynchronous copies (pages
@@ -35,8 +46,8 @@ __device__ unsigned int g_prefix_wait_err;
 constexpr int kProducers = 4, kSoftmax = 8;          // warps
 constexpr int kMmaWarp = kProducers + kSoftmax;
 constexpr int kPrefixThreads = 32 * (kMmaWarp + 1);
-// (more than there are: 80 registers per thread, which leave a warp of the own positions' kernel room on every
-// quarter of the SM)
+// (more threads than there are: 80 registers for each, which leave a warp of the own positions' kernel room on
+// every quarter of the SM)
 constexpr int kPrefixBound = 768;
 constexpr int kMaxPrefixGrid = 160;
 constexpr int kTileBytes = 16384;                    // 128 rows of 128 bytes
@@ -52,6 +63,7 @@ struct Bars {
   int group;
   Group its;                                     // (that group)
   uint32_t valid[kMetas][kProducers];
+  float sums[kPrefixRows];                       // of the second softmax warps' weights
   uint32_t tmem_slot;
   int abort_flag;
 };
@@ -475,18 +487,18 @@ __global__ void __launch_bounds__(kPrefixBound) prefix_kernel(const PrefixArgs a
               for (int e = 0; e < 32; ++e)
                 if (!(v >> e & 1u)) s[e] = 0x7FFFFFFFu;  // (NaN: no maximum)
             }
+            if (!(c2 > 0.0f)) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e) s[e] = __float_as_uint(__uint_as_float(s[e]) * c2);
+            }
             float m4[4] = {top, top, top, top};
 #pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-              const float2 x = __fmul2_rn(make_float2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), c22);
-              const float2 y = __fmul2_rn(make_float2(__uint_as_float(s[e + 2]), __uint_as_float(s[e + 3])), c22);
-              m4[e >> 2 & 3] = max3(m4[e >> 2 & 3], x.x, x.y);
-              m4[(e >> 2) + 2 & 3] = max3(m4[(e >> 2) + 2 & 3], y.x, y.y);
-            }
+            for (int e = 0; e < 32; e += 2) m4[e >> 1 & 3] = max3(m4[e >> 1 & 3], __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
             top = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
           }
           // both warps have read all of their rows' scores: either overwrites only its own pieces with weights,
           // but the other one's maxima are of all
+          if (c2 > 0.0f) top *= c2;  // (rounding keeps the order: the largest product)
           named_bar_sync(1 + quad, 64);
           float alpha = 1.0f;
           if (top > ref + kMove<kBf16>) {  // (-inf: the first score)
@@ -558,11 +570,11 @@ __global__ void __launch_bounds__(kPrefixBound) prefix_kernel(const PrefixArgs a
       const int jl = j - 1;
       ok = ok && mbar_wait_all(&br.pv_done[jl & 1], (jl >> 1) & 1, abort_flag, &g_prefix_wait_err);
       tc_fence_after();
+      const int h = w.hk * G + min(idx, rows - 1) % G;
+      const long long all = static_cast<long long>(c.seqs) * a.H;
+      float* const part = a.parts + pitch * (w.c0 == 0 ? copy * all + static_cast<long long>(b) * a.H + h
+                                                       : kCopies * all + static_cast<long long>(blockIdx.x) * kPrefixRows + r);
       if (used && ok) {
-        const int h = w.hk * G + min(idx, rows - 1) % G;
-        const long long all = static_cast<long long>(c.seqs) * a.H;
-        float* part = a.parts + pitch * (w.c0 == 0 ? copy * all + static_cast<long long>(b) * a.H + h
-                                                   : kCopies * all + static_cast<long long>(blockIdx.x) * kPrefixRows + r);
 #pragma unroll 1
         for (int i = 0; i < kDh / 64; ++i) {
           uint32_t o[32];
@@ -575,11 +587,14 @@ __global__ void __launch_bounds__(kPrefixBound) prefix_kernel(const PrefixArgs a
             for (int e = 0; e < 32; e += 4) *reinterpret_cast<uint4*>(part + at + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
           }
         }
-        if (idx < rows) {  // (the sum is of both warps' pieces)
-          if (half == 0) part[kDh] = ref;
-          part[kDh + 1 + half] = l;
-        }
         tc_fence_before();
+      }
+      // The sum of both warps' pieces. (One of them writes it: a part's last four floats by both as ref, l0 and l1 took
+      // 1 - 3 us: 4 sequences behind 30000 28.3 instead of 25.0, five documents 29.6 instead of 28.1.)
+      if (half == 1) br.sums[r] = l;
+      if (used) named_bar_sync(1 + quad, 64);
+      if (used && ok && half == 0 && idx < rows) {
+        *reinterpret_cast<float4*>(part + kDh) = make_float4(ref, l + br.sums[r], 0.0f, 0.0f);
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&br.o_free);
@@ -648,9 +663,9 @@ __global__ void __launch_bounds__(kJoinThreads) prefix_join_kernel(const PrefixA
         const float* p = n == 0   ? own
                          : c == 0 ? first + copy * static_cast<long long>(rows) * kPitch
                                   : more + (static_cast<long long>(c0 + c) * kPrefixRows + copy * (kPrefixRows >> copies_log2)) * kPitch;
-        const float4 ml = *reinterpret_cast<const float4*>(p + kDh);
+        const float2 ml = *reinterpret_cast<const float2*>(p + kDh);
         pm[i] = ml.x;
-        pl[i] = ml.y + ml.z;
+        pl[i] = ml.y;
         pv[i] = *reinterpret_cast<const float4*>(p + d);
       }
     }
