@@ -23,9 +23,12 @@
 // of any size count against the largest p sv seen and not against fp16's range.
 //
 // What bounds it. 8 bits: HBM, 24 ragged sequences of up to 2048 x 40 heads 54 us, 0.74 of a copy's
-// rate (loads of single heads' rows; 16-bit rows, twice as long, reach 0.92). 4 bits: instructions, about 300 per
-// block of 16 positions of 128 (537 in the first version, with codes converted to whole numbers one by one),
-// 155 cycles of an SM against 93 of HBM: 128 sequences of up to 8190 x 8 heads 77 us, 0.56.
+// rate (loads of single heads' rows; 16-bit rows, twice as long, reach 0.92). 4 bits: instructions and their latencies at twelve
+// warps per SM, about 300 per block of 16 positions of 128 (537 in the first version, with codes converted to
+// whole numbers one by one), 155 cycles of an SM against 93 of HBM: 128 sequences of up to 8190 x 8 heads 77 us,
+// 0.56. Tiles of one block and four CTAs of 126 registers 87, of four blocks 84 - 108; values' nibbles too as what
+// fp16 reads in them, their 8s taken back by products with the weights 80, by sums per tile (23 instructions
+// fewer) 77, so not worth their rounding.
 #pragma once
 
 #include "p4q_paged.cuh"

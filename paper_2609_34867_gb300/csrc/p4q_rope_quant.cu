@@ -27,7 +27,8 @@ constexpr int kThreads = 256;
 // Items per thread, at most: eight share the index, the page and the angles (22528 x 120 heads 260 us;
 // four 288, sixteen 266 at four CTAs per SM).
 constexpr int kItems = 8;
-constexpr int kResident = 5;  // CTAs per SM (four 269 us, six 264)
+// CTAs per SM (four 269 us, six 264; the next head's loads ahead of this one's work: 273, at four 261)
+constexpr int kResident = 5;
 
 // Pairs (x, y) of four dimensions each turned by angles c, s, each operation rounded.
 __device__ __forceinline__ float2 turned(float x, float y, float c, float s) {
