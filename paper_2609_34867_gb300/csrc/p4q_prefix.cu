@@ -591,10 +591,11 @@ __global__ void __launch_bounds__(kPrefixBound) prefix_kernel(const PrefixArgs a
       }
       // The sum of both warps' pieces. (One of them writes it: a part's last four floats by both as ref, l0 and l1 took
       // 1 - 3 us: 4 sequences behind 30000 28.3 instead of 25.0, five documents 29.6 instead of 28.1.)
-      if (half == 1) br.sums[r] = l;
-      if (used) named_bar_sync(1 + quad, 64);
-      if (used && ok && half == 0 && idx < rows) {
-        *reinterpret_cast<float4*>(part + kDh) = make_float4(ref, l + br.sums[r], 0.0f, 0.0f);
+      if (used) {
+        if (half == 1) br.sums[r] = l;
+        named_bar_sync(1 + quad, 64);
+        if (ok && half == 0 && idx < rows)
+          *reinterpret_cast<float4*>(part + kDh) = make_float4(ref, l + br.sums[r], 0.0f, 0.0f);
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&br.o_free);
