@@ -117,8 +117,10 @@ def run_case(p4q, dev, T, seqs, H, Hkv, dh, rot, inter, dt, bits, page, order="s
     cache = make_cache(dev, seqs * cols + 5, page, Hkv, dh, bits, order)
     new = lambda n: torch.full((T, n + 8), SFILL, dtype=dtype, device=dev)[:, :n]  # noqa: E731
     q_out, k_out, v_out = (q, k, v) if in_place else (new(H * dh), new(Hkv * dh), new(Hkv * dh))
-    if not rows:
-        k_out = v_out = None
+    if rows in (False, "v"):
+        k_out = None
+    if rows in (False, "k"):
+        v_out = None
     up = lambda y: torch.from_numpy(np.ascontiguousarray(y)).to(dev)  # noqa: E731
     p4q.p4q_rope_append_quant(q, k, v, up(cos), up(sin), up(pos), *cache, up(table), q_out, k_out=k_out, v_out=v_out,
                               seq=up(seq) if use_seq else None, rot_pos=up(rp) if use_rot_pos else None, interleaved=inter)
@@ -172,6 +174,14 @@ def test_in_place_without_rows_and_defaults(p4q, dev, bits):
     run_case(p4q, dev, 77, 20, 8, 4, 64, 64, False, "bf16", bits, 16, in_place=True, rows=False, special=True)
     run_case(p4q, dev, 33, 33, 8, 4, 128, 64, True, "bf16", bits, 32, rows=False, use_seq=False, use_rot_pos=False)
     run_case(p4q, dev, 33, 40, 1, 1, 128, 128, False, "fp16", bits, 32, use_seq=False)
+
+
+@pytest.mark.parametrize("H,Hkv", [(40, 40), (1, 1), (33, 11), (3, 1), (128, 2)])
+def test_rows_of_keys_or_values_alone(p4q, dev, H, Hkv):
+    """Heads of q, k and v that a thread goes through one after the other, wherever its share begins."""
+    for rows in ("k", "v"):
+        run_case(p4q, dev, 70, 20, H, Hkv, 128, 128, False, "fp16", 4, 16, rows=rows)
+        run_case(p4q, dev, 70, 20, H, Hkv, 64, 32, True, "bf16", 8, 8, rows=rows, in_place=True)
 
 
 def test_every_pair_of_fp16_values_of_a_row(p4q, dev):
