@@ -233,6 +233,20 @@ def test_pages_groups_and_lengths_outside_their_ranges(p4q, dev):
     run(p4q, dev, d, status=8)
 
 
+@pytest.mark.parametrize("page", [16, 8])
+def test_offsets_past_32_bits(p4q, dev, page):
+    dh, Hkv = 64, 2
+    c = make(dev, [(70, [20, 5, -30]), (16, [9])], 8, Hkv, dh, page, "fp16", seed=12)
+    pages = c["k"].shape[0]
+    stride = (5 << 30) // (pages - 1) // 8 * 8  # elements: pages 5 G of them apart in all
+    for name in ("k", "v"):
+        room = torch.empty((stride * pages + page * Hkv * dh,), dtype=torch.float16, device=dev)
+        far = room.as_strided((pages, page, Hkv, dh), (stride, Hkv * dh, dh, 1))
+        far.copy_(c[name])
+        c[name] = far
+    check(c, *run(p4q, dev, c))
+
+
 def test_graphs_and_streams(p4q, dev):
     """A captured call replayed on other lengths and prefixes, and two streams with a workspace each."""
     a = make(dev, [(700, [90, 3, 40])], 8, 2, 128, 16, "fp16", seed=1)

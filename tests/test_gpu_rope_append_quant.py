@@ -233,6 +233,31 @@ def test_tokens_with_indices_outside_their_tables_are_not_written(p4q, dev):
         assert torch.equal(changed, want)
 
 
+@pytest.mark.parametrize("bits", [4, 8])
+def test_offsets_past_32_bits(p4q, dev, bits):
+    """The codes of a cache whose pages lie 5 GB apart in all are those of a small one."""
+    T, H, dh, page, pages = 90, 4, 128, 16, 9
+    near = make_cache(dev, pages, page, H, dh, bits)
+    width = near[0].shape[-1]
+    stride, sstride = (5 << 30) // (pages - 1) // 16 * 16, (5 << 28) // (pages - 1)
+    far = [torch.empty((stride * pages,), dtype=torch.uint8, device=dev).view(near[0].dtype).as_strided(
+        (pages, page, H, width), (stride, H * width, width, 1)) for _ in range(2)]
+    far += [torch.empty((sstride * pages,), device=dev).as_strided((pages, page, H), (sstride, 1, page)) for _ in range(2)]
+    for x, y in zip(far, near):
+        x.copy_(y)
+    g = torch.Generator(device=dev).manual_seed(3)
+    q = torch.randn((T, 3 * H * dh), generator=g, device=dev).half()
+    ang = torch.rand((128, 64), generator=g, device=dev)
+    pos = torch.arange(T, dtype=torch.int32, device=dev)
+    table = torch.tensor([[8, 3, 7, 0, 5, 2]], dtype=torch.int32, device=dev)
+    for cache in (near, far):
+        p4q.p4q_rope_append_quant(*q.split(H * dh, 1), ang.cos(), ang.sin(), pos, *cache, table, torch.empty_like(q[:, :H * dh]),
+                                  seq=torch.zeros_like(pos))
+    assert p4q.p4q_device_status() == 0
+    for x, y in zip(far, near):
+        assert torch.equal(x, y)
+
+
 def test_no_tokens_is_no_work(p4q, dev):
     cache = make_cache(dev, 2, 16, 2, 64, 4)
     q = torch.ones((0, 128), device=dev).half()
