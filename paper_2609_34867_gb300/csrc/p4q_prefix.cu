@@ -489,7 +489,7 @@ __global__ void __launch_bounds__(kPrefixBound) prefix_kernel(const PrefixArgs a
             }
             if (!(c2 > 0.0f)) {
 #pragma unroll
-              for (int e = 0; e < 32; ++e) s[e] = __float_as_uint(__uint_as_float(s[e]) * c2);
+              for (int e = 0; e < 32; ++e) s[e] = __float_as_uint(__fmul_rn(__uint_as_float(s[e]), c2));
             }
             float m4[4] = {top, top, top, top};
 #pragma unroll
@@ -498,7 +498,7 @@ __global__ void __launch_bounds__(kPrefixBound) prefix_kernel(const PrefixArgs a
           }
           // both warps have read all of their rows' scores: either overwrites only its own pieces with weights,
           // but the other one's maxima are of all
-          if (c2 > 0.0f) top *= c2;  // (rounding keeps the order: the largest product)
+          if (c2 > 0.0f) top = __fmul_rn(top, c2);  // (rounding keeps the order: the largest product)
           named_bar_sync(1 + quad, 64);
           float alpha = 1.0f;
           if (top > ref + kMove<kBf16>) {  // (-inf: the first score)
@@ -508,7 +508,6 @@ __global__ void __launch_bounds__(kPrefixBound) prefix_kernel(const PrefixArgs a
           }
           __syncwarp();
           const float from = ref == -INFINITY ? 0.0f : ref - kShift<kBf16>;
-          const float2 from2 = make_float2(-from, -from);
           float2 l2[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
 #pragma unroll 1
           for (int i = i0 + half; i < i1; i += 2) {
@@ -519,7 +518,11 @@ __global__ void __launch_bounds__(kPrefixBound) prefix_kernel(const PrefixArgs a
             auto weights = [&](auto whole) {
 #pragma unroll
               for (int e = 0; e < 16; e += 2) {
-                float2 x = __ffma2_rn(make_float2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), c22, from2);
+                // Scores are rounded as the reference is, before it is taken off: in one fma the largest would be off the
+                // reference by half a place of fp32, which from 2^24 on is more than the powers have room for. (Two
+                // sums: the compiler makes one fma of a packed product and a packed sum.)
+                const float2 y = __fmul2_rn(make_float2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), c22);
+                float2 x = make_float2(__fsub_rn(y.x, from), __fsub_rn(y.y, from));
                 if constexpr (!decltype(whole)::value) {
                   if (!(v >> e & 1u)) x.x = -INFINITY;
                   if (!(v >> e & 2u)) x.y = -INFINITY;
