@@ -473,10 +473,11 @@ struct Codes {
             for (int r = 0; r < kRep; ++r) m = fmaxf(m, fmaxf(s[r][n][e], s[r][n][e + 2]));
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
-            const float alpha = m == top[n][e] ? 1.0f : exp2_fast((top[n][e] - m) * fq[n][e]);
+            const float to = m == -INFINITY ? 0.0f : __fmul_rn(-m, fq[n][e]);
+            const float alpha = m == top[n][e] ? 1.0f : top[n][e] == -INFINITY ? 0.0f : exp2_fast(__fsub_rn(to, back_to[n][e]));
             top[n][e] = m;
             limit[n][e] = m == -INFINITY ? -INFINITY : m + kMove / fq[n][e];
-            back_to[n][e] = m == -INFINITY ? 0.0f : -m * fq[n][e];
+            back_to[n][e] = to;
             l[n][e] *= alpha;
 #pragma unroll
             for (int hh = 0; hh < kVc; ++hh)
@@ -497,7 +498,8 @@ struct Codes {
           for (int r = 0; r < kRep; ++r)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const float p = exp2_fast(fmaf(s[r][n][2 * e + i], fq[n][i], back_to[n][i]));
+              // (rounded as the reference is: one fma would leave half a place of fp32, from 2^31 on more than p has room for)
+              const float p = exp2_fast(__fadd_rn(__fmul_rn(s[r][n][2 * e + i], fq[n][i]), back_to[n][i]));
               l[n][i] += p;
               s[r][n][2 * e + i] = p * sv[r][e];
               move = move || fabsf(s[r][n][2 * e + i]) > room[n][i];
@@ -594,7 +596,7 @@ struct Codes {
     for (int n = 0; n < kNt; ++n)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        acc.ref[n][i] = top[n][i] * fq[n][i];
+        acc.ref[n][i] = __fmul_rn(top[n][i], fq[n][i]);
         const float back = room[n][i] == 0.0f ? 1.0f : room[n][i] * 0x1p-15f;  // 1 / wf
 #pragma unroll
         for (int hh = 0; hh < kVc; ++hh)
