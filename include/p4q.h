@@ -625,7 +625,8 @@ p4q_status p4q_rope_append_quant(const uint16_t* q, int ldq, const uint16_t* k, 
 
 /* p4q_paged_attention over a cache of codes; q and o of type dtype, P4Q_F16 or
  * P4Q_BF16. Scores are (scale log2 e s_j) (q . c_j) with whole codes c_j; the
- * weights times the values' scales enter the product with the codes in 22 bits.
+ * weights times the values' scales enter the product with the codes in 22 bits (and not below
+ * 2^-34 of the largest such weight of the head).
  * fp32 products, softmax and sums; o rounded once. Scales may have any sign. q enters the
  * products in 16 bits: values below 2^-25 of the largest of their head may lose bits (2^-35 of
  * that one at most). What is not finite in a head's q, or 2^118

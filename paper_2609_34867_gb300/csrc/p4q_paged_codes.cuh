@@ -19,8 +19,8 @@
 // q enters the product in fp16: with 8 bits q of fp16 as it is, else times the power of two that
 // brings its head's largest finite value below 2^15: exact where |q| is not below 2^-25 of that one, and
 // off by less than 2^-35 of it elsewhere. The weights p sv enter theirs as two fp16 values (22 bits)
-// times a power of two per head that moves like the softmax's reference, so scales
-// of any size count against the largest p sv seen and not against fp16's range.
+// times a power of two per head that moves like the softmax's reference and with it, so scales of any
+// size count against the largest p sv seen, each at its weight now, and not against fp16's range.
 //
 // What bounds it. 8 bits: HBM, 24 ragged sequences of up to 2048 x 40 heads 54 us, 0.74 of a copy's
 // rate (loads of single heads' rows; 16-bit rows, twice as long, reach 0.92). 4 bits: instructions and their latencies at twelve
@@ -479,12 +479,22 @@ struct Codes {
             limit[n][e] = m == -INFINITY ? -INFINITY : m + kMove / fq[n][e];
             back_to[n][e] = to;
             l[n][e] *= alpha;
+            // the largest p sv so far follows the reference, and the weights' factor with it: by the power of two
+            // above alpha (within what fp32 has), the rest by which o gets smaller is between 1/2 and 1
+            float back = alpha;
+            if (alpha < 1.0f && room[n][e] > 0.0f) {
+              const int r = static_cast<int>(__float_as_uint(room[n][e]) >> 23) - 127;
+              const int to_r = max(-105, r + static_cast<int>(__float_as_uint(alpha) >> 23) - 126);
+              room[n][e] = __uint_as_float(static_cast<uint32_t>(127 + to_r) << 23);
+              wf[n][e] = __uint_as_float(static_cast<uint32_t>(127 + 15 - to_r) << 23);
+              back *= __uint_as_float(static_cast<uint32_t>(127 + r - to_r) << 23);
+            }
 #pragma unroll
             for (int hh = 0; hh < kVc; ++hh)
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
-                o[n][hh][j][e] *= alpha;
-                o[n][hh][j][e + 2] *= alpha;
+                o[n][hh][j][e] *= back;
+                o[n][hh][j][e + 2] *= back;
               }
           }
       }
