@@ -2,7 +2,8 @@
 
 Each .cu under csrc/ is compiled in parallel for sm_103a only, then linked
 into paper_2609_34867_gb300/lib/libp4q.so; the Python module of csrc/p4q_call.c, which
-marshals the calls of a decode step, goes beside it. No fast-math: the quantizer and the
+marshals the calls of a decode step, goes beside it where there are Python's headers to compile
+it (without it the binding marshals these calls through ctypes). No fast-math: the quantizer and the
 cosine rely on IEEE-rounded fp32 division and square root.
 """
 from __future__ import annotations
@@ -39,11 +40,44 @@ def _deps():
         glob.glob(os.path.join(INCLUDE, "*.h")) + glob.glob(os.path.join(CSRC, "*.c"))
 
 
+def python_headers():
+    """The folder of Python.h, None where Python has none (they are a package of their own in most systems)."""
+    path = sysconfig.get_paths()["include"]
+    return path if os.path.exists(os.path.join(path, "Python.h")) else None
+
+
 def up_to_date() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(CALL):
+    built = [LIB, CALL] if python_headers() else [LIB]
+    if not all(os.path.exists(p) for p in built):
         return False
-    t = min(os.path.getmtime(LIB), os.path.getmtime(CALL))
+    t = min(os.path.getmtime(p) for p in built)
     return all(os.path.getmtime(p) <= t for p in _deps())
+
+
+def _start_call(verbose: bool):
+    """The compiler at work on csrc/p4q_call.c and the file that it writes; None without Python's headers."""
+    headers = python_headers()
+    if headers is None:
+        print(f"no Python.h in {sysconfig.get_paths()['include']}: calls of a decode step go through ctypes", file=sys.stderr)
+        return None
+    tmp = f"{CALL}.tmp{os.getpid()}"
+    cmd = [shutil.which("gcc") or "cc", "-O2", "-Wall", "-shared", "-fPIC", "-I", headers, "-I", INCLUDE,
+           os.path.join(CSRC, "p4q_call.c"), "-o", tmp]
+    if verbose:
+        print(" ".join(cmd), file=sys.stderr)
+    return subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True), tmp
+
+
+def _finish_call(started) -> None:
+    if started is None:
+        if os.path.exists(CALL):  # (of another source, perhaps)
+            os.remove(CALL)
+        return
+    p, tmp = started
+    out, _ = p.communicate()
+    if p.returncode:
+        raise RuntimeError(f"the C compiler failed for p4q_call.c (libp4q.so is built):\n{out}")
+    os.replace(tmp, CALL)
 
 
 def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) -> str:
@@ -64,11 +98,7 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
         if verbose:
             print(" ".join(cmd), file=sys.stderr)
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
-    call = f"{CALL}.tmp{os.getpid()}"
-    src = os.path.join(CSRC, "p4q_call.c")
-    cmd = [shutil.which("gcc") or "cc", "-O2", "-Wall", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"], "-I", INCLUDE,
-           src, "-o", call]
-    procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+    call = _start_call(verbose)
     failed = []
     for src, p in procs:
         out, _ = p.communicate()
@@ -82,7 +112,7 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
     # every symbol resolved at link time (a missing definition fails here, not at load)
     subprocess.run([nvcc(), GENCODE, "-shared", "-Xlinker", "--no-undefined", "-o", tmp] + objs, check=True)
     os.replace(tmp, LIB)
-    os.replace(call, CALL)
+    _finish_call(call)
     return LIB
 
 

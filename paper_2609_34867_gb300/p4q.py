@@ -6,7 +6,8 @@ work runs in the library's sm_103a kernels. A missing library raises: there is
 no fallback path. Decoding over caches of codes and behind shared prefixes, where a
 call's time on the host counts, goes through a small C module that does the same
 marshalling (csrc/p4q_call.c; attention of one sequence 11.5 us without it, 7 with
-it); arguments that it does not take are checked here and refused with a message.
+it); arguments that it does not take are checked here and refused with a message. Where it could
+not be compiled, for want of Python's headers, these calls are marshalled here as all others are.
 """
 from __future__ import annotations
 
@@ -137,6 +138,11 @@ def lib() -> ctypes.CDLL:
 _fast = None
 
 
+class _NoCall:
+    """In the C module's place where there is none: leaves every call to the wrapper."""
+    rope_append_quant = paged_attention_quant = prefix_attention = staticmethod(lambda *args: -1)
+
+
 def _call():
     """csrc/p4q_call.c, bound to the library: the calls that sit in a decode loop. Its functions take
     a wrapper's arguments by position and give the status, or -1 for arguments that the
@@ -144,6 +150,9 @@ def _call():
     global _fast
     if _fast is None:
         L = lib()
+        if not os.path.exists(_build.CALL):
+            _fast = _NoCall
+            return _fast
         loader = importlib.machinery.ExtensionFileLoader("p4q_call", _build.CALL)
         module = importlib.util.module_from_spec(importlib.util.spec_from_loader("p4q_call", loader))
         loader.exec_module(module)
