@@ -104,8 +104,8 @@ class Decoder:
 
 class Cache:
     """Paged keys and values of every layer for `seqs` sequences of up to `most` positions: fp16, or codes of 8 or 4
-    bits with their scales. answers > 1: each so many sequences share their first `prompt` positions, which the
-    first of them has in its pages."""
+    bits with their scales. answers > 1: each so many sequences share their first `prompt` positions, whose whole
+    pages only the first of them has."""
 
     def __init__(self, decoder: Decoder, seqs: int, most: int, positions: int, seed: int = 0, bits: int = 16,
                  answers: int = 1, prompt: int = 0):
@@ -113,10 +113,14 @@ class Cache:
         if answers > 1 and bits != 16:
             raise ValueError("several answers share a prompt in a cache of 16 bits only")
         per = (most + c.page - 1) // c.page
-        pages = seqs * per
+        # pages that lie whole within a shared prompt: of the first answer to it only (the others' are not looked at)
+        has = torch.ones((seqs, per), dtype=torch.bool, device="cuda")
+        has.view(seqs // answers, answers, per)[:, 1:, :prompt // c.page] = False
+        pages = seqs * per - (seqs - seqs // answers) * (prompt // c.page)
         g = torch.Generator(device="cuda").manual_seed(seed)
         # pages in no order, as a running server's free list leaves them
-        self.table = torch.randperm(pages, generator=g, device="cuda").to(torch.int32).view(seqs, per)
+        self.table = torch.full((seqs, per), -1, dtype=torch.int32, device="cuda")
+        self.table[has] = torch.randperm(pages, generator=g, device="cuda").to(torch.int32)
         self.bits, self.answers = bits, answers
         if bits == 16:
             shape = (c.layers, pages, c.page, c.kv_heads, 128)
