@@ -655,7 +655,14 @@ p4q_status p4q_paged_attention_quant(const uint16_t* q, int ldq, int H, const p4
  *   ws    device workspace of p4q_prefix_attention_workspace_bytes() bytes for
  *         these seqs, groups, H and dh (never less for more of one of them)
  * Requires 1 <= groups <= kv->seqs, kv->seqs * H < 2^31 - 255. Other arguments, rules and precision as
- * p4q_paged_attention. */
+ * p4q_paged_attention, and one thing more: a group's rows of queries (sequences times query heads per key/value head)
+ * go in tiles of 128, and in a tile of 64 rows and fewer each of up to 3/4 of the prefix's positions adds a least weight
+ * besides its own (0 would make NaN of an infinite value): below 2^-124 of the weight at the largest score in
+ * bf16, 2^-34 of it in fp16 (2^-23 where scores, in powers of two, are 2^28 and above).
+ * Meant for prefixes that are long against what is behind them: positions that are not a shared prefix's (those of
+ * a sequence of its own, or of one that ends in the prefix, among them) are dealt by sequence and key/value head, to eight
+ * CTAs at most and to one in a large batch, so one sequence far longer than the others holds
+ * the call up, where p4q_paged_attention deals its positions to all. */
 size_t p4q_prefix_attention_workspace_bytes(int seqs, int groups, int H, int dh);
 p4q_status p4q_prefix_attention(const uint16_t* q, int ldq, int H, const p4q_paged_kv* kv, const int32_t* lens,
                                 const int32_t* group_start, const int32_t* prefix_lens, int groups, float scale,

@@ -52,8 +52,11 @@ __device__ __forceinline__ float exp2_fast(float x) {
 }
 
 // For a kernel that reads what the stream's earlier kernels wrote without waiting for the one before it, which writes
-// none of that: the one before has waited for all of them before it let this one begin, so they
-// are complete; what this SM's L1 may still have of their data from before is given up here.
+// none of that: the one before has waited for all of them (griddepcontrol.wait: they are complete, and what they
+// wrote is performed) before it let this one begin, in every thread of its CTAs; what this SM's L1 may still have of their data
+// from before is given up here. What it rests on: a launch that griddepcontrol.launch_dependents releases is
+// promised no sight of anything by itself; that it begins behind the instruction that released it, and
+// that the fence drops this SM's older lines, is what makes it see writes performed before.
 __device__ __forceinline__ void see_earlier_kernels() { __threadfence(); }
 
 // What a unit is to the part of the kernel that goes through its tiles: heads h0 ..

@@ -22,13 +22,14 @@
 // times a power of two per head that moves like the softmax's reference and with it, so scales of any
 // size count against the largest p sv seen, each at its weight now, and not against fp16's range.
 //
-// What bounds it. 8 bits: HBM, 24 ragged sequences of up to 2048 x 40 heads 54 us, 0.74 of a copy's
-// rate (loads of single heads' rows; 16-bit rows, twice as long, reach 0.92). 4 bits: instructions and their latencies at twelve
+// What bounds it. 8 bits: HBM, 24 ragged sequences of up to 2048 x 40 heads 52 - 55 us, 0.72 - 0.77 of a copy's
+// rate (loads of single heads' rows by two stages; 16-bit rows, twice as long, reach 0.92). 4 bits: instructions and their latencies at twelve
 // warps per SM, about 300 per block of 16 positions of 128 (537 in the first version, with codes converted to
-// whole numbers one by one), 155 cycles of an SM against 93 of HBM: 128 sequences of up to 8190 x 8 heads 77 us,
-// 0.56. Tiles of one block and four CTAs of 126 registers 87, of four blocks 84 - 108; values' nibbles too as what
-// fp16 reads in them, their 8s taken back by products with the weights 80, by sums per tile (23 instructions
-// fewer) 77, so not worth their rounding.
+// whole numbers one by one), 158 cycles of an SM against 93 of HBM: 128 sequences of up to 8190 x 8 heads 79 us,
+// 0.55 (77.5 with scores that were not rounded before the reference is taken off and a factor of the weights that did
+// not follow it). Tried at 77: tiles of one block and four CTAs of 126 registers 87, of four blocks 84 - 108; values'
+// nibbles too as what fp16 reads in them, their 8s taken back by products with the weights 80, by sums per tile (23
+// instructions fewer) 77, so not worth their rounding.
 #pragma once
 
 #include "p4q_paged.cuh"

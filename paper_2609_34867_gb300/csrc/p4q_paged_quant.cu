@@ -10,7 +10,7 @@ template <int kBits, int kDh, bool kSmall>
 cudaError_t launch_for(const QuantAttnArgs& a, cudaStream_t stream, unsigned int* launches) {
   const int group = a.H / a.kv.Hkv;
   // 8-bit rows of 64 bytes: two heads of a line of HBM to a CTA (64 sequences of up to 4096 x 40 heads of 64
-  // 135 us; one, fetched as half lines 165, as whole ones 141). 4-bit codes are bound by instructions before
+  // 135 us, on other GPUs to 144; on the first, with one head to a CTA, fetched as half lines 165, as whole ones 141). 4-bit codes are bound by instructions before
   // that, and finer units are better (128 of up to 8190 x 8 heads 79.5 us, two to a CTA 84.8).
   constexpr bool kTwo = kBits == 8 && kDh == 64;
   if (kTwo && a.kv.Hkv % 2 == 0 && group <= 8)

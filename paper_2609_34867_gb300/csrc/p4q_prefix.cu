@@ -23,7 +23,7 @@
 //   warps 0-3  queries, keys and values into shared memory with 16-byte asynchronous copies (pages
 //              may be of any size and order, and positions past the prefix or of a page outside the
 //              cache have to be zeros: 0 weight times an infinite value is NaN), in the 128-byte
-//              swizzle that the products read; two stages each of keys and values;
+//              swizzle that the products read; three stages of keys, two of values;
 //   warps 4-11 two threads per row (its TMEM lane): scores' maximum, p = 2^(s - reference),
 //              their sum, p as two fp16 or three bf16 values over the scores in TMEM; the
 //              reference moves, and O with it, only when a score exceeds it by 2^4 (bf16 2^8);
@@ -46,8 +46,9 @@ __device__ unsigned int g_prefix_wait_err;
 constexpr int kProducers = 4, kSoftmax = 8;          // warps
 constexpr int kMmaWarp = kProducers + kSoftmax;
 constexpr int kPrefixThreads = 32 * (kMmaWarp + 1);
-// (more threads than there are: 80 registers for each, which leave a warp of the own positions' kernel room on
-// every quarter of the SM)
+// (more threads than there are: 80 registers for each, which leave 192 for each thread of one more warp on the quarter
+// of the SM that has four of these: room for the own positions' kernel of up to 8 heads per key/value head (164 - 168),
+// not for the one of more (210 - 252), which has what SMs without a CTA of the prefix leave it)
 constexpr int kPrefixBound = 768;
 constexpr int kMaxPrefixGrid = 160;
 constexpr int kTileBytes = 16384;                    // 128 rows of 128 bytes
@@ -425,7 +426,7 @@ __global__ void __launch_bounds__(kPrefixBound) prefix_kernel(const PrefixArgs a
     // A tile of 32 rows and less stands in the products four times, of 64 and less twice; each copy
     // has weights for its share of a chunk's positions only, so that all warps work on them, and leaves
     // a part of its own. (For the others a copy has the least weights there are, not 0, which
-    // would make NaN of an infinite value: 2^-34 of that at the reference in fp16, 2^-125 in bf16.)
+    // would make NaN of an infinite value: 2^-34 of that at the reference in fp16, below 2^-124 in bf16.)
     constexpr uint32_t kNone = kBf16 ? 0x00800080u : 0x00010001u;
     constexpr int kPieces = kPrefixChunk / 16;
     const int quad = warp & 3, half = (warp - kProducers) >> 2, r = quad * 32 + lane;
@@ -746,8 +747,8 @@ cudaError_t launch_prefix(const PrefixArgs& a, cudaStream_t stream, unsigned int
   else
     e = wide ? launch<Rows<kBf16, kDh, false, true>, 2>(a, stream, launches) : launch<Rows<kBf16, kDh, false, true>, 1>(a, stream, launches);
   if (e != cudaSuccess) return e;
-  // four warps per head, of many heads two (us, with four, two, one: 64 x 32 heads of 6 parts 39.4, 36.8, 37.1; 96 x 24 of
-  // 64 dimensions and up to 20 40.4, 38.8, 40.4; 4 x 8 of 120 28.0, 37.6)
+  // four warps per head, of many heads two (us, with four, two, one: 64 x 32 heads of 6 parts 39.4, 36.9, 36.7; 96 x 24 of
+  // 64 dimensions and up to 20 28.7, 28.8, 29.4; 32 x 32 of up to 4 119.7, 120.6, 121.3; 4 x 8 of 120 24.6, 28.9, 37.9)
   const long long rows = static_cast<long long>(a.kv.seqs) * a.H;
   constexpr int kSides = kDh == 64 ? 2 : 1;
   const bool few = rows <= 8ll * num_sms();
